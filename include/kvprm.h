@@ -10,11 +10,11 @@
  *
  * Conventions for every entry point
  *   - All tensor pointers are DEVICE pointers unless the name ends in _host. The caller owns
- *     every buffer; the library never frees, never writes the cache (except kvprm_steer, which
- *     exists to update it), the page table or the weights, and never allocates device memory
- *     in any call (the caller passes a workspace sized by the matching kvprm_workspace_size*
- *     query), so every scoring call can be captured in a HIP graph (no memset nodes either;
- *     not in the KVPRM_DEBUG mode below, which synchronises).
+ *     every buffer; the library never frees, never writes the cache (except kvprm_steer and
+ *     kvprm_write_kv, which exist to update it), the page table or the weights, and never
+ *     allocates device memory in any call (the caller passes a workspace sized by the matching
+ *     kvprm_workspace_size* query), so every call but kvprm_create can be captured in a HIP
+ *     graph (no memset nodes either; not in the KVPRM_DEBUG mode below, which synchronises).
  *   - Calls only enqueue work on `stream` (a hipStream_t; NULL = the null stream) and never
  *     synchronise the host. Outputs are valid once the stream reaches that point.
  *   - Arguments are validated on the host before anything is enqueued; on any error nothing
@@ -304,9 +304,8 @@ kvprm_status kvprm_score_grad(kvprm_handle h, const kvprm_kv_cache *cache,
 
 /* KV Steering (appendix algorithm): `steps` times, every cached key and value the candidates
  * read (slots 0..L_b-1) becomes round_bf16(kv - eta * d(-log P(+))/d kv), the gradient taken at
- * the cache as it is at that step. The pools of `cache` are WRITTEN in place (the only entry
- * point that writes the cache). scores_before[b] = P(+) before the first step, scores_after[b]
- * = P(+) after the last (device fp32 [B]). Requirements as for kvprm_score_grad; steps >= 1. */
+ * the cache as it is at that step. The pools of `cache` are WRITTEN in place. scores_before[b]
+ * = P(+) before the first step, scores_after[b] = P(+) after the last (device fp32 [B]). Requirements as for kvprm_score_grad; steps >= 1. */
 kvprm_status kvprm_steer(kvprm_handle h, const kvprm_kv_cache *cache, const kvprm_batch *batch,
                          const kvprm_readout_weights *weights, float eta, int32_t steps,
                          void *workspace, size_t ws_bytes, float *scores_before,
@@ -339,6 +338,136 @@ typedef enum { KVPRM_KEYS = 0, KVPRM_VALUES = 1 } kvprm_kv_part;
  * does nothing. Nothing is allocated; enqueued on `stream`. */
 kvprm_status kvprm_pack_kv(const void *src, void *dst, int64_t num_tiles, int32_t head_dim,
                            kvprm_dtype dtype, kvprm_kv_part part, void *stream);
+
+/* ---------------------------------------------------------------- a cache that grows
+ * The calls below serve a generator that verifies trees of drafted tokens over the cache it lets
+ * this library score: rotate queries and keys, attend from every drafted token to the cached
+ * tokens and its ancestors, write the accepted tokens' keys and values into the pages, read
+ * cached tokens back.
+ * Rows are token-major vectors of dtype F32 or BF16. Row strides are in elements. */
+
+typedef enum {
+  KVPRM_ROPE_HALF = 0,       /* pair i = dims i and i + rotary_dim / 2 */
+  KVPRM_ROPE_INTERLEAVED = 1 /* pair i = dims 2i and 2i + 1 */
+} kvprm_rope_layout;
+
+/* How the frequencies f_i = theta^(-2i / rotary_dim) are changed for contexts of `factor` times
+ * the trained length. turns_i = trained_len * f_i / (2 pi). */
+typedef enum {
+  KVPRM_ROPE_NONE = 0,
+  KVPRM_ROPE_LINEAR = 1, /* f_i / factor: positions interpolated */
+  KVPRM_ROPE_BASE = 2,   /* theta * factor^(n / (n - 2)) in theta's place, n = rotary_dim */
+  /* f_i (w + (1 - w) / factor) with w = clamp((turns_i - low) / (high - low), 0, 1): slow pairs
+   * interpolated, fast ones left (NTK-by-parts of YaRN, arXiv 2309.00071) */
+  KVPRM_ROPE_PARTS = 3,
+  /* the same with the ramp over the pair index: w = 1 - clamp((i - a) / max(b - a, 0.001), 0, 1),
+   * a = max(floor(at(high)), 0), b = min(ceil(at(low)), n - 1), where at(t) = n ln(trained_len /
+   * (2 pi t)) / (2 ln theta) is the pair that makes t turns */
+  KVPRM_ROPE_RAMP = 4
+} kvprm_rope_scaling;
+
+typedef struct {
+  int32_t head_dim;   /* even, 2 to 256 */
+  int32_t rotary_dim; /* even, 2 to head_dim: the first rotary_dim dims are rotated, the others kept */
+  kvprm_rope_layout layout;
+  kvprm_rope_scaling scaling;
+  double theta;       /* > 1 */
+  double factor;      /* >= 1 (not read for NONE) */
+  double trained_len; /* > 0 (PARTS and RAMP only, as low and high) */
+  double low, high;   /* turns, 0 < low < high */
+  double magnitude;   /* factor on the rotated values (1: a rotation), finite */
+} kvprm_rope;
+
+/* One tensor to rotate: `heads` heads of head_dim values side by side in each row. */
+typedef struct {
+  const void *src;
+  void *dst;
+  int32_t heads;
+  int64_t src_stride, dst_stride; /* >= heads * head_dim */
+} kvprm_rope_heads;
+
+/* dst = magnitude * R(p f) src for every row and head of num_parts (1 or 2: queries and keys)
+ * tensors of `rows` rows, p = positions[row] (device int32, any value): pair (a, b) becomes
+ * (a cos - b sin, b cos + a sin) with angle p f_i. transpose != 0 applies magnitude * R^T, the
+ * gradient of the rotation (sines negated). Angles are formed in 64 bits, products in 32, each
+ * result is rounded once. dst may be src (same stride); otherwise the rows written must not be
+ * rows read. KVPRM_E_INVALID: a null or misaligned pointer (element size), a stride below the
+ * row, overlapping src and dst, values outside the ranges above. rows = 0 does nothing. */
+kvprm_status kvprm_rotary(const kvprm_rope *rope, kvprm_dtype dtype, int64_t rows,
+                          const int32_t *positions, const kvprm_rope_heads *parts,
+                          int32_t num_parts, int32_t transpose, void *stream);
+
+/* Rows of keys and values beside the cache, [rows][num_kv_heads][head_dim]. Candidate b of the
+ * batch owns places start[b] .. start[b + 1] - 1; place i is row i, or row index[i].
+ * Pointers 16-byte aligned, strides multiples of 16 bytes and >= num_kv_heads * head_dim. */
+typedef struct {
+  void *k, *v;
+  kvprm_dtype dtype;          /* F32 or BF16 */
+  int64_t k_stride, v_stride;
+  int64_t num_rows;           /* rows of k and v: no row at or past it is touched */
+  const int32_t *start;       /* device [B + 1], not decreasing */
+  const int32_t *index;       /* device [start[B]], or NULL */
+  int32_t max_rows;           /* no candidate has more rows (sizes the launch; rows past it are dropped) */
+} kvprm_kv_rows;
+
+/* Appends rows to the cache of one layer: row i of candidate b becomes the token at position
+ * lengths[b] + i (lengths as they are before the call; the caller raises them afterwards), in the
+ * stored tile layouts, rounded to the cache's type (nearest even). The pools (and, for fp8, the
+ * scales) of `cache` are WRITTEN; other slots and pages keep their bytes, but for this:
+ * an fp8 tile's scale becomes the smallest power of two s >= 2^-100 with 448 s >= |x| for every
+ * new x of the tile, at least its present scale (rounded up to a power of two) if the page holds
+ * earlier tokens, whose codes are then rounded to the new scale where it changes. A power of two
+ * costs no significant bit on either way, so that a code is rounded again only where it leaves e4m3's
+ * normal range. Infinities and NaN are stored as NaN in fp8 (and do not enter the scale).
+ * Rows past max_pages * 16 tokens, with a row number outside [0, num_rows) or whose page id is outside
+ * [0, num_pages) are dropped. No page may get rows of two candidates (checked with KVPRM_DEBUG=1).
+ * The prefix-sharing hint is not read. */
+kvprm_status kvprm_write_kv(kvprm_handle h, const kvprm_kv_cache *cache, const kvprm_batch *batch,
+                            int32_t layer, const kvprm_kv_rows *rows, void *stream);
+
+/* Reads cached tokens of one layer back: row i of candidate b receives the key and value at
+ * position first[b] + i (first: device [B], or NULL for 0), code times scale for fp8, rounded to
+ * the rows' type. Rows of positions outside [0, lengths[b]), rows past max_rows or num_rows and rows
+ * that no candidate owns are left as they are. index must be NULL (KVPRM_E_INVALID). k or v may be
+ * NULL (that part is not read). The prefix-sharing hint is not read. */
+kvprm_status kvprm_read_kv(kvprm_handle h, const kvprm_kv_cache *cache, const kvprm_batch *batch,
+                           int32_t layer, const kvprm_kv_rows *rows, const int32_t *first,
+                           void *stream);
+
+/* Drafted tokens of every candidate, one row each, packed: candidate b owns rows start[b] ..
+ * start[b + 1] - 1 (its tokens 0, 1, ...). All four arrays have `dtype`; pointers 16-byte aligned,
+ * strides multiples of 16 bytes and at least a row. */
+typedef struct {
+  const void *q;              /* [rows][num_q_heads][head_dim], rotated */
+  const void *k, *v;          /* [rows][num_kv_heads][head_dim], keys rotated */
+  void *o;                    /* [rows][num_q_heads][head_dim] */
+  kvprm_dtype dtype;          /* F32 or BF16 */
+  int64_t q_stride, k_stride, v_stride, o_stride;
+  int64_t num_rows;           /* rows of the arrays: no row at or past it is touched */
+  const int32_t *start;       /* device [B + 1], not decreasing */
+  int32_t max_rows;           /* 1 to 256: no candidate has more tokens (rows past it are dropped) */
+  /* Which drafted tokens each one attends to: bit t % 32 of word t / 32 of row r's mask_words
+   * words is token t of the same candidate (itself and its ancestors, in a tree; any set is
+   * allowed, bits past the candidate's tokens are not read). NULL: tokens 0 .. its own (a chain). */
+  const uint32_t *mask;       /* device [rows][mask_words], or NULL */
+  int32_t mask_words;         /* >= ceil(max_rows / 32) with a mask */
+} kvprm_tree;
+
+/* Bytes of device workspace kvprm_attention_tree needs (from the batch's size and max_pages, and the
+ * tree's num_rows, max_rows and dtype alone). */
+kvprm_status kvprm_workspace_size_tree(kvprm_handle h, const kvprm_batch *batch,
+                                       const kvprm_tree *tree, size_t *bytes);
+
+/* Attention of drafted tokens over the cache of one layer: for every drafted token and q-head,
+ * o = softmax(q K^T / sqrt(d_h)) V over the candidate's lengths[b] cached tokens and the drafted
+ * tokens of its mask. A token that attends to nothing gets zeros. Keys and values that a token
+ * does not attend to never reach its output, whatever they hold (infinities, NaN). Scores, the softmax and the
+ * sums are fp32; F32 rows keep 24 bits of q and of the probabilities, BF16 rows 16 bits of the
+ * probabilities. The cache is not written. Rows that no candidate owns are left as they are.
+ * Conventions as for kvprm_attention; the prefix-sharing hint is not read. */
+kvprm_status kvprm_attention_tree(kvprm_handle h, const kvprm_kv_cache *cache,
+                                  const kvprm_batch *batch, int32_t layer, const kvprm_tree *tree,
+                                  void *workspace, size_t ws_bytes, void *stream);
 
 /* Diagnostic (measurement, not part of scoring): read `bytes` of device memory at `buf` once,
  * with the access pattern of the cache and weight streams (16-byte non-temporal loads, 512

@@ -24,9 +24,13 @@ EXPORTED = ["kvprm_create", "kvprm_destroy", "kvprm_workspace_size", "kvprm_scor
             "kvprm_attention", "kvprm_attention_partials", "kvprm_pack_weight",
             "kvprm_workspace_size_lora", "kvprm_score_lora", "kvprm_workspace_size_ex",
             "kvprm_score_ex", "kvprm_workspace_size_grad", "kvprm_score_grad", "kvprm_steer",
-            "kvprm_stream_read", "kvprm_score_static", "kvprm_pack_kv", "kvprm_last_error"]
+            "kvprm_stream_read", "kvprm_score_static", "kvprm_pack_kv", "kvprm_rotary",
+            "kvprm_write_kv", "kvprm_read_kv", "kvprm_workspace_size_tree",
+            "kvprm_attention_tree", "kvprm_last_error"]
 KVPRM_KEYS, KVPRM_VALUES = 0, 1
 STATIC_WORKSPACE_BYTES = 64 << 20  # KVPRM_STATIC_WORKSPACE_BYTES
+ROPE_LAYOUT = {"half": 0, "interleaved": 1}
+ROPE_SCALING = {"none": 0, "linear": 1, "base": 2, "parts": 3, "ramp": 4}
 LORA_PROJECTIONS = ("q", "k", "v", "o", "gate", "up", "down")
 
 
@@ -80,6 +84,35 @@ class Batch(ctypes.Structure):
                 ("num_groups", ctypes.c_int32),
                 ("group_start_host", ctypes.POINTER(ctypes.c_int32)),
                 ("group_prefix_len_host", ctypes.POINTER(ctypes.c_int32))]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+                ("layout", ctypes.c_int), ("scaling", ctypes.c_int), ("theta", ctypes.c_double),
+                ("factor", ctypes.c_double), ("trained_len", ctypes.c_double),
+                ("low", ctypes.c_double), ("high", ctypes.c_double),
+                ("magnitude", ctypes.c_double)]
+
+
+class RopeHeads(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("heads", ctypes.c_int32),
+                ("src_stride", ctypes.c_int64), ("dst_stride", ctypes.c_int64)]
+
+
+class KVRows(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("dtype", ctypes.c_int),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("num_rows", ctypes.c_int64), ("start", ctypes.c_void_p),
+                ("index", ctypes.c_void_p), ("max_rows", ctypes.c_int32)]
+
+
+class Tree(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("o", ctypes.c_void_p), ("dtype", ctypes.c_int), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("o_stride", ctypes.c_int64), ("num_rows", ctypes.c_int64),
+                ("start", ctypes.c_void_p), ("max_rows", ctypes.c_int32),
+                ("mask", ctypes.c_void_p), ("mask_words", ctypes.c_int32)]
 
 
 class KvprmError(RuntimeError):
@@ -138,11 +171,23 @@ def _load():
     lib.kvprm_steer.argtypes = [vp, ctypes.POINTER(KVCache), ctypes.POINTER(Batch),
                                 ctypes.POINTER(ReadoutWeights), ctypes.c_float, ctypes.c_int32, vp,
                                 sz, vp, vp, vp]
+    lib.kvprm_rotary.argtypes = [ctypes.POINTER(Rope), ctypes.c_int, ctypes.c_int64, vp,
+                                 ctypes.POINTER(RopeHeads), ctypes.c_int32, ctypes.c_int32, vp]
+    lib.kvprm_write_kv.argtypes = [vp, ctypes.POINTER(KVCache), ctypes.POINTER(Batch),
+                                   ctypes.c_int32, ctypes.POINTER(KVRows), vp]
+    lib.kvprm_read_kv.argtypes = [vp, ctypes.POINTER(KVCache), ctypes.POINTER(Batch),
+                                  ctypes.c_int32, ctypes.POINTER(KVRows), vp, vp]
+    lib.kvprm_workspace_size_tree.argtypes = [vp, ctypes.POINTER(Batch), ctypes.POINTER(Tree),
+                                              ctypes.POINTER(sz)]
+    lib.kvprm_attention_tree.argtypes = [vp, ctypes.POINTER(KVCache), ctypes.POINTER(Batch),
+                                         ctypes.c_int32, ctypes.POINTER(Tree), vp, sz, vp]
     for f in ("kvprm_create", "kvprm_destroy", "kvprm_workspace_size", "kvprm_score",
               "kvprm_attention", "kvprm_attention_partials", "kvprm_pack_weight",
               "kvprm_workspace_size_lora", "kvprm_score_lora", "kvprm_workspace_size_ex",
               "kvprm_score_ex", "kvprm_workspace_size_grad", "kvprm_score_grad", "kvprm_steer",
-              "kvprm_stream_read", "kvprm_score_static", "kvprm_pack_kv"):
+              "kvprm_stream_read", "kvprm_score_static", "kvprm_pack_kv", "kvprm_rotary",
+              "kvprm_write_kv", "kvprm_read_kv", "kvprm_workspace_size_tree",
+              "kvprm_attention_tree"):
         getattr(lib, f).restype = ctypes.c_int
     lib.kvprm_last_error.argtypes = []
     lib.kvprm_last_error.restype = ctypes.c_char_p
@@ -340,3 +385,65 @@ def kvprm_attention(handle: int, cache: KVCache, batch: Batch, layer: int, q_ptr
     _check(lib.kvprm_attention(handle, ctypes.byref(cache), ctypes.byref(batch), layer, q_ptr,
                                k_self_ptr, v_self_ptr, workspace_ptr, ws_bytes, o_ptr,
                                stream or None))
+
+
+def make_rope(head_dim: int, rotary_dim: Optional[int] = None, layout: str = "half",
+              theta: float = 1.0e6, scaling: str = "none", factor: float = 1.0,
+              trained_len: float = 0.0, low: float = 1.0, high: float = 32.0,
+              magnitude: float = 1.0) -> Rope:
+    """Rotary embedding: the first rotary_dim (default: all) dims of each head; layout "half" or
+    "interleaved"; scaling "none", "linear", "base", "parts" or "ramp" (kvprm_rope_scaling)."""
+    return Rope(head_dim, head_dim if rotary_dim is None else rotary_dim, ROPE_LAYOUT[layout],
+                ROPE_SCALING[scaling], theta, factor, trained_len, low, high, magnitude)
+
+
+def make_rope_heads(tensors: Sequence[tuple]):
+    """tensors: one or two of (src_ptr, dst_ptr, heads, src_stride, dst_stride)."""
+    return (RopeHeads * len(tensors))(*[RopeHeads(s or None, d or None, *rest)
+                                        for s, d, *rest in tensors])
+
+
+def kvprm_rotary(rope: Rope, dtype: str, rows: int, positions_ptr: int, tensors,
+                 transpose: bool = False, stream: int = 0) -> None:
+    """tensors: of make_rope_heads."""
+    _check(lib.kvprm_rotary(ctypes.byref(rope), DTYPE_CODE[dtype], rows, positions_ptr or None,
+                            tensors, len(tensors), int(transpose), stream or None))
+
+
+def make_kv_rows(k_ptr: int, v_ptr: int, dtype: str, k_stride: int, v_stride: int, num_rows: int,
+                 start_ptr: int, max_rows: int, index_ptr: int = 0) -> KVRows:
+    return KVRows(k_ptr or None, v_ptr or None, DTYPE_CODE[dtype], k_stride, v_stride, num_rows,
+                  start_ptr or None, index_ptr or None, max_rows)
+
+
+def kvprm_write_kv(handle: int, cache: KVCache, batch: Batch, layer: int, rows: KVRows,
+                   stream: int = 0) -> None:
+    _check(lib.kvprm_write_kv(handle, ctypes.byref(cache), ctypes.byref(batch), layer,
+                              ctypes.byref(rows), stream or None))
+
+
+def kvprm_read_kv(handle: int, cache: KVCache, batch: Batch, layer: int, rows: KVRows,
+                  first_ptr: int = 0, stream: int = 0) -> None:
+    _check(lib.kvprm_read_kv(handle, ctypes.byref(cache), ctypes.byref(batch), layer,
+                             ctypes.byref(rows), first_ptr or None, stream or None))
+
+
+def make_tree(q_ptr: int, k_ptr: int, v_ptr: int, o_ptr: int, dtype: str, q_stride: int,
+              k_stride: int, v_stride: int, o_stride: int, num_rows: int, start_ptr: int,
+              max_rows: int, mask_ptr: int = 0, mask_words: int = 0) -> Tree:
+    return Tree(q_ptr or None, k_ptr or None, v_ptr or None, o_ptr or None, DTYPE_CODE[dtype],
+                q_stride, k_stride, v_stride, o_stride, num_rows, start_ptr or None, max_rows,
+                mask_ptr or None, mask_words)
+
+
+def kvprm_workspace_size_tree(handle: int, batch: Batch, tree: Tree) -> int:
+    n = ctypes.c_size_t()
+    _check(lib.kvprm_workspace_size_tree(handle, ctypes.byref(batch), ctypes.byref(tree),
+                                         ctypes.byref(n)))
+    return n.value
+
+
+def kvprm_attention_tree(handle: int, cache: KVCache, batch: Batch, layer: int, tree: Tree,
+                         workspace_ptr: int, ws_bytes: int, stream: int = 0) -> None:
+    _check(lib.kvprm_attention_tree(handle, ctypes.byref(cache), ctypes.byref(batch), layer,
+                                    ctypes.byref(tree), workspace_ptr, ws_bytes, stream or None))

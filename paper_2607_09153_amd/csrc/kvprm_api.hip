@@ -1,6 +1,7 @@
 // C ABI of libkvprm: argument validation, workspace carving and launch sequencing of the
 // verify-token pass. Nothing here allocates device memory; only the debug check of the page
 // table (KVPRM_DEBUG=1 at kvprm_create) synchronises the host.
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <stdlib.h>
@@ -798,6 +799,248 @@ kvprm_status kvprm_attention_partials(kvprm_handle h, const kvprm_kv_cache *cach
                            group_table(h, b, p), q, nullptr, nullptr, nullptr, nullptr,
                            (hipStream_t)stream, nullptr, true),
           "attention partials");
+  return ok();
+}
+
+// ------------------------------------------------------------------ a cache that grows
+
+// Turns per position of every rotary pair (frequency / 2 pi), in 64 bits.
+static void rope_turns(const kvprm_rope &r, double *turn) {
+  const double two_pi = 6.283185307179586476925286766559;
+  const int n = r.rotary_dim;
+  double theta = r.theta;
+  if (r.scaling == KVPRM_ROPE_BASE && n > 2) theta *= pow(r.factor, n / (n - 2.0));
+  double a = 0, b = 0;  // the ramp's ends
+  if (r.scaling == KVPRM_ROPE_RAMP) {
+    const double per = n / (2 * log(theta));
+    a = fmax(floor(per * log(r.trained_len / (two_pi * r.high))), 0.0);
+    b = fmin(ceil(per * log(r.trained_len / (two_pi * r.low))), n - 1.0);
+  }
+  for (int i = 0; i < n / 2; ++i) {
+    double f = pow(theta, -2.0 * i / n), w = 1;  // w: share of the frequency that is not interpolated
+    if (r.scaling == KVPRM_ROPE_LINEAR) w = 0;
+    if (r.scaling == KVPRM_ROPE_PARTS)
+      w = fmin(fmax((r.trained_len * f / two_pi - r.low) / (r.high - r.low), 0.0), 1.0);
+    if (r.scaling == KVPRM_ROPE_RAMP) w = 1 - fmin(fmax((i - a) / fmax(b - a, 0.001), 0.0), 1.0);
+    if (w < 1) f = f * w + f / r.factor * (1 - w);
+    turn[i] = f / two_pi;
+  }
+}
+
+kvprm_status kvprm_rotary(const kvprm_rope *rope, kvprm_dtype dtype, int64_t rows,
+                          const int32_t *positions, const kvprm_rope_heads *parts,
+                          int32_t num_parts, int32_t transpose, void *stream) {
+  const char *fn = "kvprm_rotary";
+  if (!rope || !parts) return fail(KVPRM_E_INVALID, "%s: null argument", fn);
+  const kvprm_rope &r = *rope;
+  if (r.head_dim < 2 || r.head_dim > 2 * kMaxRotaryPairs || r.head_dim % 2 != 0)
+    return fail(KVPRM_E_INVALID, "%s: head_dim %d not an even number in [2, %d]", fn, r.head_dim,
+                2 * kMaxRotaryPairs);
+  if (r.rotary_dim < 2 || r.rotary_dim > r.head_dim || r.rotary_dim % 2 != 0)
+    return fail(KVPRM_E_INVALID, "%s: rotary_dim %d not an even number in [2, %d]", fn, r.rotary_dim,
+                r.head_dim);
+  if (r.layout != KVPRM_ROPE_HALF && r.layout != KVPRM_ROPE_INTERLEAVED)
+    return fail(KVPRM_E_INVALID, "%s: unknown layout %d", fn, (int)r.layout);
+  if (r.scaling < KVPRM_ROPE_NONE || r.scaling > KVPRM_ROPE_RAMP)
+    return fail(KVPRM_E_INVALID, "%s: unknown scaling %d", fn, (int)r.scaling);
+  if (!(r.theta > 1.0) || !isfinite(r.theta) || !isfinite(r.magnitude))
+    return fail(KVPRM_E_INVALID, "%s: theta must be above 1, theta and magnitude finite", fn);
+  if (r.scaling != KVPRM_ROPE_NONE && (!(r.factor >= 1.0) || !isfinite(r.factor)))
+    return fail(KVPRM_E_INVALID, "%s: factor must be finite and at least 1", fn);
+  if ((r.scaling == KVPRM_ROPE_PARTS || r.scaling == KVPRM_ROPE_RAMP) &&
+      (!(r.trained_len > 0) || !isfinite(r.trained_len) || !(r.low > 0) || !(r.high > r.low) ||
+       !isfinite(r.high)))
+    return fail(KVPRM_E_INVALID, "%s: trained_len > 0 and 0 < low < high needed", fn);
+  if (dtype != KVPRM_F32 && dtype != KVPRM_BF16)
+    return fail(KVPRM_E_INVALID, "%s: dtype must be F32 or BF16", fn);
+  if (num_parts != 1 && num_parts != 2) return fail(KVPRM_E_INVALID, "%s: num_parts must be 1 or 2", fn);
+  if (rows < 0) return fail(KVPRM_E_INVALID, "%s: rows < 0", fn);
+  if (rows > INT32_MAX) return fail(KVPRM_E_UNSUPPORTED, "%s: at most 2^31 - 1 rows", fn);
+  const int64_t eb = dtype == KVPRM_BF16 ? 2 : 4;
+  int64_t heads = 0;
+  for (int i = 0; i < num_parts; ++i) {
+    const kvprm_rope_heads &p = parts[i];
+    const int64_t width = (int64_t)p.heads * r.head_dim;
+    if (p.heads < 1) return fail(KVPRM_E_INVALID, "%s: tensor %d has no heads", fn, i);
+    heads += p.heads;
+    if (heads > 1024) return fail(KVPRM_E_UNSUPPORTED, "%s: at most 1024 heads", fn);
+    if (p.src_stride < width || p.dst_stride < width)
+      return fail(KVPRM_E_INVALID, "%s: tensor %d: a stride below the row's %lld values", fn, i,
+                  (long long)width);
+    if (rows == 0) continue;
+    if (!p.src || !p.dst) return fail(KVPRM_E_INVALID, "%s: null tensor %d", fn, i);
+    if (((uintptr_t)p.src | (uintptr_t)p.dst) % eb != 0)
+      return fail(KVPRM_E_INVALID, "%s: tensor %d not aligned to its elements", fn, i);
+    if (p.src == p.dst && p.src_stride == p.dst_stride) continue;
+    // rows written next to rows read (other columns of one buffer) are no overlap
+    const uintptr_t a = (uintptr_t)p.src, b = (uintptr_t)p.dst;
+    const uintptr_t na = (uintptr_t)(((rows - 1) * p.src_stride + width) * eb);
+    const uintptr_t nb = (uintptr_t)(((rows - 1) * p.dst_stride + width) * eb);
+    if (a < b + nb && b < a + na) {
+      const uintptr_t step = (uintptr_t)(p.src_stride * eb), w = (uintptr_t)(width * eb);
+      const uintptr_t off = (a > b ? a - b : b - a) % step;
+      if (p.src_stride != p.dst_stride || off < w || step - off < w)
+        return fail(KVPRM_E_INVALID, "%s: src and dst of tensor %d overlap", fn, i);
+    }
+  }
+  if (rows == 0) return ok();
+  if (!positions) return fail(KVPRM_E_INVALID, "%s: null positions", fn);
+  double turn[kMaxRotaryPairs];
+  rope_turns(r, turn);
+  HIP_TRY(launch_rotary(r, turn, dtype == KVPRM_BF16, rows, positions, parts, num_parts, transpose != 0,
+                        (hipStream_t)stream),
+          "rotary");
+  return ok();
+}
+
+// A row array of `width` values a row.
+static kvprm_status check_rows(const void *p, int64_t stride, int64_t width, kvprm_dtype dtype,
+                               const char *what, const char *fn) {
+  const int64_t v = dtype == KVPRM_BF16 ? 8 : 4;  // values in 16 bytes
+  if (((uintptr_t)p & 15) != 0) return fail(KVPRM_E_INVALID, "%s: %s not 16-byte aligned", fn, what);
+  if (stride < width || stride % v != 0)
+    return fail(KVPRM_E_INVALID, "%s: %s stride %lld: a multiple of %lld and at least %lld needed", fn, what,
+                (long long)stride, (long long)v, (long long)width);
+  return KVPRM_OK;
+}
+
+static kvprm_status check_kv_rows(const kvprm_handle h, const kvprm_kv_cache *cache, const kvprm_batch *b,
+                                  int32_t layer, const kvprm_kv_rows *r, bool optional, const char *fn) {
+  kvprm_status st = check_cache(h, cache, fn);
+  if (st != KVPRM_OK) return st;
+  if (layer < 0 || layer >= h->dm.layers)
+    return fail(KVPRM_E_INVALID, "%s: layer %d outside [0, %d)", fn, layer, h->dm.layers);
+  if (!r || !r->start) return fail(KVPRM_E_INVALID, "%s: null rows or start", fn);
+  if (r->dtype != KVPRM_F32 && r->dtype != KVPRM_BF16)
+    return fail(KVPRM_E_INVALID, "%s: rows must be F32 or BF16", fn);
+  if (r->num_rows < 0 || r->max_rows < 0) return fail(KVPRM_E_INVALID, "%s: a row count below 0", fn);
+  if (r->num_rows > INT32_MAX) return fail(KVPRM_E_UNSUPPORTED, "%s: at most 2^31 - 1 rows", fn);
+  if (r->num_rows == 0 || r->max_rows == 0) return KVPRM_OK;
+  if (optional ? !r->k && !r->v : !r->k || !r->v) return fail(KVPRM_E_INVALID, "%s: null k or v rows", fn);
+  const int64_t width = (int64_t)h->dm.nkv * h->dm.d;
+  if (r->k && (st = check_rows(r->k, r->k_stride, width, r->dtype, "k", fn)) != KVPRM_OK) return st;
+  if (r->v && (st = check_rows(r->v, r->v_stride, width, r->dtype, "v", fn)) != KVPRM_OK) return st;
+  return KVPRM_OK;
+}
+
+// Debug mode only: the pages that would get rows are in the pool, and get rows of one candidate each.
+static kvprm_status check_written_debug(const kvprm_handle h, const kvprm_kv_cache *c, const kvprm_batch *b,
+                                        const kvprm_kv_rows *r, hipStream_t s, const char *fn) {
+  if (!h->debug) return KVPRM_OK;
+  std::vector<int32_t> len(b->batch), start(b->batch + 1), pt((size_t)b->batch * b->max_pages);
+  if (hipMemcpyAsync(len.data(), b->lengths, len.size() * 4, hipMemcpyDeviceToHost, s) != hipSuccess ||
+      hipMemcpyAsync(start.data(), r->start, start.size() * 4, hipMemcpyDeviceToHost, s) != hipSuccess ||
+      hipMemcpyAsync(pt.data(), b->page_table, pt.size() * 4, hipMemcpyDeviceToHost, s) != hipSuccess ||
+      hipStreamSynchronize(s) != hipSuccess)
+    return fail(KVPRM_E_HIP, "%s: debug copy of the page table failed", fn);
+  const int cap = b->max_pages * kPage;
+  std::vector<int32_t> owner((size_t)c->num_pages, -1);
+  for (int i = 0; i < b->batch; ++i) {
+    const int64_t n = (int64_t)start[i + 1] - start[i];
+    if (start[i] < 0 || n < 0 || n > r->max_rows)
+      return fail(KVPRM_E_INVALID, "%s: start[%d..%d] = %d, %d", fn, i, i + 1, start[i], start[i + 1]);
+    if (len[i] < 0 || len[i] + n > cap)
+      return fail(KVPRM_E_INVALID, "%s: candidate %d: %d tokens and %lld rows exceed %d", fn, i, len[i],
+                  (long long)n, cap);
+    for (int k = len[i] / kPage; n > 0 && k * kPage < len[i] + n; ++k) {
+      const int32_t id = pt[(size_t)i * b->max_pages + k];
+      if (id < 0 || id >= c->num_pages)
+        return fail(KVPRM_E_INVALID, "%s: page_table[%d][%d] = %d outside [0, %d)", fn, i, k, id,
+                    c->num_pages);
+      if (owner[id] >= 0)
+        return fail(KVPRM_E_INVALID, "%s: page %d gets rows of candidates %d and %d", fn, id, owner[id], i);
+      owner[id] = i;
+    }
+  }
+  return KVPRM_OK;
+}
+
+kvprm_status kvprm_write_kv(kvprm_handle h, const kvprm_kv_cache *cache, const kvprm_batch *b,
+                            int32_t layer, const kvprm_kv_rows *rows, void *stream) {
+  const char *fn = "kvprm_write_kv";
+  if (!h) return fail(KVPRM_E_INVALID, "%s: null handle", fn);
+  kvprm_status st = check_batch(h, b, fn);
+  if (st != KVPRM_OK) return st;
+  if (b->batch == 0) return ok();
+  if ((st = check_kv_rows(h, cache, b, layer, rows, false, fn)) != KVPRM_OK) return st;
+  if (rows->num_rows == 0 || rows->max_rows == 0) return ok();
+  if ((st = check_written_debug(h, cache, b, rows, (hipStream_t)stream, fn)) != KVPRM_OK) return st;
+  HIP_TRY(launch_write_kv(h->dm, *cache, *b, layer, *rows, (hipStream_t)stream), "write kv");
+  return ok();
+}
+
+kvprm_status kvprm_read_kv(kvprm_handle h, const kvprm_kv_cache *cache, const kvprm_batch *b,
+                           int32_t layer, const kvprm_kv_rows *rows, const int32_t *first,
+                           void *stream) {
+  const char *fn = "kvprm_read_kv";
+  if (!h) return fail(KVPRM_E_INVALID, "%s: null handle", fn);
+  kvprm_status st = check_batch(h, b, fn);
+  if (st != KVPRM_OK) return st;
+  if (b->batch == 0) return ok();
+  if ((st = check_kv_rows(h, cache, b, layer, rows, true, fn)) != KVPRM_OK) return st;
+  if (rows->index) return fail(KVPRM_E_INVALID, "%s: index must be null", fn);
+  if (rows->num_rows == 0 || rows->max_rows == 0) return ok();
+  if ((st = check_pages_debug(h, cache, b, (hipStream_t)stream, fn)) != KVPRM_OK) return st;
+  HIP_TRY(launch_read_kv(h->dm, *cache, *b, layer, *rows, first, (hipStream_t)stream), "read kv");
+  return ok();
+}
+
+static kvprm_status check_tree(const kvprm_handle h, const kvprm_batch *b, const kvprm_tree *t,
+                               const char *fn) {
+  if (!t) return fail(KVPRM_E_INVALID, "%s: null tree", fn);
+  if (t->dtype != KVPRM_F32 && t->dtype != KVPRM_BF16)
+    return fail(KVPRM_E_INVALID, "%s: rows must be F32 or BF16", fn);
+  if (t->num_rows < 0 || t->max_rows < 1)
+    return fail(KVPRM_E_INVALID, "%s: num_rows < 0 or max_rows < 1", fn);
+  if (t->max_rows > kMaxTreeRows)
+    return fail(KVPRM_E_UNSUPPORTED, "%s: at most %d drafted tokens per candidate", fn, kMaxTreeRows);
+  if (t->num_rows > INT32_MAX) return fail(KVPRM_E_UNSUPPORTED, "%s: at most 2^31 - 1 rows", fn);
+  if ((int64_t)b->batch * h->dm.nkv > 65535)  // (the launch grid's third side)
+    return fail(KVPRM_E_UNSUPPORTED, "%s: at most 65535 kv-heads over the batch", fn);
+  return KVPRM_OK;
+}
+
+kvprm_status kvprm_workspace_size_tree(kvprm_handle h, const kvprm_batch *b, const kvprm_tree *t,
+                                       size_t *bytes) {
+  const char *fn = "kvprm_workspace_size_tree";
+  if (!h || !bytes) return fail(KVPRM_E_INVALID, "%s: null argument", fn);
+  kvprm_status st = check_batch(h, b, fn);
+  if (st != KVPRM_OK) return st;
+  if ((st = check_tree(h, b, t, fn)) != KVPRM_OK) return st;
+  *bytes = b->batch == 0 ? 0 : tree_ws_bytes(h->dm, *b, *t);
+  return ok();
+}
+
+kvprm_status kvprm_attention_tree(kvprm_handle h, const kvprm_kv_cache *cache, const kvprm_batch *b,
+                                  int32_t layer, const kvprm_tree *t, void *workspace,
+                                  size_t ws_bytes, void *stream) {
+  const char *fn = "kvprm_attention_tree";
+  if (!h) return fail(KVPRM_E_INVALID, "%s: null handle", fn);
+  kvprm_status st = check_batch(h, b, fn);
+  if (st != KVPRM_OK) return st;
+  if (b->batch == 0) return ok();
+  if ((st = check_cache(h, cache, fn)) != KVPRM_OK) return st;
+  if (layer < 0 || layer >= h->dm.layers)
+    return fail(KVPRM_E_INVALID, "%s: layer %d outside [0, %d)", fn, layer, h->dm.layers);
+  if ((st = check_tree(h, b, t, fn)) != KVPRM_OK) return st;
+  if (t->num_rows == 0) return ok();
+  if (!t->q || !t->k || !t->v || !t->o || !t->start)
+    return fail(KVPRM_E_INVALID, "%s: null q, k, v, o or start", fn);
+  const int64_t nq = (int64_t)h->dm.nq * h->dm.d, nkv = (int64_t)h->dm.nkv * h->dm.d;
+  if ((st = check_rows(t->q, t->q_stride, nq, t->dtype, "q", fn)) != KVPRM_OK) return st;
+  if ((st = check_rows(t->k, t->k_stride, nkv, t->dtype, "k", fn)) != KVPRM_OK) return st;
+  if ((st = check_rows(t->v, t->v_stride, nkv, t->dtype, "v", fn)) != KVPRM_OK) return st;
+  if ((st = check_rows(t->o, t->o_stride, nq, t->dtype, "o", fn)) != KVPRM_OK) return st;
+  if (t->mask && t->mask_words < (t->max_rows + 31) / 32)
+    return fail(KVPRM_E_INVALID, "%s: mask_words %d below %d", fn, t->mask_words, (t->max_rows + 31) / 32);
+  const size_t need = tree_ws_bytes(h->dm, *b, *t);
+  if (!workspace || ws_bytes < need)
+    return fail(KVPRM_E_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need,
+                workspace ? ws_bytes : (size_t)0);
+  if (((uintptr_t)workspace & 255) != 0)
+    return fail(KVPRM_E_WORKSPACE, "%s: workspace not 256-byte aligned", fn);
+  if ((st = check_pages_debug(h, cache, b, (hipStream_t)stream, fn)) != KVPRM_OK) return st;
+  HIP_TRY(launch_tree(h->dm, *cache, *b, layer, *t, workspace, (hipStream_t)stream), "tree attention");
   return ok();
 }
 

@@ -1,0 +1,529 @@
+// The cache's traffic outside scoring for gfx950: rotary positions of queries and keys (k_rotary),
+// rows of keys and values written into the paged cache (k_write_kv) and read back (k_read_kv).
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include "kvprm_internal.h"
+#include "kvprm_mx_common.h"
+
+namespace kvprm {
+
+// ------------------------------------------------------------------------------- rotary
+
+struct RotaryPart {
+  const char *src;
+  char *dst;
+  int64_t ss, ds;  // row strides in elements
+};
+struct RotaryArgs {
+  RotaryPart p[2];
+  int heads0, heads;      // heads of the first tensor, of both
+  int d, half, nrot;      // nrot: units of a head that are rotated
+  int units;              // units per head
+  uint32_t uinv, hinv;    // ceil(2^32 / units), ceil(2^32 / heads)
+  int64_t rows;
+  int rpb;                // rows per block
+  const int32_t *pos;
+  float mag, smag;        // factor on cosines and sines (the sines' negated for the transpose)
+  double turn[kMaxRotaryPairs];  // turns per position of each pair
+};
+
+// A vector of V elements of T, widened and back (rounded to nearest even).
+template <typename T, int V>
+struct Vec;
+template <>
+struct Vec<float, 4> {
+  static __device__ __forceinline__ void load(const float *p, float *v) {
+    const float4 x = *(const float4 *)p;
+    v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+  }
+  static __device__ __forceinline__ void store(float *p, const float *v) {
+    *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]);
+  }
+};
+template <>
+struct Vec<float, 1> {
+  static __device__ __forceinline__ void load(const float *p, float *v) { v[0] = *p; }
+  static __device__ __forceinline__ void store(float *p, const float *v) { *p = v[0]; }
+};
+__device__ __forceinline__ uint32_t bf16x2(float a, float b) {
+  typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+  typedef float f32x2v __attribute__((ext_vector_type(2)));
+  const f32x2v x = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2v));
+}
+template <>
+struct Vec<uint16_t, 8> {
+  static __device__ __forceinline__ void load(const uint16_t *p, float *v) {
+    const uint4 x = *(const uint4 *)p;
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+  static __device__ __forceinline__ void store(uint16_t *p, const float *v) {
+    *(uint4 *)p = make_uint4(bf16x2(v[0], v[1]), bf16x2(v[2], v[3]), bf16x2(v[4], v[5]),
+                             bf16x2(v[6], v[7]));
+  }
+};
+template <>
+struct Vec<uint16_t, 1> {
+  static __device__ __forceinline__ void load(const uint16_t *p, float *v) {
+    v[0] = __uint_as_float((uint32_t)*p << 16);
+  }
+  static __device__ __forceinline__ void store(uint16_t *p, const float *v) {
+    *p = (uint16_t)bf16x2(v[0], 0.f);
+  }
+};
+
+// (a, b) -> m R(p f) (a, b) for every pair of the first 2 half dims of each head; the others are
+// copied. Bound by memory. A block takes rpb rows: it first forms the cosine and sine of every
+// (row, pair) in LDS, once for all heads, then walks the rows' units: V elements of a pair's first
+// halves and the V matching ones (HALF), or V adjacent elements (INTERLEAVED), or V elements past
+// the rotated ones. The angle's turns are reduced in 64 bits, p * f - round(p * f), since p f reaches
+// 10^5 turns and more; the rest, at most half a turn, is exact enough in 32.
+// V = 16 bytes where widths, strides and addresses allow, else one element.
+template <typename T, int V, bool HALF>
+__global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
+  __shared__ float2 cs[kRotaryCs];
+  const int64_t row0 = (int64_t)blockIdx.x * a.rpb;
+  const int nr = (int)min((int64_t)a.rpb, a.rows - row0);
+  for (int i = threadIdx.x; i < nr * a.half; i += 256) {
+    const int r = i / a.half, pair = i - r * a.half;
+    const double t = (double)a.pos[row0 + r] * a.turn[pair];
+    const float rest = (float)(t - rint(t));
+    float s, c;
+    sincospif(2.f * rest, &s, &c);
+    cs[i] = make_float2(c * a.mag, s * a.smag);
+  }
+  __syncthreads();
+  const uint32_t n = (uint32_t)nr * a.heads * a.units;
+  for (uint32_t i = threadIdx.x; i < n; i += 256) {
+    // (row, head), unit; the divisors' inverses are 0 for 1
+    const uint32_t hr = a.uinv ? __umulhi(i, a.uinv) : i, u = i - hr * a.units;
+    const uint32_t r = a.hinv ? __umulhi(hr, a.hinv) : hr, h = hr - r * a.heads;
+    const bool second = (int)h >= a.heads0;
+    const RotaryPart p = second ? a.p[1] : a.p[0];
+    const int64_t at = (row0 + r);
+    const int hh = (int)h - (second ? a.heads0 : 0);
+    const T *src = (const T *)p.src + at * p.ss + (int64_t)hh * a.d;
+    T *dst = (T *)p.dst + at * p.ds + (int64_t)hh * a.d;
+    const float2 *c = cs + r * a.half;
+    if ((int)u >= a.nrot) {  // kept dims
+      const int e = 2 * a.half + ((int)u - a.nrot) * V;
+      float x[V];
+      Vec<T, V>::load(src + e, x);
+      Vec<T, V>::store(dst + e, x);
+    } else if (HALF) {
+      const int e = (int)u * V;
+      float x[V], y[V];
+      Vec<T, V>::load(src + e, x);
+      Vec<T, V>::load(src + a.half + e, y);
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float2 w = c[e + k];
+        const float xa = x[k], xb = y[k];
+        x[k] = xa * w.x - xb * w.y;
+        y[k] = xb * w.x + xa * w.y;
+      }
+      Vec<T, V>::store(dst + e, x);
+      Vec<T, V>::store(dst + a.half + e, y);
+    } else {
+      // (one element at a time: a unit is a pair)
+      constexpr int W = V == 1 ? 2 : V;
+      const int e = (int)u * W;
+      float x[W];
+      if (V == 1) {
+        Vec<T, 1>::load(src + e, x);
+        Vec<T, 1>::load(src + e + 1, x + 1);
+      } else {
+        Vec<T, V>::load(src + e, x);
+      }
+#pragma unroll
+      for (int k = 0; k < W; k += 2) {
+        const float2 w = c[(e + k) >> 1];
+        const float xa = x[k], xb = x[k + 1];
+        x[k] = xa * w.x - xb * w.y;
+        x[k + 1] = xb * w.x + xa * w.y;
+      }
+      if (V == 1) {
+        Vec<T, 1>::store(dst + e, x);
+        Vec<T, 1>::store(dst + e + 1, x + 1);
+      } else {
+        Vec<T, V>::store(dst + e, x);
+      }
+    }
+  }
+}
+
+hipError_t launch_rotary(const kvprm_rope &rp, const double *turn, bool bf16, int64_t rows,
+                         const int32_t *pos, const kvprm_rope_heads *parts, int num_parts,
+                         bool transpose, hipStream_t s) {
+  RotaryArgs a;
+  const int eb = bf16 ? 2 : 4, v = 16 / eb;
+  bool wide = true;
+  a.heads = 0;
+  a.heads0 = parts[0].heads;
+  for (int i = 0; i < 2; ++i) {
+    const kvprm_rope_heads &q = parts[i < num_parts ? i : 0];
+    a.p[i] = RotaryPart{(const char *)q.src, (char *)q.dst, q.src_stride, q.dst_stride};
+    if (i < num_parts) a.heads += q.heads;
+    wide = wide && (((uintptr_t)q.src | (uintptr_t)q.dst) & 15) == 0 && q.src_stride % v == 0 &&
+           q.dst_stride % v == 0;
+  }
+  const bool half = rp.layout == KVPRM_ROPE_HALF;
+  a.d = rp.head_dim;
+  a.half = rp.rotary_dim / 2;
+  wide = wide && a.d % v == 0 && (half ? a.half : rp.rotary_dim) % v == 0;
+  const int V = wide ? v : 1;
+  a.nrot = half || !wide ? a.half / (half ? V : 1) : rp.rotary_dim / V;
+  a.units = a.nrot + (a.d - rp.rotary_dim) / V;
+  a.uinv = (uint32_t)(((1ull << 32) + a.units - 1) / a.units);
+  a.hinv = (uint32_t)(((1ull << 32) + a.heads - 1) / a.heads);
+  a.rows = rows;
+  a.pos = pos;
+  a.mag = (float)rp.magnitude;
+  a.smag = transpose ? -a.mag : a.mag;
+  for (int i = 0; i < a.half; ++i) a.turn[i] = turn[i];
+  // rows per block: one while that leaves the chip unfilled, then enough for four units a thread,
+  // within the table
+  const int64_t per_row = (int64_t)a.heads * a.units;
+  int64_t rpb = 1;
+  while (rpb < 16 && rpb * 2 * a.half <= kRotaryCs && rows > rpb * 1024 && rpb * per_row < 1024)
+    rpb *= 2;
+  a.rpb = (int)rpb;
+  const dim3 grid((unsigned)((rows + rpb - 1) / rpb));
+#define KVPRM_ROT(T_, V_)                                                             \
+  if (half) hipLaunchKernelGGL((k_rotary<T_, V_, true>), grid, dim3(256), 0, s, a);   \
+  else hipLaunchKernelGGL((k_rotary<T_, V_, false>), grid, dim3(256), 0, s, a)
+  if (bf16) {
+    if (wide) { KVPRM_ROT(uint16_t, 8); }
+    else { KVPRM_ROT(uint16_t, 1); }
+  } else {
+    if (wide) { KVPRM_ROT(float, 4); }
+    else { KVPRM_ROT(float, 1); }
+  }
+#undef KVPRM_ROT
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------------------- cache rows
+
+struct RowArgs {
+  char *kp, *vp;       // this layer's pools
+  float *ksc, *vsc;    // this layer's fp8 scales (or null)
+  int nkv, num_pages;
+  const int32_t *page_table;
+  int max_pages;
+  const int32_t *lengths;
+  char *k, *v;         // rows
+  int64_t ks, vs;      // row strides in elements
+  int64_t num_rows;
+  const int32_t *start, *index, *first;
+  int max_rows;
+};
+
+// Exponent of the smallest power of two s with 448 s >= amax (448 = 1.75 * 2^8), from the bits of
+// a finite amax >= 0: 2^(E - 135), or the next one where the significand exceeds 1.75.
+__device__ __forceinline__ int scale_exponent(float amax) {
+  const uint32_t b = __float_as_uint(amax);
+  return max((int)(b >> 23) - 135 + ((b & 0x7FFFFFu) > 0x600000u), kMinScaleExp);
+}
+// Exponent of the smallest power of two >= s (s a positive normal number).
+__device__ __forceinline__ int ceil_exponent(float s) {
+  const uint32_t b = __float_as_uint(s);
+  return (int)((b >> 23) & 255) - 127 + ((b & 0x7FFFFFu) != 0);
+}
+__device__ __forceinline__ float exp2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// Four values to e4m3 codes (nearest even; NaN and infinities to NaN).
+__device__ __forceinline__ uint32_t fp8x4(const float *x) {
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = fabsf(x[i]) < INFINITY ? x[i] : __builtin_nanf("");
+  int w = 0;
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], w, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+  return (uint32_t)w;
+}
+
+// Rows of one (page, kv-head, part) tile, one wave: the tile's new rows in registers (16 bytes of a
+// row per lane), for fp8 their largest magnitude and the tile's scale, the codes through LDS into
+// the stored order, 16 bytes per lane and store. Only groups of 16 bytes that hold a new slot (or an
+// old one whose scale grew) are stored; those that also hold other slots are read first.
+// Bound by memory on long prompts, by the launch on single tokens.
+template <int KVT, int D, typename S>
+__global__ __launch_bounds__(256) void k_write_kv(RowArgs a) {
+  constexpr int EB = KVT == 0 ? 4 : KVT == 1 ? 2 : 1;
+  constexpr int X = 16 / EB, R = X / 4;
+  constexpr int VS = 16 / (int)sizeof(S);  // elements of a row per lane and load
+  constexpr int LPR = D / VS;              // lanes per row
+  constexpr int RPL = 64 / LPR;            // rows per load
+  constexpr int NL = 16 / RPL;             // loads
+  __shared__ uint4 lds[4][D * EB];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int b = blockIdx.y;
+  const int item = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + wave);
+  const int per = 2 * a.nkv, slotpage = item / per, pj = item - slotpage * per;
+  const bool part = pj >= a.nkv;
+  const int j = part ? pj - a.nkv : pj;
+  const int L = a.lengths[b], r0 = a.start[b];
+  if (L < 0 || r0 < 0) return;
+  // rows of this candidate: at most max_rows, and no further than the page table
+  const int n = (int)min((int64_t)min(a.start[b + 1] - r0, a.max_rows), (int64_t)a.max_pages * kPage - L);
+  const int page = L / kPage + slotpage;
+  if (n <= 0 || page * kPage >= L + n) return;
+  const int id = a.page_table[(size_t)b * a.max_pages + page];
+  if (id < 0 || id >= a.num_pages) return;
+  const S *rows = (const S *)(part ? a.v : a.k);
+  const int64_t stride = part ? a.vs : a.ks;
+
+  const int lr = lane / LPR, lc = lane - lr * LPR;
+  float x[NL][VS];
+  uint32_t news = 0;  // slots this lane loads that are new
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    const int slot = i * RPL + lr, t = page * kPage + slot - L;
+    bool ok = t >= 0 && t < n;
+    int64_t row = 0;
+    if (ok) {
+      row = a.index ? a.index[r0 + t] : r0 + t;
+      ok = row >= 0 && row < a.num_rows;
+    }
+    if (ok) {
+      Vec<S, VS>::load(rows + row * stride + (int64_t)j * D + lc * VS, x[i]);
+      news |= 1u << slot;
+    } else {
+#pragma unroll
+      for (int k = 0; k < VS; ++k) x[i][k] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int off = LPR; off < 64; off <<= 1) news |= __shfl_xor(news, off, 64);
+  const int old = max(0, min(kPage, L - page * kPage));  // slots before the new ones
+
+  const size_t tile = (size_t)id * a.nkv + j;
+  uint4 *out = (uint4 *)(part ? a.vp : a.kp) + tile * (D * EB);
+  float inv = 1.f, ratio = 1.f;
+  bool grew = false;
+  if (KVT == 2) {
+    float *scp = (part ? a.vsc : a.ksc) + tile;
+    const float before = *scp;
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < NL; ++i)
+#pragma unroll
+      for (int k = 0; k < VS; ++k) {
+        const float y = fabsf(x[i][k]);
+        m = fmaxf(m, y < INFINITY ? y : 0.f);
+      }
+    int e = scale_exponent(wmax(m));
+    if (old > 0) e = max(e, ceil_exponent(before));
+    e = min(e, 120);
+    const float scale = exp2i(e);
+    inv = exp2i(-e);
+    if (old > 0 && scale != before) {
+      grew = true;
+      ratio = before * inv;
+    }
+    if (lane == 0 && news) *scp = scale;
+    if (!news) return;
+  }
+
+  // the new slots' values in the cache's type, token-major
+  unsigned char *tb = (unsigned char *)lds[wave];
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    const int slot = i * RPL + lr;
+    unsigned char *p = tb + (slot * D + lc * VS) * EB;
+    if (KVT == 0) {
+#pragma unroll
+      for (int k = 0; k < VS; k += 4)
+        *(float4 *)(p + 4 * k) = make_float4(x[i][k], x[i][k + 1], x[i][k + 2], x[i][k + 3]);
+    } else if (KVT == 1) {
+#pragma unroll
+      for (int k = 0; k < VS; k += 2) *(uint32_t *)(p + 2 * k) = bf16x2(x[i][k], x[i][k + 1]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < VS; k += 4) {
+        const float y[4] = {x[i][k] * inv, x[i][k + 1] * inv, x[i][k + 2] * inv, x[i][k + 3] * inv};
+        *(uint32_t *)(p + k) = fp8x4(y);
+      }
+    }
+  }
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  const uint32_t olds = old >= 16 ? 0xFFFFu : (1u << old) - 1u;
+  const uint32_t touched = news | (grew ? olds : 0u);
+  // codes of old slots at the grown scale
+  auto rescaled = [&](uint32_t w) {
+    const float y[4] = {__builtin_amdgcn_cvt_f32_fp8(w, 0) * ratio, __builtin_amdgcn_cvt_f32_fp8(w, 1) * ratio,
+                        __builtin_amdgcn_cvt_f32_fp8(w, 2) * ratio, __builtin_amdgcn_cvt_f32_fp8(w, 3) * ratio};
+    return fp8x4(y);
+  };
+#pragma unroll
+  for (int it = 0; it < D * EB / 64; ++it) {
+    const int gi = it * 64 + lane;
+    if (!part) {
+      const int s = gi & 15, mb = gi >> 4;
+      if (!(touched >> s & 1)) continue;
+      uint4 w;
+      if (news >> s & 1) {
+        w = *(const uint4 *)(tb + s * D * EB + mb * 16);
+      } else {  // (fp8 only)
+        w = out[gi];
+        w = make_uint4(rescaled(w.x), rescaled(w.y), rescaled(w.z), rescaled(w.w));
+      }
+      out[gi] = w;
+    } else {
+      const int mm = gi & 15, sq = (gi >> 4) & 3, blk = gi >> 6;
+      if (!(touched >> (4 * sq) & 15)) continue;
+      uint4 w = make_uint4(0, 0, 0, 0);
+      const bool all = (news >> (4 * sq) & 15) == 15;
+      if (!all) w = out[gi];
+      unsigned char wb[16];
+      __builtin_memcpy(wb, &w, 16);
+      if (KVT == 2 && grew && !all) {
+        uint32_t q[4] = {rescaled(w.x), rescaled(w.y), rescaled(w.z), rescaled(w.w)};
+        unsigned char qb[16];
+        __builtin_memcpy(qb, q, 16);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (olds >> (4 * sq + (i & 3)) & 1) wb[i] = qb[i];
+      }
+#pragma unroll
+      for (int q = 0; q < R; ++q)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int m = blk * 16 * R + q * 16 + mm, s = 4 * sq + k;
+          if (news >> s & 1) {
+#pragma unroll
+            for (int e = 0; e < EB; ++e) wb[(q * 4 + k) * EB + e] = tb[(s * D + m) * EB + e];
+          }
+        }
+      __builtin_memcpy(&w, wb, 16);
+      out[gi] = w;
+    }
+  }
+}
+
+// The reverse: one wave per (page, kv-head, part) tile, its 16-byte groups through LDS, rows of the
+// wanted positions out, 16 bytes per lane and store.
+template <int KVT, int D, typename S>
+__global__ __launch_bounds__(256) void k_read_kv(RowArgs a) {
+  constexpr int EB = KVT == 0 ? 4 : KVT == 1 ? 2 : 1;
+  constexpr int X = 16 / EB, R = X / 4;
+  constexpr int VS = 16 / (int)sizeof(S);
+  constexpr int LPR = D / VS, RPL = 64 / LPR, NL = 16 / RPL;
+  __shared__ uint4 lds[4][D * EB];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int b = blockIdx.y;
+  const int item = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + wave);
+  const int parts = (a.k ? 1 : 0) + (a.v ? 1 : 0);
+  const int per = parts * a.nkv, slotpage = item / per, pj = item - slotpage * per;
+  const bool part = !a.k || pj >= a.nkv;
+  const int j = pj >= a.nkv ? pj - a.nkv : pj;
+  const int L = (int)min((int64_t)a.lengths[b], (int64_t)a.max_pages * kPage);
+  const int r0 = a.start[b], n = min(a.start[b + 1] - r0, a.max_rows);
+  const int p0 = a.first ? a.first[b] : 0;  // position of the first row
+  const int from = max(p0, 0), to = (int)min((int64_t)L, (int64_t)p0 + n);
+  const int page = from / kPage + slotpage;
+  if (n <= 0 || page * kPage >= to || from >= to) return;
+  const int id = a.page_table[(size_t)b * a.max_pages + page];
+  if (id < 0 || id >= a.num_pages) return;
+  const size_t tile = (size_t)id * a.nkv + j;
+  const uint4 *in = (const uint4 *)(part ? a.vp : a.kp) + tile * (D * EB);
+  const float scale = KVT == 2 ? (part ? a.vsc : a.ksc)[tile] : 1.f;
+  uint4 *tw = lds[wave];
+#pragma unroll
+  for (int it = 0; it < D * EB / 64; ++it) tw[it * 64 + lane] = in[it * 64 + lane];
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  const unsigned char *tb = (const unsigned char *)tw;
+  S *rows = (S *)(part ? a.v : a.k);
+  const int64_t stride = part ? a.vs : a.ks;
+  const int lr = lane / LPR, lc = lane - lr * LPR;
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    const int slot = i * RPL + lr, pos = page * kPage + slot;
+    const int64_t row = (int64_t)r0 + (pos - p0);
+    if (pos < from || pos >= to || row < 0 || row >= a.num_rows) continue;
+    float x[VS];
+#pragma unroll
+    for (int k = 0; k < VS; ++k) {
+      const int m = lc * VS + k;
+      const int at = !part ? ((m / X) * 16 + slot) * X + m % X
+                           : ((((m / (16 * R)) * 4 + slot / 4) * 16 + m % 16) * R + (m / 16) % R) * 4 + slot % 4;
+      if (KVT == 0) x[k] = *(const float *)(tb + 4 * at);
+      if (KVT == 1) x[k] = __uint_as_float((uint32_t)*(const uint16_t *)(tb + 2 * at) << 16);
+      if (KVT == 2) x[k] = __builtin_amdgcn_cvt_f32_fp8(tb[at], 0) * scale;
+    }
+    Vec<S, VS>::store(rows + row * stride + (int64_t)j * D + lc * VS, x);
+  }
+}
+
+static RowArgs row_args(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batch &b, int layer,
+                        const kvprm_kv_rows &r) {
+  const size_t tiles = (size_t)c.num_pages * dm.nkv;
+  const size_t bytes = tiles * kPage * dm.d * (dm.kvdt == 0 ? 4 : dm.kvdt == 1 ? 2 : 1);
+  RowArgs a;
+  a.kp = (char *)c.k_pages + layer * bytes;
+  a.vp = (char *)c.v_pages + layer * bytes;
+  a.ksc = dm.kvdt == 2 ? (float *)c.k_scale + layer * tiles : nullptr;
+  a.vsc = dm.kvdt == 2 ? (float *)c.v_scale + layer * tiles : nullptr;
+  a.nkv = dm.nkv;
+  a.num_pages = c.num_pages;
+  a.page_table = b.page_table;
+  a.max_pages = b.max_pages;
+  a.lengths = b.lengths;
+  a.k = (char *)r.k;
+  a.v = (char *)r.v;
+  a.ks = r.k_stride;
+  a.vs = r.v_stride;
+  a.num_rows = r.num_rows;
+  a.start = r.start;
+  a.index = r.index;
+  a.first = nullptr;
+  a.max_rows = min(r.max_rows, b.max_pages * kPage);
+  return a;
+}
+
+// Pages that hold at most n consecutive tokens, wherever they start.
+static int pages_of(int n) { return (n + 2 * kPage - 2) / kPage; }
+
+#define KVPRM_ROWS_S(K_, T_, D_)                                                                  \
+  if (bf16) hipLaunchKernelGGL((K_<T_, D_, uint16_t>), grid, dim3(256), 0, s, a);                 \
+  else hipLaunchKernelGGL((K_<T_, D_, float>), grid, dim3(256), 0, s, a)
+#define KVPRM_ROWS_D(K_, T_)                                                                      \
+  if (dm.d == 64) { KVPRM_ROWS_S(K_, T_, 64); }                                                   \
+  else { KVPRM_ROWS_S(K_, T_, 128); }
+#define KVPRM_ROWS(K_)                                                                            \
+  if (dm.kvdt == 0) { KVPRM_ROWS_D(K_, 0) }                                                       \
+  else if (dm.kvdt == 1) { KVPRM_ROWS_D(K_, 1) }                                                  \
+  else { KVPRM_ROWS_D(K_, 2) }
+
+hipError_t launch_write_kv(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batch &b, int layer,
+                           const kvprm_kv_rows &r, hipStream_t s) {
+  const RowArgs a = row_args(dm, c, b, layer, r);
+  const bool bf16 = r.dtype == KVPRM_BF16;
+  const int pages = min(pages_of(a.max_rows), b.max_pages);
+  const dim3 grid((unsigned)(((int64_t)pages * 2 * dm.nkv + 3) / 4), b.batch);
+  KVPRM_ROWS(k_write_kv)
+  return hipGetLastError();
+}
+
+hipError_t launch_read_kv(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batch &b, int layer,
+                          const kvprm_kv_rows &r, const int32_t *first, hipStream_t s) {
+  RowArgs a = row_args(dm, c, b, layer, r);
+  a.first = first;
+  const bool bf16 = r.dtype == KVPRM_BF16;
+  const int parts = (r.k ? 1 : 0) + (r.v ? 1 : 0);
+  const int pages = min(pages_of(a.max_rows), b.max_pages);
+  const dim3 grid((unsigned)(((int64_t)pages * parts * dm.nkv + 3) / 4), b.batch);
+  KVPRM_ROWS(k_read_kv)
+  return hipGetLastError();
+}
+
+}  // namespace kvprm

@@ -232,6 +232,23 @@ hipError_t launch_attention(const Dims &dm, const Plan &p, const Workspace &w, i
                             const int32_t *lengths, const GroupTable &gt, const float *q,
                             const float *kself, const float *vself, float *o, uint16_t *op,
                             hipStream_t s, float *lse = nullptr, bool partials_only = false);
+// rotary positions, cache rows (kvprm_cache.hip)
+constexpr int kMaxRotaryPairs = 128;
+constexpr int kRotaryCs = 1024;      // (row, pair) angles a block holds
+constexpr int kMinScaleExp = -100;   // exponent of the smallest fp8 scale written
+// turn[i]: turns per position of pair i
+hipError_t launch_rotary(const kvprm_rope &rp, const double *turn, bool bf16, int64_t rows,
+                         const int32_t *pos, const kvprm_rope_heads *parts, int num_parts,
+                         bool transpose, hipStream_t s);
+hipError_t launch_write_kv(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batch &b, int layer,
+                           const kvprm_kv_rows &r, hipStream_t s);
+hipError_t launch_read_kv(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batch &b, int layer,
+                          const kvprm_kv_rows &r, const int32_t *first, hipStream_t s);
+// attention of drafted tokens (kvprm_tree.hip)
+constexpr int kMaxTreeRows = 256;
+size_t tree_ws_bytes(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t);
+hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batch &b, int layer,
+                       const kvprm_tree &t, void *ws, hipStream_t s);
 hipError_t launch_head(const Dims &dm, const Plan &p, const Workspace &w, const void *final_norm,
                        const void *reward_w, float reward_b, float *scores, float *logits,
                        hipStream_t s);
