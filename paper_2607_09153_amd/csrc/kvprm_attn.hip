@@ -255,17 +255,6 @@ __device__ __forceinline__ void walk_pages(const AttnArgs &a, int b, int j, int 
     chunk_loop(std::integral_constant<bool, true>{});
 }
 
-// Inclusive sum over the lanes of a wave.
-__device__ __forceinline__ int lane_scan(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);  // row shifts by 1, 2, 4, 8
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // row 0 into 1, 2 into 3
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // rows 0 and 1 into 2 and 3
-  return v;
-}
-
 // One wave per kv-head j and chunk of a candidate's private pages, over the whole batch; it writes its
 // unnormalised partial (acc, m, l) per q-head. A wave is a block of its own, or the waves of all
 // kv-heads are one (private_chunk_rule).

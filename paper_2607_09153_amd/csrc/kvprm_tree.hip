@@ -12,7 +12,7 @@ namespace kvprm {
 struct TreeArgs {
   const char *kp, *vp;     // this layer's pools
   const float *ksc, *vsc;  // this layer's fp8 scales (or null)
-  int nkv, g, nq, num_pages;
+  int nkv, g, nq, num_pages, B;
   const int32_t *page_table;
   int max_pages;
   const int32_t *lengths;
@@ -33,6 +33,7 @@ struct TreeArgs {
 };
 
 constexpr int kTreeWaves = 4;
+constexpr int kTreeSegStages = 128;  // page pairs whose ids (and scales) a k_tree_wide block holds at a time
 constexpr int kTreeSeg = 64 * kTreeWaves;  // pages whose ids a block's lanes hold at a time
 
 // The rows of one candidate, kept inside the arrays whatever `start` holds.
@@ -52,6 +53,55 @@ __device__ __forceinline__ TreeRows tree_rows(const TreeArgs &a, int b) {
 // Chunks of a candidate with npages cached pages.
 __device__ __forceinline__ int tree_chunks(const TreeArgs &a, int npages) {
   return max(1, min(a.chunks, (npages + a.chunk_pages - 1) / a.chunk_pages));
+}
+
+// The block's work: candidate, kv-head, chunk of its cached pages and block of its columns. The grid is
+// one-dimensional and holds the blocks that exist, candidate by candidate (a scan over the lanes finds the
+// candidate), then blocks without work, which leave at once: a grid of (chunk, column block, candidate) sides
+// leaves them in a pattern that keeps part of the compute units idle on ragged batches. Blocks go to the
+// eight XCDs in turn; the column blocks of one chunk, which read the same pages, lie eight apart, so
+// that they share an L2.
+struct TreeItem {
+  int b, j, chunk, colblock;
+};
+__device__ __forceinline__ bool tree_item(const TreeArgs &a, int cols_per_block, TreeItem &it) {
+  const int lane = threadIdx.x & 63;
+  int id = blockIdx.x;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    int items_l = 0, cb_l = 0;
+    if (b0 + lane < a.B) {
+      const TreeRows r = tree_rows(a, b0 + lane);
+      if (r.n > 0) {
+        items_l = tree_chunks(a, (r.L + kPage - 1) / kPage) * a.nkv;
+        cb_l = (r.n * a.g + cols_per_block - 1) / cols_per_block;
+      }
+    }
+    const int n_l = items_l * cb_l, cum_l = lane_scan(n_l);
+    const int total = __builtin_amdgcn_readlane(cum_l, 63);
+    if (id >= total) {
+      id -= total;
+      continue;
+    }
+    const int k = __builtin_popcountll(__ballot(id >= cum_l));
+    const int items = lane_value(items_l, k), cb = lane_value(cb_l, k);
+    id -= lane_value(cum_l, k) - items * cb;
+    const int full = items & ~7;  // items in groups of eight
+    int item;
+    if (id < full * cb) {
+      const int grp = id / (8 * cb), rem = id - grp * 8 * cb;
+      it.colblock = rem >> 3;
+      item = grp * 8 + (rem & 7);
+    } else {
+      const int rem = id - full * cb, last = items - full;
+      it.colblock = rem / last;
+      item = full + rem - it.colblock * last;
+    }
+    it.b = b0 + k;
+    it.chunk = item / a.nkv;
+    it.j = item - it.chunk * a.nkv;
+    return true;
+  }
+  return false;
 }
 
 __device__ __forceinline__ float widen(float x) { return x; }
@@ -164,8 +214,8 @@ struct Terms<float> {
 
 // o = softmax(q K^T / sqrt(d)) V for NC tiles of 16 columns (drafted token, q-head of the kv-head's
 // group), over one chunk of a candidate's cached pages; the last chunk also takes the drafted keys.
-// grid: chunk, column block, candidate x kv-head; a block's four waves take page pairs in turn and
-// join their softmax states in LDS, so that a chunk is one partial result.
+// A block's four waves take page pairs in turn and join their softmax states in LDS, so that a chunk is
+// one partial result.
 // A page pair (32 tokens) is one step: S = K Q^T, a running softmax in registers, O^T += V^T P^T, all
 // on the matrix cores with the cache's tiles as they lie in memory (see kvprm_attn.hip).
 template <int KVT, int D, int NC, typename T>
@@ -175,14 +225,13 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
   constexpr size_t TILE = (size_t)kPage * D * (KVT == 0 ? 4 : KVT == 1 ? 2 : 1);
   __shared__ floatx4 sacc[W][NC][NDB][64];
   __shared__ float2 sml[W][NC * 16];
-  const int b = blockIdx.z / a.nkv, j = blockIdx.z - b * a.nkv;
+  TreeItem it;
+  if (!tree_item(a, 16 * NC, it)) return;
+  const int b = it.b, j = it.j, c = it.chunk;
   const TreeRows tr = tree_rows(a, b);
   const int L = tr.L, n = tr.n, g = a.g;
-  const int cols = n * g, col0 = blockIdx.y * 16 * NC;
-  if (col0 >= cols || n <= 0) return;
-  const int npages = (L + kPage - 1) / kPage, c = blockIdx.x;
-  const int nc = tree_chunks(a, npages);
-  if (c >= nc) return;
+  const int cols = n * g, col0 = it.colblock * 16 * NC;
+  const int npages = (L + kPage - 1) / kPage, nc = tree_chunks(a, npages);
   const int p0 = c * a.chunk_pages, np = min(a.chunk_pages, npages - p0);
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, cn = lane & 15, cq = lane >> 4;
@@ -478,6 +527,332 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
   }
 }
 
+// ------------------------------------------------------------------------------- wide drafts
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ floatx16 mfma32(const uint4 &a, const uint4 &b, const floatx16 &c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                 __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// The same for drafts of many columns (bf16 rows): here the waves share the pages and split the
+// columns, 32 each. A stage is a page pair (32 tokens) in LDS as bf16 tiles in the stored order (fp8
+// tiles are widened on their way, exactly), double buffered, the next pair's loads in flight while one is
+// computed. 32x32x16 products: S = K Q^T (a lane holds tokens 8 i + 4 h + e, h = lane / 32, of
+// column lane % 32), softmax, O^T += V^T P^T with P in two bf16 terms, tokens in S's order (8 slots 4 h..,
+// 8 + 4 h.. of one page are one operand). The drafted keys are stages of their own behind the last
+// chunk's pages, laid out as a page pair.
+template <int KVT, int D, int W>
+__global__ __launch_bounds__(64 * W, 2) void k_tree_wide(TreeArgs a) {
+  typedef uint16_t T;
+  constexpr int KS = D / 16, NT = D / 32, TC = 2 * D;  // k steps, output tiles, 16-byte groups of a bf16 tile
+  constexpr int SC = KVT == 1 ? 2 * TC : TC;           // 16-byte groups of a pair in memory
+  constexpr int NLC = (SC + 64 * W - 1) / (64 * W);    // of these per thread, K or V
+  constexpr int SEG = kTreeSegStages;
+  __shared__ uint4 kb[2][2 * TC], vb[2][2 * TC];
+  __shared__ int id_s[2 * SEG];                        // page ids of a segment, and their scales
+  __shared__ float ksc_s[KVT == 2 ? 2 * SEG : 1], vsc_s[KVT == 2 ? 2 * SEG : 1];
+  __shared__ int bad_s;
+  TreeItem it;
+  if (!tree_item(a, 32 * W, it)) return;
+  const int b = it.b, j = it.j, c = it.chunk;
+  const TreeRows tr = tree_rows(a, b);
+  const int L = tr.L, n = tr.n, g = a.g;
+  const int npages = (L + kPage - 1) / kPage, nc = tree_chunks(a, npages);
+  const int p0 = c * a.chunk_pages, np = min(a.chunk_pages, npages - p0);
+  const int tid = threadIdx.x, lane = tid & 63, cn = lane & 31, h = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int cols = n * g, col0 = it.colblock * 32 * W + w * 32, col = col0 + cn;
+  const bool busy = col0 < cols, present = col < cols;
+  const int tok = present ? (int)(((uint32_t)col * a.ginv) >> 18) : 0;
+  const int head = j * g + (present ? col - tok * g : 0);
+  const float rs = kLog2e / sqrtf((float)D);
+  const int ncache = (np + 1) >> 1;                    // stages of cached pages
+  const int nfull = max(0, L - p0 * kPage) >> 5;       // of these, the first without a slot at or past L
+  const T *kd = (const T *)a.k + tr.r0 * a.ks + (int64_t)j * D;
+  const T *vd = (const T *)a.v + tr.r0 * a.vs + (int64_t)j * D;
+
+  uint4 qo[KS];
+  {
+    const T *q = (const T *)a.q + (tr.r0 + tok) * a.qs + (int64_t)head * D;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const uint4 v = *(const uint4 *)(q + 16 * ks + 8 * h);
+      qo[ks] = present ? v : make_uint4(0, 0, 0, 0);
+    }
+  }
+  // A stage's tiles in registers: 16-byte groups of K and V.
+  struct Pair {
+    uint4 k[NLC], v[NLC];
+  };
+  int s0 = 0, se = 0;  // the segment's stages
+  // (no branch around the loads, which would join registers still in flight: stages past the end repeat
+  // the last one)
+  auto load_stage = [&](int s, Pair &r) {
+    const int i = 2 * (min(s, se - 1) - s0);
+    constexpr size_t TILE = (size_t)kPage * D * (KVT == 1 ? 2 : 1);
+    const size_t ta = ((size_t)__builtin_amdgcn_readfirstlane(id_s[i]) * a.nkv + j) * TILE;
+    const size_t tb = ((size_t)__builtin_amdgcn_readfirstlane(id_s[i + 1]) * a.nkv + j) * TILE;
+#pragma unroll
+    for (int k = 0; k < NLC; ++k) {
+      // this wave's first group; pairs of fewer groups than threads are read twice
+      const int i0 = (k * 64 * W + w * 64) % SC;
+      const size_t t = i0 >= SC / 2 ? tb : ta;
+      r.k[k] = ((const uint4 *)(a.kp + t))[i0 % (SC / 2) + lane];
+      r.v[k] = ((const uint4 *)(a.vp + t))[i0 % (SC / 2) + lane];
+    }
+  };
+  auto store_stage = [&](int s, const Pair &r) {
+    if (s >= se) return;
+    uint4 *kt = kb[s & 1], *vt = vb[s & 1];
+    const int left = L - (p0 + 2 * s) * kPage;  // valid slots from the pair's first on
+#pragma unroll
+    for (int k = 0; k < NLC; ++k) {
+      const int i0 = (k * 64 * W + w * 64) % SC;
+      const bool second = i0 >= SC / 2;
+      const int i = i0 % (SC / 2) + lane, at = second ? TC : 0;
+      // slots at or past L may hold anything: as values they become zeros
+      uint32_t m0 = ~0u, m1 = ~0u;
+      if (left < 32) {
+        const int q = left - (second ? 16 : 0) - 4 * ((i >> 4) & 3);
+        m0 = (q > 0 ? 0xFFFFu : 0u) | (q > 1 ? 0xFFFF0000u : 0u);
+        m1 = (q > 2 ? 0xFFFFu : 0u) | (q > 3 ? 0xFFFF0000u : 0u);
+      }
+      const uint4 rk = r.k[k], rv = r.v[k];
+      if (KVT == 1) {
+        kt[at + i] = rk;
+        vt[at + i] = make_uint4(rv.x & m0, rv.y & m1, rv.z & m0, rv.w & m1);
+      } else {
+        // 16 dims of a slot -> two groups of 8; 4 dims of 4 slots -> two groups of 2
+        uint4 *kp = kt + at + (i >> 4) * 32 + (i & 15);
+        kp[0] = make_uint4(fp8x2_to_bf16x2<false>(rk.x), fp8x2_to_bf16x2<true>(rk.x),
+                           fp8x2_to_bf16x2<false>(rk.y), fp8x2_to_bf16x2<true>(rk.y));
+        kp[16] = make_uint4(fp8x2_to_bf16x2<false>(rk.z), fp8x2_to_bf16x2<true>(rk.z),
+                            fp8x2_to_bf16x2<false>(rk.w), fp8x2_to_bf16x2<true>(rk.w));
+        uint4 *vp = vt + at + (i >> 6) * 128 + (i & 63);
+        vp[0] = make_uint4(fp8x2_to_bf16x2<false>(rv.x) & m0, fp8x2_to_bf16x2<true>(rv.x) & m1,
+                           fp8x2_to_bf16x2<false>(rv.y) & m0, fp8x2_to_bf16x2<true>(rv.y) & m1);
+        vp[64] = make_uint4(fp8x2_to_bf16x2<false>(rv.z) & m0, fp8x2_to_bf16x2<true>(rv.z) & m1,
+                            fp8x2_to_bf16x2<false>(rv.w) & m0, fp8x2_to_bf16x2<true>(rv.w) & m1);
+      }
+    }
+  };
+  // 32 drafted tokens from t0 on as a page pair in buffer 0.
+  auto store_draft = [&](int t0) {
+    uint4 *kt = kb[0], *vt = vb[0];
+    bool bad = false;
+    for (int i = tid; i < 2 * TC; i += 64 * W) {
+      const int t = i / (D / 8), e = 8 * (i % (D / 8)), at = (t >> 4) * TC, sl = t & 15;
+      uint4 rk = make_uint4(0, 0, 0, 0), rv = rk;
+      if (t0 + t < n) {
+        rk = *(const uint4 *)(kd + (t0 + t) * a.ks + e);
+        rv = *(const uint4 *)(vd + (t0 + t) * a.vs + e);
+      }
+      kt[at + (e >> 3) * 16 + sl] = rk;
+      const uint32_t x[4] = {rv.x, rv.y, rv.z, rv.w};
+#pragma unroll
+      for (int y = 0; y < 8; ++y) {
+        const int mm = e + y;
+        uint32_t v = (x[y >> 1] >> (16 * (y & 1))) & 0xFFFFu;
+        // infinities and NaN leave the product (see below)
+        if ((v & 0x7F80u) == 0x7F80u) bad = true, v = 0;
+        ((uint16_t *)(vt + at))[((((mm >> 5) * 4 + (sl >> 2)) * 16 + (mm & 15)) * 2 + ((mm >> 4) & 1)) * 4 + (sl & 3)] =
+            (uint16_t)v;
+      }
+    }
+    if (bad) bad_s = 1;
+  };
+
+  float m = -INFINITY, l = 0.f;
+  floatx16 acc[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
+
+  // One stage, cached pages (d0 < 0) or the drafted tokens from d0 on; MASKED: only the tokens of `ok`
+  // (bit r: this lane's r-th) count.
+  auto compute = [&](int s, auto masked, uint32_t ok, int d0) {
+    const int buf = d0 < 0 ? s & 1 : 0;
+    const uint4 *kt = kb[buf] + (cn >> 4) * TC + h * 16 + (cn & 15);
+    const uint4 *vt = vb[buf] + (cn >> 4) * 64 + h * 16 + (cn & 15);
+    floatx16 sv;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sv[e] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) sv = mfma32(kt[ks * 32], qo[ks], sv);
+    float ka = rs, kc = rs, va = 1.f, vc = 1.f;
+    if (KVT == 2 && d0 < 0) {
+      const int i = 2 * (s - s0);
+      ka = ksc_s[i] * rs, kc = ksc_s[i + 1] * rs, va = vsc_s[i], vc = vsc_s[i + 1];
+    }
+    if (decltype(masked)::value) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sv[e] = ok >> e & 1 ? sv[e] : -INFINITY;
+    }
+    float ma = sv[0], mb = sv[8];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) {
+      ma = fmaxf(ma, sv[e]);
+      mb = fmaxf(mb, sv[8 + e]);
+    }
+    float mx = fmaxf(ma * ka, mb * kc);  // (scales are positive; -inf stays -inf)
+    {
+      const uint32_t u = __float_as_uint(mx);
+      const auto t = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+      mx = fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
+    }
+    const float mn = fmaxf(m, mx);
+    if (__any(mn > m)) {
+      const float alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= alpha;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[t][e] *= alpha;
+    }
+    const float ms = m == -INFINITY ? 0.f : m;
+    float p[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(fmaf(sv[e], e < 8 ? ka : kc, -ms));
+      if (decltype(masked)::value) p[e] = ok >> e & 1 ? p[e] : 0.f;  // (a scale of 0 times -inf)
+      l += p[e];
+    }
+    uint4 ph[2], pl[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float y0 = p[8 * x + 2 * e], y1 = p[8 * x + 2 * e + 1];
+        if (KVT == 2) {
+          y0 *= x ? vc : va;
+          y1 *= x ? vc : va;
+        }
+        split2(y0, y1, hi[e], lo[e]);
+      }
+      ph[x] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      pl[x] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; t += 2)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        // two groups of (2 dims 16 apart) x 4 slots: the two dims' operands
+        const uint4 u = vt[x * TC + t * 64], v = vt[x * TC + t * 64 + 32];
+        const uint4 o0 = make_uint4(u.x, u.y, v.x, v.y), o1 = make_uint4(u.z, u.w, v.z, v.w);
+        acc[t] = mfma32(o0, ph[x], acc[t]);
+        acc[t + 1] = mfma32(o1, ph[x], acc[t + 1]);
+        acc[t] = mfma32(o0, pl[x], acc[t]);
+        acc[t + 1] = mfma32(o1, pl[x], acc[t + 1]);
+      }
+    if (decltype(masked)::value && d0 >= 0 && bad_s) {
+      // Infinities and NaN among the drafted values: 0 times them would reach the columns that do not
+      // attend to them, so they are added column by column.
+      for (int t = 0; t < 32 && d0 + t < n; ++t) {
+        const int r = (t >> 3) * 4 + (t & 3), from = ((t >> 2) & 1) * 32 + cn;
+        float pt = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (e == r) pt = p[e];
+        pt = __shfl(pt, from, 64);
+        const bool okt = (__shfl((int)ok, from, 64) >> r & 1) != 0;
+#pragma unroll
+        for (int y = 0; y < NT; ++y)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int d = 64 * (y >> 1) + 16 * (y & 1) + 32 * (e >> 3) + 8 * ((e >> 2) & 1) + 4 * h + (e & 3);
+            const float v = widen(vd[(int64_t)(d0 + t) * a.vs + d]);
+            if (okt && !(fabsf(v) < INFINITY)) acc[y][e] += pt * v;
+          }
+      }
+    }
+  };
+
+  // this lane's tokens out of a pair's 32 bits
+  auto own_bits = [&](uint32_t bits) {
+    uint32_t ok = 0;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) ok |= (bits >> (8 * (e >> 2) + 4 * h + (e & 3)) & 1u) << e;
+    return ok;
+  };
+  const std::integral_constant<bool, false> full;
+  const std::integral_constant<bool, true> masked;
+  for (s0 = 0; s0 < ncache; s0 += SEG) {
+    se = min(ncache, s0 + SEG);
+    if (s0 > 0) __syncthreads();
+    for (int i = tid; i < 2 * (se - s0); i += 64 * W) {
+      const int id = min(max(a.page_table[(size_t)b * a.max_pages + p0 + min(2 * s0 + i, np - 1)], 0), a.num_pages - 1);
+      id_s[i] = id;
+      if (KVT == 2) {
+        ksc_s[i] = a.ksc[(size_t)id * a.nkv + j];
+        vsc_s[i] = a.vsc[(size_t)id * a.nkv + j];
+      }
+    }
+    __syncthreads();
+    Pair r0, r1;
+    load_stage(s0, r0);
+    load_stage(s0 + 1, r1);
+    store_stage(s0, r0);
+    load_stage(s0 + 2, r0);
+    __syncthreads();
+    auto step = [&](int s, Pair &r) {
+      store_stage(s + 1, r);
+      load_stage(s + 3, r);
+      __builtin_amdgcn_sched_barrier(0);
+      if (busy) compute(s, full, 0u, -1);
+      __syncthreads();
+    };
+    const int end = min(se, nfull);
+    int s = s0;
+    for (; s + 1 < end; s += 2) {
+      step(s, r1);
+      step(s + 1, r0);
+    }
+    if (s < end) step(s, r1);
+    if (end < se && busy)  // the candidate's last pair (in its buffer since the step before)
+      compute(end, masked, own_bits((1u << (L - (p0 + 2 * end) * kPage)) - 1u), -1);
+  }
+  if (c == nc - 1) {
+    for (int t0 = 0; t0 < n; t0 += 32) {
+      __syncthreads();
+      if (tid == 0) bad_s = 0;
+      __syncthreads();
+      store_draft(t0);
+      __syncthreads();
+      if (!busy) continue;
+      uint32_t bits;
+      const int own = tok - t0;
+      if (a.mask) bits = a.mask[(tr.r0 + tok) * a.mask_words + (t0 >> 5)];
+      else bits = own >= 31 ? ~0u : own < 0 ? 0u : (2u << own) - 1u;
+      if (n - t0 < 32) bits &= (1u << (n - t0)) - 1u;
+      compute(0, masked, own_bits(bits), t0);
+    }
+  }
+  if (!present) return;
+  {
+    const uint32_t u = __float_as_uint(l);
+    const auto t = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    l = __uint_as_float(t[0]) + __uint_as_float(t[1]);
+  }
+  const int64_t row = tr.r0 + tok, at = (row * a.nq + head) * a.slots + c;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int d = 64 * (t >> 1) + 16 * (t & 1) + 32 * (i >> 1) + 8 * (i & 1) + 4 * h;
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = acc[t][4 * i + e] * (nc == 1 ? inv : 1.f);
+      if (nc == 1) store4((T *)a.o + row * a.os + (int64_t)head * D + d, v);
+      else store4(a.pacc + at * D + d, v);
+    }
+  if (nc > 1 && h == 0) a.pml[at] = make_float2(m, l);
+}
+
 // Joins the chunks of one (drafted token, q-head), one wave each: weights 2^(m - M) from one load
 // per lane (at most 64 chunks), then the chunk sums in order.
 template <int D, typename T>
@@ -497,7 +872,6 @@ __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a) {
   constexpr int E = D / 64;
   float v[E] = {};
   const float *p = a.pacc + at * D + lane * E;
-#pragma unroll 8
   for (int i = 0; i < nc; ++i) {
     const float w = lane_value(f, i);
 #pragma unroll
@@ -520,25 +894,29 @@ __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a) {
 // ------------------------------------------------------------------------------- launch
 
 struct TreePlan {
-  int nc;      // column tiles of a block
+  int wide;    // waves of a k_tree_wide block, 0 = k_tree
+  int nc;      // column tiles of a k_tree block
+  int cols;    // columns of a block
   int blocks;  // column blocks of the longest draft
+  int fill;    // blocks that fill the chip
+  int unit;    // pages that a chunk is a multiple of
   int slots;   // chunk slots
 };
 
-constexpr int kTreeBlocks = 512;  // blocks that fill the chip
-
-// Column tiles per block: as many of 16 columns as the drafts can fill, at most 4 (fp32 rows, with
-// three query terms in registers, 2). Chunk slots: what fills the chip eight times over if the
-// batch's candidates were all as long as the table, one chunk being at least a page pair per wave.
+// Kernel by the longest draft's columns. Chunk slots: what fills the chip eight times over if the
+// batch's candidates were all as long as the table.
 static TreePlan tree_plan(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t) {
   TreePlan p;
   const int cols = t.max_rows * dm.g;
-  const bool wide = t.dtype == KVPRM_BF16 && dm.kvdt != 0;
-  p.nc = cols <= 16 ? 1 : cols <= 32 || !wide ? 2 : 4;
-  p.blocks = (cols + 16 * p.nc - 1) / (16 * p.nc);
+  p.wide = t.dtype == KVPRM_BF16 && dm.kvdt != 0 && cols > 32 ? (cols <= 64 ? 2 : 4) : 0;
+  p.nc = cols <= 16 ? 1 : 2;
+  p.cols = p.wide ? 32 * p.wide : 16 * p.nc;
+  p.blocks = (cols + p.cols - 1) / p.cols;
+  p.fill = p.wide ? 2048 / p.wide : 512;
+  p.unit = p.wide ? 2 : 2 * kTreeWaves;
   const int64_t items = (int64_t)b.batch * dm.nkv * p.blocks;
-  int64_t slots = (8 * kTreeBlocks + items - 1) / items;
-  slots = min(slots, (int64_t)(b.max_pages + 2 * kTreeWaves - 1) / (2 * kTreeWaves));
+  int64_t slots = (8 * p.fill + items - 1) / items;
+  slots = min(slots, (int64_t)(b.max_pages + p.unit - 1) / p.unit);
   p.slots = (int)max((int64_t)1, min(slots, (int64_t)64));
   return p;
 }
@@ -552,23 +930,21 @@ size_t tree_ws_bytes(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t) 
   return align256(parts * dm.d * 4) + align256(parts * 8);
 }
 
-// Pages of a chunk: the fewest (a page pair for each wave, and multiples of that) whose chunks
-// leave the grid within kTreeBlocks and each candidate within its slots.
+static int cached_pages(const kvprm_batch &b, int i) {
+  return b.lengths_host ? (b.lengths_host[i] + kPage - 1) / kPage : b.max_pages;
+}
+
+// Pages of a chunk: the fewest (multiples of p.unit) whose chunks leave the grid within p.fill blocks
+// and each candidate within its slots.
 static int tree_chunk_pages(const Dims &dm, const kvprm_batch &b, const TreePlan &p) {
-  constexpr int unit = 2 * kTreeWaves;
   int longest = 0;
-  for (int i = 0; i < b.batch; ++i) {
-    const int np = b.lengths_host ? (b.lengths_host[i] + kPage - 1) / kPage : b.max_pages;
-    longest = max(longest, np);
-  }
-  int cp = max(unit, ((longest + p.slots - 1) / p.slots + unit - 1) / unit * unit);
-  const int64_t most = kTreeBlocks / ((int64_t)dm.nkv * p.blocks);
-  for (;; cp += max(unit, cp / 8 / unit * unit)) {
+  for (int i = 0; i < b.batch; ++i) longest = max(longest, cached_pages(b, i));
+  const int least = p.wide ? 16 : p.unit;
+  int cp = max(least, ((longest + p.slots - 1) / p.slots + p.unit - 1) / p.unit * p.unit);
+  const int64_t most = p.fill / ((int64_t)dm.nkv * p.blocks);
+  for (;; cp += max(p.unit, cp / 8 / p.unit * p.unit)) {
     int64_t chunks = 0;
-    for (int i = 0; i < b.batch; ++i) {
-      const int np = b.lengths_host ? (b.lengths_host[i] + kPage - 1) / kPage : b.max_pages;
-      chunks += max(1, (np + cp - 1) / cp);
-    }
+    for (int i = 0; i < b.batch; ++i) chunks += max(1, (cached_pages(b, i) + cp - 1) / cp);
     if (chunks <= max(most, (int64_t)b.batch) || cp >= longest) return cp;
   }
 }
@@ -583,6 +959,7 @@ hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batc
   a.vp = (const char *)c.v_pages + layer * bytes;
   a.ksc = dm.kvdt == 2 ? c.k_scale + layer * tiles : nullptr;
   a.vsc = dm.kvdt == 2 ? c.v_scale + layer * tiles : nullptr;
+  a.B = b.batch;
   a.nkv = dm.nkv;
   a.g = dm.g;
   a.nq = dm.nq;
@@ -602,33 +979,41 @@ hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batc
   a.slots = p.slots;
   a.pacc = (float *)ws;
   a.pml = (float2 *)((char *)ws + align256((size_t)t.num_rows * dm.nq * p.slots * dm.d * 4));
-  int longest = 0;
-  for (int i = 0; i < b.batch; ++i)
-    longest = max(longest, b.lengths_host ? (b.lengths_host[i] + kPage - 1) / kPage : b.max_pages);
-  const int chunks = max(1, (longest + a.chunk_pages - 1) / a.chunk_pages);
-  a.chunks = chunks;
-  const dim3 grid(chunks, p.blocks, b.batch * dm.nkv), block(64 * kTreeWaves);
-  const bool bf16 = t.dtype == KVPRM_BF16;
-#define KVPRM_TREE(K_, D_, N_, T_) hipLaunchKernelGGL((k_tree<K_, D_, N_, T_>), grid, block, 0, s, a)
-#define KVPRM_TREE_N(K_, D_)                                  \
-  if (bf16 && K_ != 0) {                                      \
-    if (p.nc == 1) { KVPRM_TREE(K_, D_, 1, uint16_t); }       \
-    else if (p.nc == 2) { KVPRM_TREE(K_, D_, 2, uint16_t); }  \
-    else { KVPRM_TREE(K_ == 0 ? 1 : K_, D_, 4, uint16_t); }   \
-  } else if (bf16) {                                          \
-    if (p.nc == 1) { KVPRM_TREE(K_, D_, 1, uint16_t); }       \
-    else { KVPRM_TREE(K_, D_, 2, uint16_t); }                 \
-  } else {                                                    \
-    if (p.nc == 1) { KVPRM_TREE(K_, D_, 1, float); }          \
-    else { KVPRM_TREE(K_, D_, 2, float); }                    \
+  int chunks = 1;
+  int64_t items = 0;  // chunks of all candidates
+  for (int i = 0; i < b.batch; ++i) {
+    const int nc = max(1, (cached_pages(b, i) + a.chunk_pages - 1) / a.chunk_pages);
+    chunks = max(chunks, nc);
+    items += nc;
   }
-#define KVPRM_TREE_D(K_)                 \
-  if (dm.d == 64) { KVPRM_TREE_N(K_, 64) } \
-  else { KVPRM_TREE_N(K_, 128) }
-  if (dm.kvdt == 0) { KVPRM_TREE_D(0) }
+  a.chunks = chunks;
+  const dim3 grid((unsigned)(items * dm.nkv * p.blocks));
+  const bool bf16 = t.dtype == KVPRM_BF16;
+#define KVPRM_TREE(K_, D_, N_, T_) \
+  hipLaunchKernelGGL((k_tree<K_, D_, N_, T_>), grid, dim3(64 * kTreeWaves), 0, s, a)
+#define KVPRM_TREE_N(K_, D_, T_)                  \
+  if (p.nc == 1) { KVPRM_TREE(K_, D_, 1, T_); }   \
+  else { KVPRM_TREE(K_, D_, 2, T_); }
+#define KVPRM_TREE_T(K_, D_)                      \
+  if (bf16) { KVPRM_TREE_N(K_, D_, uint16_t) }    \
+  else { KVPRM_TREE_N(K_, D_, float) }
+#define KVPRM_TREE_D(K_)                          \
+  if (dm.d == 64) { KVPRM_TREE_T(K_, 64) }        \
+  else { KVPRM_TREE_T(K_, 128) }
+#define KVPRM_WIDE(K_, D_)                                                                              \
+  if (p.wide == 2) hipLaunchKernelGGL((k_tree_wide<K_, D_, 2>), grid, dim3(128), 0, s, a);              \
+  else hipLaunchKernelGGL((k_tree_wide<K_, D_, 4>), grid, dim3(256), 0, s, a)
+  if (p.wide) {
+    if (dm.kvdt == 1 && dm.d == 64) { KVPRM_WIDE(1, 64); }
+    else if (dm.kvdt == 1) { KVPRM_WIDE(1, 128); }
+    else if (dm.d == 64) { KVPRM_WIDE(2, 64); }
+    else { KVPRM_WIDE(2, 128); }
+  } else if (dm.kvdt == 0) { KVPRM_TREE_D(0) }
   else if (dm.kvdt == 1) { KVPRM_TREE_D(1) }
   else { KVPRM_TREE_D(2) }
+#undef KVPRM_WIDE
 #undef KVPRM_TREE_D
+#undef KVPRM_TREE_T
 #undef KVPRM_TREE_N
 #undef KVPRM_TREE
   hipError_t e = hipGetLastError();

@@ -248,17 +248,25 @@ def test_tree_large_scores(cdt, dtype):
 
 
 def test_tree_drops_rows():
-    """Rows past max_rows and num_rows are left alone; the others do not change."""
+    """Rows past max_rows and num_rows are left alone; the others are as in the whole call. (Fewer rows can
+    mean another kernel, whose sums have another order: each result is within the tolerance of 64 bits,
+    so their difference is within two of them.)"""
     _say("drops rows")
     c = Case("bf16", "bf16", 4, 2, 64, [40, 100], [12, 30], seed=5, masked="chain")
     full = c.run()
+    c.check(full)
+
+    def same(x, y):
+        x, y = x[:, :256].double(), y[:, :256].double()
+        return bool(torch.all((x - y).abs() <= 2 * (10 * (2.0 ** -16 + 1e-5) + 2.0 ** -8 * y.abs())))
+
     c.o.fill_(7.0)
     got = c.run(tree=c.tree(max_rows=10))
-    assert torch.equal(got[:10], full[:10]) and torch.all(got[10:12] == 7.0)
-    assert torch.equal(got[12:22], full[12:22]) and torch.all(got[22:] == 7.0)
+    assert same(got[:10], full[:10]) and torch.all(got[10:12] == 7.0)
+    assert same(got[12:22], full[12:22]) and torch.all(got[22:] == 7.0)
     c.o.fill_(7.0)
     got = c.run(tree=c.tree(num_rows=20))
-    assert torch.equal(got[:20], full[:20]) and torch.all(got[20:] == 7.0)
+    assert same(got[:20], full[:20]) and torch.all(got[20:] == 7.0)
 
 
 def test_tree_without_pages():
