@@ -2,6 +2,7 @@
 // the drafted keys, by sequence, kv-head and columns) and k_tree_merge (the chunks' join).
 #include <hip/hip_runtime.h>
 #include <math.h>
+#include <stdlib.h>
 
 #include "kvprm_attn_common.h"
 #include "kvprm_internal.h"
@@ -25,7 +26,9 @@ struct TreeArgs {
   const uint32_t *mask;
   int mask_words;
   uint32_t ginv;           // ceil(2^18 / g): c / g = (c * ginv) >> 18 for c < 4096 + 64, g <= 16
-  int chunk_pages;         // cached pages of a chunk (a multiple of 2 kTreeWaves)
+  int chunk_pages;         // most cached pages of a chunk (a multiple of unit)
+  int block_cols;          // columns of a k_tree_wide block, a multiple of 32
+  int unit;                // pages that chunks are multiples of: a step of every wave of the block
   int chunks;              // chunks of the grid: a candidate has no more
   int slots;               // chunk slots of a (row, q-head) in the workspace (at least chunks)
   float *pacc;             // [row][q-head][slot][D] chunk sums
@@ -50,9 +53,17 @@ __device__ __forceinline__ TreeRows tree_rows(const TreeArgs &a, int b) {
   return r;
 }
 
-// Chunks of a candidate with npages cached pages.
-__device__ __forceinline__ int tree_chunks(const TreeArgs &a, int npages) {
-  return max(1, min(a.chunks, (npages + a.chunk_pages - 1) / a.chunk_pages));
+// A candidate's npages cached pages in chunks of equal size (to a unit), as few as have at most
+// chunk_pages each.
+struct TreeSplit {
+  int chunks, pages;  // pages of each chunk but the last
+};
+__device__ __forceinline__ TreeSplit tree_split(const TreeArgs &a, int npages) {
+  const int most = max(1, min(a.chunks, (npages + a.chunk_pages - 1) / a.chunk_pages));
+  TreeSplit s;
+  s.pages = max(1, (npages + most * a.unit - 1) / (most * a.unit)) * a.unit;
+  s.chunks = max(1, (npages + s.pages - 1) / s.pages);
+  return s;
 }
 
 // The block's work: candidate, kv-head, chunk of its cached pages and block of its columns. The grid is
@@ -72,7 +83,7 @@ __device__ __forceinline__ bool tree_item(const TreeArgs &a, int cols_per_block,
     if (b0 + lane < a.B) {
       const TreeRows r = tree_rows(a, b0 + lane);
       if (r.n > 0) {
-        items_l = tree_chunks(a, (r.L + kPage - 1) / kPage) * a.nkv;
+        items_l = tree_split(a, (r.L + kPage - 1) / kPage).chunks * a.nkv;
         cb_l = (r.n * a.g + cols_per_block - 1) / cols_per_block;
       }
     }
@@ -231,8 +242,10 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
   const TreeRows tr = tree_rows(a, b);
   const int L = tr.L, n = tr.n, g = a.g;
   const int cols = n * g, col0 = it.colblock * 16 * NC;
-  const int npages = (L + kPage - 1) / kPage, nc = tree_chunks(a, npages);
-  const int p0 = c * a.chunk_pages, np = min(a.chunk_pages, npages - p0);
+  const int npages = (L + kPage - 1) / kPage;
+  const TreeSplit sp = tree_split(a, npages);
+  const int nc = sp.chunks;
+  const int p0 = c * sp.pages, np = min(sp.pages, npages - p0);
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, cn = lane & 15, cq = lane >> 4;
   const float rs = kLog2e / sqrtf((float)D);
@@ -253,20 +266,20 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
   for (int ct = 0; ct < NC; ++ct) st[ct].init();
 
   for (int seg = 0; seg < np; seg += kTreeSeg) {
-    const int sp = p0 + seg, sn = min(kTreeSeg, np - seg);  // pages of this segment
+    const int first = p0 + seg, sn = min(kTreeSeg, np - seg);  // pages of this segment
     if constexpr (KVT == 0) {
       // wave w takes pages w, w + W, ...; lane i holds the id of its i-th page
       const int mine = (sn - w + W - 1) / W;
       if (mine <= 0) continue;
       const int id_l =
-          min(max(a.page_table[(size_t)b * a.max_pages + sp + min(w + W * lane, sn - 1)], 0), a.num_pages - 1);
+          min(max(a.page_table[(size_t)b * a.max_pages + first + min(w + W * lane, sn - 1)], 0), a.num_pages - 1);
       float qf[NC][D / 4];
 #pragma unroll
       for (int ct = 0; ct < NC; ++ct) query32<D>(qrow(ct), cq, present[ct], qf[ct]);
       for (int i = 0; i < mine; ++i) {
         const size_t tile = ((size_t)lane_value(id_l, i) * a.nkv + j) * TILE;
         const float4 *kt = (const float4 *)(a.kp + tile), *vt = (const float4 *)(a.vp + tile);
-        const int t0 = (sp + w + W * i) * kPage + 4 * cq;
+        const int t0 = (first + w + W * i) * kPage + 4 * cq;
         bool ok[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) ok[e] = t0 + e < L;
@@ -290,7 +303,7 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
       const int pairs = (sn + 1) >> 1, mine = (pairs - w + W - 1) / W;
       if (mine <= 0) continue;
       const int pg = min(2 * (w + W * (lane >> 1)) + (lane & 1), sn - 1);
-      const int id_l = min(max(a.page_table[(size_t)b * a.max_pages + sp + pg], 0), a.num_pages - 1);
+      const int id_l = min(max(a.page_table[(size_t)b * a.max_pages + first + pg], 0), a.num_pages - 1);
       float ksc_l = 0.f, vsc_l = 0.f;
       if (KVT == 2) {
         ksc_l = a.ksc[(size_t)id_l * a.nkv + j];
@@ -335,7 +348,7 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
         const int la = 2 * i;
         const float sca = KVT == 2 ? lane_value(ksc_l, la) * rs : rs;
         const float scb = KVT == 2 ? lane_value(ksc_l, la + 1) * rs : rs;
-        const int t0 = (sp + 2 * (w + W * i)) * kPage;
+        const int t0 = (first + 2 * (w + W * i)) * kPage;
         const bool tail = t0 + 2 * kPage > L;  // slots at or past L in this pair (they may hold anything)
         const int left = L - t0 - 4 * cq;      // this lane's tokens: 0..3 of page A, 16..19 of page B
         if (tail) {
@@ -530,9 +543,53 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
 // ------------------------------------------------------------------------------- wide drafts
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ floatx16 mfma32(const uint4 &a, const uint4 &b, const floatx16 &c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
                                                  __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ floatx16 mfma32h(const uint4 &a, const uint4 &b, const floatx16 &c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(halfx8, a),
+                                                __builtin_bit_cast(halfx8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ uint32_t half2(float x, float y) {  // nearest even
+  typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
+  typedef float f32x2v __attribute__((ext_vector_type(2)));
+  const f32x2v v = {x, y};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, halfx2));
+}
+template <bool HIGH>
+__device__ __forceinline__ uint32_t fp8x2_to_half2(uint32_t word) {  // (every e4m3 value is an fp16 value)
+  typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
+  const halfx2 v = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(word, 1.0f, HIGH);
+  return __builtin_bit_cast(uint32_t, v);
+}
+// The largest of 64 lanes' values (unsigned), as a scalar.
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+  auto step = [](uint32_t x, uint32_t y) { return x > y ? x : y; };
+  v = step(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false));  // as in lane_scan
+  v = step(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false));
+  v = step(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false));
+  v = step(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false));
+  v = step(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));
+  v = step(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false));
+  return __builtin_amdgcn_readlane(v, 63);
+}
+// Exponent that bf16 values of the largest magnitude `mag` (bits) are divided by on their way to fp16:
+// it comes to lie in [2^14, 2^15). Values down to 2^-28 of it keep all their bits, smaller ones become 0.
+__device__ __forceinline__ int half_exponent(uint32_t mag) {
+  return mag == 0 ? 0 : max((int)(mag >> 7) - 141, -112);
+}
+// Two bf16 values divided by 2^(bias / 128 - 112) as fp16; `bias` in both halves.
+__device__ __forceinline__ uint32_t bf16x2_to_half2(uint32_t x, uint32_t bias) {
+  const ushortx2 m = __builtin_bit_cast(ushortx2, x & 0x7FFF7FFFu);
+  const ushortx2 r = __builtin_elementwise_sub_sat(m, __builtin_bit_cast(ushortx2, bias)) << 3;
+  return (x & 0x80008000u) | __builtin_bit_cast(uint32_t, r);
+}
+__device__ __forceinline__ uint32_t max_mag(uint32_t m, uint32_t x) {  // by halves
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushortx2, m),
+                                                                __builtin_bit_cast(ushortx2, x & 0x7FFF7FFFu)));
 }
 
 // The same for drafts of many columns (bf16 rows): here the waves share the pages and split the
@@ -549,21 +606,25 @@ __global__ __launch_bounds__(64 * W, 2) void k_tree_wide(TreeArgs a) {
   constexpr int SC = KVT == 1 ? 2 * TC : TC;           // 16-byte groups of a pair in memory
   constexpr int NLC = (SC + 64 * W - 1) / (64 * W);    // of these per thread, K or V
   constexpr int SEG = kTreeSegStages;
+  constexpr bool HALF = KVT == 2;  // values and weights in fp16
   __shared__ uint4 kb[2][2 * TC], vb[2][2 * TC];
-  __shared__ int id_s[2 * SEG];                        // page ids of a segment, and their scales
-  __shared__ float ksc_s[KVT == 2 ? 2 * SEG : 1], vsc_s[KVT == 2 ? 2 * SEG : 1];
+  __shared__ int id_s[2 * SEG + 12];                    // page ids of a segment, and their scales
+  __shared__ float ksc_s[KVT == 2 ? 2 * SEG + 12 : 1], vsc_s[KVT == 2 ? 2 * SEG + 12 : 1];
+  __shared__ uint32_t mag_s;  // largest magnitude of the drafted values of a stage
   __shared__ int bad_s;
   TreeItem it;
-  if (!tree_item(a, 32 * W, it)) return;
+  if (!tree_item(a, a.block_cols, it)) return;
   const int b = it.b, j = it.j, c = it.chunk;
   const TreeRows tr = tree_rows(a, b);
   const int L = tr.L, n = tr.n, g = a.g;
-  const int npages = (L + kPage - 1) / kPage, nc = tree_chunks(a, npages);
-  const int p0 = c * a.chunk_pages, np = min(a.chunk_pages, npages - p0);
+  const int npages = (L + kPage - 1) / kPage;
+  const TreeSplit sp = tree_split(a, npages);
+  const int nc = sp.chunks;
+  const int p0 = c * sp.pages, np = min(sp.pages, npages - p0);
   const int tid = threadIdx.x, lane = tid & 63, cn = lane & 31, h = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int cols = n * g, col0 = it.colblock * 32 * W + w * 32, col = col0 + cn;
-  const bool busy = col0 < cols, present = col < cols;
+  const int cols = n * g, col0 = it.colblock * a.block_cols + w * 32, col = col0 + cn;
+  const bool busy = col0 < cols && w * 32 < a.block_cols, present = busy && col < cols;
   const int tok = present ? (int)(((uint32_t)col * a.ginv) >> 18) : 0;
   const int head = j * g + (present ? col - tok * g : 0);
   const float rs = kLog2e / sqrtf((float)D);
@@ -581,86 +642,129 @@ __global__ __launch_bounds__(64 * W, 2) void k_tree_wide(TreeArgs a) {
       qo[ks] = present ? v : make_uint4(0, 0, 0, 0);
     }
   }
-  // A stage's tiles in registers: 16-byte groups of K and V.
-  struct Pair {
-    uint4 k[NLC], v[NLC];
+  // A stage's keys or values in registers, as 16-byte groups in memory order. (No branch around loads,
+  // which would join registers still in flight: stages past the segment's end repeat its last page.)
+  struct Half {
+    uint4 g[NLC];
   };
-  int s0 = 0, se = 0;  // the segment's stages
-  // (no branch around the loads, which would join registers still in flight: stages past the end repeat
-  // the last one)
-  auto load_stage = [&](int s, Pair &r) {
-    const int i = 2 * (min(s, se - 1) - s0);
+  int s0 = 0, se = 0;         // the segment's stages
+  int kid_l = 0, vid_l = 0;   // lane i: page id i of the 64 that the key (value) loads are in
+  auto load_half = [&](const char *pool, int s, int &id_l, Half &r) {
+    const int i = 2 * (s - s0);
+    if ((i & 63) == 0) id_l = id_s[min(i + lane, 2 * SEG + 11)];
     constexpr size_t TILE = (size_t)kPage * D * (KVT == 1 ? 2 : 1);
-    const size_t ta = ((size_t)__builtin_amdgcn_readfirstlane(id_s[i]) * a.nkv + j) * TILE;
-    const size_t tb = ((size_t)__builtin_amdgcn_readfirstlane(id_s[i + 1]) * a.nkv + j) * TILE;
+    const int ia = lane_value(id_l, i & 63), ib = lane_value(id_l, (i & 63) + 1);
 #pragma unroll
     for (int k = 0; k < NLC; ++k) {
       // this wave's first group; pairs of fewer groups than threads are read twice
       const int i0 = (k * 64 * W + w * 64) % SC;
-      const size_t t = i0 >= SC / 2 ? tb : ta;
-      r.k[k] = ((const uint4 *)(a.kp + t))[i0 % (SC / 2) + lane];
-      r.v[k] = ((const uint4 *)(a.vp + t))[i0 % (SC / 2) + lane];
+      const char *t = pool + ((size_t)(i0 >= SC / 2 ? ib : ia) * a.nkv + j) * TILE + (i0 % (SC / 2)) * 16;
+      r.g[k] = *(const uint4 *)(t + (uint32_t)(lane * 16));
     }
   };
-  auto store_stage = [&](int s, const Pair &r) {
-    if (s >= se) return;
-    uint4 *kt = kb[s & 1], *vt = vb[s & 1];
-    const int left = L - (p0 + 2 * s) * kPage;  // valid slots from the pair's first on
+  auto load_keys = [&](int s, Half &r) { load_half(a.kp, s, kid_l, r); };
+  auto load_values = [&](int s, Half &r) { load_half(a.vp, s, vid_l, r); };
+  // Keys: group (8 dims c, page, slot) at 32 c + 16 page + slot: step ks of the products reads groups
+  // 64 ks + lane.
+  auto store_keys = [&](int s, const Half &r) {
+    uint4 *kt = kb[s & 1];
 #pragma unroll
     for (int k = 0; k < NLC; ++k) {
-      const int i0 = (k * 64 * W + w * 64) % SC;
-      const bool second = i0 >= SC / 2;
-      const int i = i0 % (SC / 2) + lane, at = second ? TC : 0;
-      // slots at or past L may hold anything: as values they become zeros
-      uint32_t m0 = ~0u, m1 = ~0u;
-      if (left < 32) {
-        const int q = left - (second ? 16 : 0) - 4 * ((i >> 4) & 3);
-        m0 = (q > 0 ? 0xFFFFu : 0u) | (q > 1 ? 0xFFFF0000u : 0u);
-        m1 = (q > 2 ? 0xFFFFu : 0u) | (q > 3 ? 0xFFFF0000u : 0u);
-      }
-      const uint4 rk = r.k[k], rv = r.v[k];
+      const int i0 = (k * 64 * W + w * 64) % SC, i = i0 % (SC / 2) + lane;
+      const int at = (i >> 4) * (KVT == 1 ? 32 : 64) + (i0 >= SC / 2 ? 16 : 0) + (i & 15);
+      const uint4 x = r.g[k];
       if (KVT == 1) {
-        kt[at + i] = rk;
-        vt[at + i] = make_uint4(rv.x & m0, rv.y & m1, rv.z & m0, rv.w & m1);
-      } else {
-        // 16 dims of a slot -> two groups of 8; 4 dims of 4 slots -> two groups of 2
-        uint4 *kp = kt + at + (i >> 4) * 32 + (i & 15);
-        kp[0] = make_uint4(fp8x2_to_bf16x2<false>(rk.x), fp8x2_to_bf16x2<true>(rk.x),
-                           fp8x2_to_bf16x2<false>(rk.y), fp8x2_to_bf16x2<true>(rk.y));
-        kp[16] = make_uint4(fp8x2_to_bf16x2<false>(rk.z), fp8x2_to_bf16x2<true>(rk.z),
-                            fp8x2_to_bf16x2<false>(rk.w), fp8x2_to_bf16x2<true>(rk.w));
-        uint4 *vp = vt + at + (i >> 6) * 128 + (i & 63);
-        vp[0] = make_uint4(fp8x2_to_bf16x2<false>(rv.x) & m0, fp8x2_to_bf16x2<true>(rv.x) & m1,
-                           fp8x2_to_bf16x2<false>(rv.y) & m0, fp8x2_to_bf16x2<true>(rv.y) & m1);
-        vp[64] = make_uint4(fp8x2_to_bf16x2<false>(rv.z) & m0, fp8x2_to_bf16x2<true>(rv.z) & m1,
-                            fp8x2_to_bf16x2<false>(rv.w) & m0, fp8x2_to_bf16x2<true>(rv.w) & m1);
+        kt[at] = x;
+      } else {  // 16 dims of a slot -> two groups of 8
+        kt[at] = make_uint4(fp8x2_to_bf16x2<false>(x.x), fp8x2_to_bf16x2<true>(x.x),
+                            fp8x2_to_bf16x2<false>(x.y), fp8x2_to_bf16x2<true>(x.y));
+        kt[at + 32] = make_uint4(fp8x2_to_bf16x2<false>(x.z), fp8x2_to_bf16x2<true>(x.z),
+                                 fp8x2_to_bf16x2<false>(x.w), fp8x2_to_bf16x2<true>(x.w));
       }
     }
   };
-  // 32 drafted tokens from t0 on as a page pair in buffer 0.
-  auto store_draft = [&](int t0) {
-    uint4 *kt = kb[0], *vt = vb[0];
-    bool bad = false;
-    for (int i = tid; i < 2 * TC; i += 64 * W) {
-      const int t = i / (D / 8), e = 8 * (i % (D / 8)), at = (t >> 4) * TC, sl = t & 15;
-      uint4 rk = make_uint4(0, 0, 0, 0), rv = rk;
-      if (t0 + t < n) {
-        rk = *(const uint4 *)(kd + (t0 + t) * a.ks + e);
-        rv = *(const uint4 *)(vd + (t0 + t) * a.vs + e);
-      }
-      kt[at + (e >> 3) * 16 + sl] = rk;
-      const uint32_t x[4] = {rv.x, rv.y, rv.z, rv.w};
+  // Values: 4 slots 4 q .. of dim 32 t + mm of a page, 8 bytes, at [page][t][q & 1][mm][q >> 1]: the
+  // product of page and tile t reads groups 64 t + lane of the page.
+  auto value_at = [&](int t, int mm, int q) { return ((t * 2 + (q & 1)) * 32 + mm) * 2 + (q >> 1); };
+  auto store_values = [&](int s, const Half &r) {
 #pragma unroll
-      for (int y = 0; y < 8; ++y) {
-        const int mm = e + y;
-        uint32_t v = (x[y >> 1] >> (16 * (y & 1))) & 0xFFFFu;
+    for (int k = 0; k < NLC; ++k) {
+      const int i0 = (k * 64 * W + w * 64) % SC, i = i0 % (SC / 2) + lane;
+      const bool second = i0 >= SC / 2;
+      uint2 *vt = (uint2 *)(vb[s & 1] + (second ? TC : 0));
+      const int q = (i >> 4) & 3, mm = i & 15;
+      uint4 x = r.g[k];
+      if (s >= nfull) {  // slots at or past L may hold anything: they become zeros
+        const int have = L - (p0 + 2 * s + second) * kPage - 4 * q;
+        if (KVT == 1) {
+          const uint32_t m0 = (have > 0 ? 0xFFFFu : 0u) | (have > 1 ? 0xFFFF0000u : 0u);
+          const uint32_t m1 = (have > 2 ? 0xFFFFu : 0u) | (have > 3 ? 0xFFFF0000u : 0u);
+          x = make_uint4(x.x & m0, x.y & m1, x.z & m0, x.w & m1);
+        } else {
+          const uint32_t m0 = have <= 0 ? 0u : have > 3 ? ~0u : (1u << 8 * have) - 1u;
+          x = make_uint4(x.x & m0, x.y & m0, x.z & m0, x.w & m0);
+        }
+      }
+      if (KVT == 1) {  // dims mm and mm + 16 of tile t
+        const int t = i0 % (SC / 2) >> 6;
+        vt[value_at(t, mm, q)] = make_uint2(x.x, x.y);
+        vt[value_at(t, mm + 16, q)] = make_uint2(x.z, x.w);
+      } else {  // dims mm, mm + 16, .. + 48 of 64
+        const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          vt[value_at(2 * (i >> 6) + (e >> 1), mm + 16 * (e & 1), q)] =
+              make_uint2(fp8x2_to_half2<false>(y[e]), fp8x2_to_half2<true>(y[e]));
+      }
+    }
+  };
+  // 32 drafted tokens from t0 on as a page pair in buffer 0 (in fp16: one exponent for all their values).
+  auto store_draft = [&](int t0) {
+    constexpr int ND = (2 * TC + 64 * W - 1) / (64 * W);
+    uint4 *kt = kb[0];
+    uint16_t *vt = (uint16_t *)vb[0];
+    uint4 rv[ND];
+    uint32_t mag = 0;
+    bool bad = false;
+#pragma unroll
+    for (int k = 0; k < ND; ++k) {
+      const int i = k * 64 * W + tid, t = i / (D / 8), e = 8 * (i % (D / 8));
+      rv[k] = make_uint4(0, 0, 0, 0);
+      uint4 rk = rv[k];
+      if (i < 2 * TC && t0 + t < n) {
+        rk = *(const uint4 *)(kd + (t0 + t) * a.ks + e);
+        rv[k] = *(const uint4 *)(vd + (t0 + t) * a.vs + e);
+      }
+      if (i < 2 * TC) kt[(e >> 3) * 32 + t] = rk;
+      uint32_t *x = (uint32_t *)&rv[k];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
         // infinities and NaN leave the product (see below)
-        if ((v & 0x7F80u) == 0x7F80u) bad = true, v = 0;
-        ((uint16_t *)(vt + at))[((((mm >> 5) * 4 + (sl >> 2)) * 16 + (mm & 15)) * 2 + ((mm >> 4) & 1)) * 4 + (sl & 3)] =
-            (uint16_t)v;
+        if ((x[y] & 0x7F80u) == 0x7F80u) bad = true, x[y] &= 0xFFFF0000u;
+        if ((x[y] & 0x7F800000u) == 0x7F800000u) bad = true, x[y] &= 0xFFFFu;
+        mag = max_mag(mag, x[y]);
       }
     }
     if (bad) bad_s = 1;
+    uint32_t bias = 0;
+    if (HALF) {
+      mag = lanes_max(max(mag & 0xFFFFu, mag >> 16));
+      if (lane == 0) atomicMax(&mag_s, mag);
+      __syncthreads();
+      bias = (uint32_t)(112 + half_exponent(mag_s)) * 0x00800080u;
+    }
+#pragma unroll
+    for (int k = 0; k < ND; ++k) {
+      const int i = k * 64 * W + tid, t = i / (D / 8), e = 8 * (i % (D / 8)), sl = t & 15;
+      if (i >= 2 * TC) continue;
+      const uint32_t *x = (const uint32_t *)&rv[k];
+#pragma unroll
+      for (int y = 0; y < 8; ++y) {
+        const int mm = e + y;
+        vt[((t >> 4) * 2 * TC + value_at(mm >> 5, mm & 31, sl >> 2)) * 4 + (sl & 3)] =
+            (uint16_t)((HALF ? bf16x2_to_half2(x[y >> 1], bias) : x[y >> 1]) >> (16 * (y & 1)));
+      }
+    }
   };
 
   float m = -INFINITY, l = 0.f;
@@ -669,41 +773,47 @@ __global__ __launch_bounds__(64 * W, 2) void k_tree_wide(TreeArgs a) {
   for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
+  // fp16 values: acc is in units of 2^unit, the exponent that values or their scales were divided by.
+  int unit = 0;
+  auto to_unit = [&](int to) {
+    if (!HALF || to == unit) return;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[t][e] = ldexpf(acc[t][e], unit - to);  // (exact)
+    unit = to;
+  };
 
-  // One stage, cached pages (d0 < 0) or the drafted tokens from d0 on; MASKED: only the tokens of `ok`
-  // (bit r: this lane's r-th) count.
-  auto compute = [&](int s, auto masked, uint32_t ok, int d0) {
-    const int buf = d0 < 0 ? s & 1 : 0;
-    const uint4 *kt = kb[buf] + (cn >> 4) * TC + h * 16 + (cn & 15);
-    const uint4 *vt = vb[buf] + (cn >> 4) * 64 + h * 16 + (cn & 15);
-    floatx16 sv;
+  // The pair in buffer `buf`: its keys as operands, and from them the scores, unscaled.
+  auto keys = [&](int buf, uint4 (&ko)[KS]) {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) ko[ks] = kb[buf][ks * 64 + lane];
+  };
+  auto scores = [&](const uint4 (&ko)[KS], floatx16 &sv) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) sv[e] = 0.f;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) sv = mfma32(kt[ks * 32], qo[ks], sv);
-    float ka = rs, kc = rs, va = 1.f, vc = 1.f;
-    if (KVT == 2 && d0 < 0) {
-      const int i = 2 * (s - s0);
-      ka = ksc_s[i] * rs, kc = ksc_s[i + 1] * rs, va = vsc_s[i], vc = vsc_s[i + 1];
-    }
-    if (decltype(masked)::value) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sv[e] = ok >> e & 1 ? sv[e] : -INFINITY;
-    }
+    for (int ks = 0; ks < KS; ++ks) sv = mfma32(ko[ks], qo[ks], sv);
+  };
+  // The largest of a column's scores sv, of pages with scales ka, kc (positive; -inf stays -inf).
+  auto largest = [&](const floatx16 &sv, float ka, float kc) {
     float ma = sv[0], mb = sv[8];
 #pragma unroll
     for (int e = 1; e < 8; ++e) {
       ma = fmaxf(ma, sv[e]);
       mb = fmaxf(mb, sv[8 + e]);
     }
-    float mx = fmaxf(ma * ka, mb * kc);  // (scales are positive; -inf stays -inf)
-    {
-      const uint32_t u = __float_as_uint(mx);
-      const auto t = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-      mx = fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
-    }
-    const float mn = fmaxf(m, mx);
-    if (__any(mn > m)) {
+    const float mx = fmaxf(ma * ka, mb * kc);
+    const uint32_t u = __float_as_uint(mx);
+    const auto t = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
+  };
+  // The weights are 2^(score - m). m lies 8 below the largest score when it was set and moves when one
+  // comes to lie more than 12 above it, which leaves out most of the rescaling: the weights stay below
+  // 2^12, and those that fp16 holds with fewer bits, below 2^-14, are 2^-22 of the largest or less.
+  auto new_max = [&](float mx) {
+    if (__any(mx > m + 12.f)) {
+      const float mn = fmaxf(m, mx - 8.f);
       const float alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
       m = mn;
       l *= alpha;
@@ -712,43 +822,98 @@ __global__ __launch_bounds__(64 * W, 2) void k_tree_wide(TreeArgs a) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[t][e] *= alpha;
     }
-    const float ms = m == -INFINITY ? 0.f : m;
-    float p[16];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(fmaf(sv[e], e < 8 ? ka : kc, -ms));
-      if (decltype(masked)::value) p[e] = ok >> e & 1 ? p[e] : 0.f;  // (a scale of 0 times -inf)
-      l += p[e];
-    }
-    uint4 ph[2], pl[2];
+  };
+  // P's operands by page: fp16 values take the weights in fp16 (times their pages' scales va, vc), bf16
+  // values in two bf16 terms.
+  auto operands = [&](const float (&p)[16], float va, float vc, uint4 (&ph)[2], uint4 (&pl)[2]) {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       uint32_t hi[4], lo[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float y0 = p[8 * x + 2 * e], y1 = p[8 * x + 2 * e + 1];
-        if (KVT == 2) {
-          y0 *= x ? vc : va;
-          y1 *= x ? vc : va;
+        const float y0 = p[8 * x + 2 * e], y1 = p[8 * x + 2 * e + 1];
+        if (HALF) {
+          const float f = x ? vc : va;
+          hi[e] = half2(y0 * f, y1 * f);
+          lo[e] = 0;
+        } else {
+          split2(y0, y1, hi[e], lo[e]);
         }
-        split2(y0, y1, hi[e], lo[e]);
       }
       ph[x] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
       pl[x] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
     }
+  };
+  auto values = [&](int buf, uint4 (&vo)[2][NT]) {
 #pragma unroll
-    for (int t = 0; t < NT; t += 2)
+    for (int x = 0; x < 2; ++x)
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        // two groups of (2 dims 16 apart) x 4 slots: the two dims' operands
-        const uint4 u = vt[x * TC + t * 64], v = vt[x * TC + t * 64 + 32];
-        const uint4 o0 = make_uint4(u.x, u.y, v.x, v.y), o1 = make_uint4(u.z, u.w, v.z, v.w);
-        acc[t] = mfma32(o0, ph[x], acc[t]);
-        acc[t + 1] = mfma32(o1, ph[x], acc[t + 1]);
-        acc[t] = mfma32(o0, pl[x], acc[t]);
-        acc[t + 1] = mfma32(o1, pl[x], acc[t + 1]);
-      }
-    if (decltype(masked)::value && d0 >= 0 && bad_s) {
+      for (int t = 0; t < NT; ++t) vo[x][t] = vb[buf][x * TC + t * 64 + lane];
+  };
+  // (ua, uc: the units that the two pages' products come in)
+  auto products = [&](const uint4 (&vo)[2][NT], const uint4 (&ph)[2], const uint4 (&pl)[2], int ua, int uc) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      to_unit(x ? uc : ua);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        acc[t] = HALF ? mfma32h(vo[x][t], ph[x], acc[t]) : mfma32(vo[x][t], ph[x], acc[t]);
+      if (!HALF)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[t] = mfma32(vo[x][t], pl[x], acc[t]);
+    }
+  };
+  // Scales of stage s's keys and values (s < 0: drafted tokens); a page's value scale as a factor in
+  // [2^-3, 2^3] and a unit, which is kept from page to page while that allows.
+  struct Scales {
+    float ka, kc, va, vc;
+    int ua, uc;
+  };
+  int last = 0;
+  auto scales = [&](int s) {
+    Scales r = {rs, rs, 1.f, 1.f, 0, 0};
+    if (KVT == 2 && s >= 0) {
+      const int i = 2 * (s - s0);
+      r.ka = ksc_s[i] * rs, r.kc = ksc_s[i + 1] * rs;
+      auto one = [&](float v, float &f) {
+        f = ldexpf(v, -last);
+        if (!(f >= 0.125f && f <= 8.f) && v > 0.f && v < INFINITY) {
+          last = (int)(__float_as_uint(v) >> 23) - 127;
+          f = ldexpf(v, -last);
+        }
+        last = __builtin_amdgcn_readfirstlane(last);  // (the same in every lane)
+        return last;
+      };
+      r.ua = one(vsc_s[i], r.va);
+      r.uc = one(vsc_s[i + 1], r.vc);
+    }
+    if (HALF && s < 0) r.ua = r.uc = __builtin_amdgcn_readfirstlane(half_exponent(mag_s));
+    return r;
+  };
+  // A pair of which only the tokens of `ok` (bit r: this lane's r-th) count: the candidate's last cached
+  // one (stage s), or (s < 0) the drafted tokens from d0 on.
+  auto compute_masked = [&](int s, int buf, uint32_t ok, int d0) {
+    floatx16 sv;
+    uint4 ko[KS], vo[2][NT];
+    keys(buf & 1, ko);
+    scores(ko, sv);
+    const Scales sc = scales(s);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sv[e] = ok >> e & 1 ? sv[e] : -INFINITY;
+    new_max(largest(sv, sc.ka, sc.kc));
+    const float ms = m == -INFINITY ? 0.f : m;
+    float p[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      // (selected once more: a scale of 0 times -inf is NaN)
+      p[e] = ok >> e & 1 ? __builtin_amdgcn_exp2f(fmaf(sv[e], e < 8 ? sc.ka : sc.kc, -ms)) : 0.f;
+      l += p[e];
+    }
+    uint4 ph[2], pl[2];
+    operands(p, sc.va, sc.vc, ph, pl);
+    values(buf & 1, vo);
+    products(vo, ph, pl, sc.ua, sc.uc);
+    if (s < 0 && bad_s) {
       // Infinities and NaN among the drafted values: 0 times them would reach the columns that do not
       // attend to them, so they are added column by column.
       for (int t = 0; t < 32 && d0 + t < n; ++t) {
@@ -763,7 +928,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_tree_wide(TreeArgs a) {
         for (int y = 0; y < NT; ++y)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const int d = 64 * (y >> 1) + 16 * (y & 1) + 32 * (e >> 3) + 8 * ((e >> 2) & 1) + 4 * h + (e & 3);
+            const int d = 32 * y + 8 * (e >> 2) + 4 * h + (e & 3);
             const float v = widen(vd[(int64_t)(d0 + t) * a.vs + d]);
             if (okt && !(fabsf(v) < INFINITY)) acc[y][e] += pt * v;
           }
@@ -778,12 +943,11 @@ __global__ __launch_bounds__(64 * W, 2) void k_tree_wide(TreeArgs a) {
     for (int e = 0; e < 16; ++e) ok |= (bits >> (8 * (e >> 2) + 4 * h + (e & 3)) & 1u) << e;
     return ok;
   };
-  const std::integral_constant<bool, false> full;
-  const std::integral_constant<bool, true> masked;
   for (s0 = 0; s0 < ncache; s0 += SEG) {
     se = min(ncache, s0 + SEG);
     if (s0 > 0) __syncthreads();
-    for (int i = tid; i < 2 * (se - s0); i += 64 * W) {
+    // (12 more than the segment's: the loads run five stages past its end)
+    for (int i = tid; i < min(2 * (se - s0) + 12, 2 * SEG + 12); i += 64 * W) {
       const int id = min(max(a.page_table[(size_t)b * a.max_pages + p0 + min(2 * s0 + i, np - 1)], 0), a.num_pages - 1);
       id_s[i] = id;
       if (KVT == 2) {
@@ -792,33 +956,71 @@ __global__ __launch_bounds__(64 * W, 2) void k_tree_wide(TreeArgs a) {
       }
     }
     __syncthreads();
-    Pair r0, r1;
-    load_stage(s0, r0);
-    load_stage(s0 + 1, r1);
-    store_stage(s0, r0);
-    load_stage(s0 + 2, r0);
+    // Keys run a stage ahead of values: while stage s is turned into weights (vector instructions), the
+    // matrix cores form the scores of stage s + 1. In flight beyond that: keys of the next two stages, and
+    // values.
+    Half k0, k1, v0, v1;
+    load_keys(s0, k0);
+    load_values(s0, v0);
+    load_keys(s0 + 1, k1);
+    load_values(s0 + 1, v1);
+    store_keys(s0, k0);
+    store_values(s0, v0);
+    load_keys(s0 + 2, k0);
+    store_keys(s0 + 1, k1);
+    load_values(s0 + 2, v0);
+    load_keys(s0 + 3, k1);
     __syncthreads();
-    auto step = [&](int s, Pair &r) {
-      store_stage(s + 1, r);
-      load_stage(s + 3, r);
-      __builtin_amdgcn_sched_barrier(0);
-      if (busy) compute(s, full, 0u, -1);
+    floatx16 sv;
+    if (busy) {
+      uint4 ko[KS];
+      keys(s0 & 1, ko);
+      scores(ko, sv);
+    }
+    __syncthreads();
+    const int end = min(se, nfull);
+    auto step = [&](int s, Half &kr, Half &vr) {
+      // (key buffer s & 1 is free: its scores were formed a step ago)
+      auto stage = [&] {
+        store_keys(s + 2, kr);
+        store_values(s + 1, vr);
+        load_keys(s + 4, kr);
+        load_values(s + 3, vr);
+      };
+      if (busy) {
+        const Scales sc = scales(s);
+        new_max(largest(sv, sc.ka, sc.kc));
+        float p[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(fmaf(sv[e], e < 8 ? sc.ka : sc.kc, -m));
+          l += p[e];
+        }
+        uint4 ph[2], pl[2], ko[KS], vo[2][NT];
+        keys((s + 1) & 1, ko);
+        scores(ko, sv);
+        stage();
+        operands(p, sc.va, sc.vc, ph, pl);
+        values(s & 1, vo);
+        products(vo, ph, pl, sc.ua, sc.uc);
+      } else {
+        stage();
+      }
       __syncthreads();
     };
-    const int end = min(se, nfull);
     int s = s0;
     for (; s + 1 < end; s += 2) {
-      step(s, r1);
-      step(s + 1, r0);
+      step(s, k0, v1);
+      step(s + 1, k1, v0);
     }
-    if (s < end) step(s, r1);
-    if (end < se && busy)  // the candidate's last pair (in its buffer since the step before)
-      compute(end, masked, own_bits((1u << (L - (p0 + 2 * end) * kPage)) - 1u), -1);
+    if (s < end) step(s, k0, v1);
+    if (end < se && busy)  // the candidate's last pair (in its buffers since the steps before)
+      compute_masked(end, end, own_bits((1u << (L - (p0 + 2 * end) * kPage)) - 1u), -1);
   }
   if (c == nc - 1) {
     for (int t0 = 0; t0 < n; t0 += 32) {
       __syncthreads();
-      if (tid == 0) bad_s = 0;
+      if (tid == 0) bad_s = 0, mag_s = 0;
       __syncthreads();
       store_draft(t0);
       __syncthreads();
@@ -828,7 +1030,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_tree_wide(TreeArgs a) {
       if (a.mask) bits = a.mask[(tr.r0 + tok) * a.mask_words + (t0 >> 5)];
       else bits = own >= 31 ? ~0u : own < 0 ? 0u : (2u << own) - 1u;
       if (n - t0 < 32) bits &= (1u << (n - t0)) - 1u;
-      compute(0, masked, own_bits(bits), t0);
+      compute_masked(-1, 0, own_bits(bits), t0);
     }
   }
   if (!present) return;
@@ -843,51 +1045,67 @@ __global__ __launch_bounds__(64 * W, 2) void k_tree_wide(TreeArgs a) {
   for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int d = 64 * (t >> 1) + 16 * (t & 1) + 32 * (i >> 1) + 8 * (i & 1) + 4 * h;
+      const int d = 32 * t + 8 * i + 4 * h;
       float v[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = acc[t][4 * i + e] * (nc == 1 ? inv : 1.f);
+      for (int e = 0; e < 4; ++e)  // (parts: without the weights' 2^8)
+        v[e] = nc == 1 ? ldexpf(acc[t][4 * i + e] * inv, unit) : ldexpf(acc[t][4 * i + e], unit - 8);
       if (nc == 1) store4((T *)a.o + row * a.os + (int64_t)head * D + d, v);
       else store4(a.pacc + at * D + d, v);
     }
-  if (nc > 1 && h == 0) a.pml[at] = make_float2(m, l);
+  if (nc > 1 && h == 0) a.pml[at] = make_float2(m + 8.f, l * 0.00390625f);
 }
 
 // Joins the chunks of one (drafted token, q-head), one wave each: weights 2^(m - M) from one load
-// per lane (at most 64 chunks), then the chunk sums in order.
+// per lane (at most 64 chunks), then the chunk sums in order, two chunks at a time (one per half of the
+// wave, 16 or 8 bytes a lane) and four such pairs in flight.
 template <int D, typename T>
 __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a) {
-  const int b = blockIdx.y, lane = threadIdx.x & 63;
+  const int b = blockIdx.y, lane = threadIdx.x & 63, half = lane >> 5;
   const int item = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (threadIdx.x >> 6));
   const TreeRows tr = tree_rows(a, b);
   const int t = item / a.nq, head = item - t * a.nq;
-  const int npages = (tr.L + kPage - 1) / kPage;
-  const int nc = tree_chunks(a, npages);
+  const int nc = tree_split(a, (tr.L + kPage - 1) / kPage).chunks;
   if (t >= tr.n || nc == 1) return;
   const int64_t row = tr.r0 + t, at = (row * a.nq + head) * a.slots;
+  constexpr int E = D / 32;
+  typedef float vec __attribute__((ext_vector_type(E)));
+  const vec *p = (const vec *)(a.pacc + at * D) + (lane & 31);
   const float2 ml = lane < nc ? a.pml[at + lane] : make_float2(-INFINITY, 0.f);
+  vec x[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) x[u] = p[(size_t)min(2 * u + half, nc - 1) * 32];
   const float M = wmax(ml.x);
   const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
   const float l = wsum(f * ml.y);
-  constexpr int E = D / 64;
-  float v[E] = {};
-  const float *p = a.pacc + at * D + lane * E;
-  for (int i = 0; i < nc; ++i) {
-    const float w = lane_value(f, i);
+  vec v = {};
+  for (int i = 0; i < nc; i += 8) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] += w * p[(size_t)i * D + e];
+    for (int u = 0; u < 4; ++u) {
+      const int k = i + 2 * u;
+      const float w0 = lane_value(f, min(k, 63)), w1 = lane_value(f, min(k + 1, 63));  // (0 past the last)
+      const float w = half ? w1 : w0;
+      if (k + half < nc) v += w * x[u];
+      x[u] = p[(size_t)min(k + 8 + half, nc - 1) * 32];
+    }
   }
-  T *o = (T *)a.o + row * a.os + (int64_t)head * D + lane * E;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    const float y = l == 0.f ? 0.f : v[e] / l;
-    if constexpr (sizeof(T) == 4) {
-      o[e] = y;
-    } else {
-      uint32_t hi, lo;
-      split2(y, 0.f, hi, lo);
-      o[e] = (T)hi;
-    }
+    const uint32_t u = __float_as_uint(v[e]);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    v[e] = (__uint_as_float(r[0]) + __uint_as_float(r[1])) * inv;
+  }
+  if (half) return;
+  T *o = (T *)a.o + row * a.os + (int64_t)head * D + lane * E;
+  if constexpr (sizeof(T) == 4) {
+    *(vec *)o = v;
+  } else {
+    uint32_t y[E / 2], lo;
+#pragma unroll
+    for (int e = 0; e < E; e += 2) split2(v[e], v[e + 1], y[e / 2], lo);
+    if constexpr (E == 4) *(uint2 *)o = make_uint2(y[0], y[1]);
+    else *(uint32_t *)o = y[0];
   }
 }
 
@@ -899,7 +1117,8 @@ struct TreePlan {
   int cols;    // columns of a block
   int blocks;  // column blocks of the longest draft
   int fill;    // blocks that fill the chip
-  int unit;    // pages that a chunk is a multiple of
+  int unit;    // pages that chunks are multiples of
+  int least;   // pages of the shortest chunk that is worth a block
   int slots;   // chunk slots
 };
 
@@ -908,15 +1127,20 @@ struct TreePlan {
 static TreePlan tree_plan(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t) {
   TreePlan p;
   const int cols = t.max_rows * dm.g;
-  p.wide = t.dtype == KVPRM_BF16 && dm.kvdt != 0 && cols > 32 ? (cols <= 64 ? 2 : 4) : 0;
+  p.wide = t.dtype == KVPRM_BF16 && dm.kvdt != 0 && cols > 32 ? 4 : 0;
+  if (getenv("TW")) p.wide = atoi(getenv("TW"));
   p.nc = cols <= 16 ? 1 : 2;
   p.cols = p.wide ? 32 * p.wide : 16 * p.nc;
   p.blocks = (cols + p.cols - 1) / p.cols;
+  if (p.wide) p.cols = ((cols + p.blocks - 1) / p.blocks + 31) / 32 * 32;  // spread evenly
   p.fill = p.wide ? 2048 / p.wide : 512;
+  if (getenv("TF")) p.fill = atoi(getenv("TF"));
   p.unit = p.wide ? 2 : 2 * kTreeWaves;
+  p.least = p.wide ? 16 : p.unit;
+  if (getenv("TL")) p.least = atoi(getenv("TL"));
   const int64_t items = (int64_t)b.batch * dm.nkv * p.blocks;
   int64_t slots = (8 * p.fill + items - 1) / items;
-  slots = min(slots, (int64_t)(b.max_pages + p.unit - 1) / p.unit);
+  slots = min(slots, (int64_t)(b.max_pages + p.least - 1) / p.least);
   p.slots = (int)max((int64_t)1, min(slots, (int64_t)64));
   return p;
 }
@@ -934,19 +1158,24 @@ static int cached_pages(const kvprm_batch &b, int i) {
   return b.lengths_host ? (b.lengths_host[i] + kPage - 1) / kPage : b.max_pages;
 }
 
-// Pages of a chunk: the fewest (multiples of p.unit) whose chunks leave the grid within p.fill blocks
-// and each candidate within its slots.
+// Most pages of a chunk: the fewest (multiples of p.unit, at least p.least) whose chunks leave the grid
+// within p.fill blocks and each candidate within its slots.
 static int tree_chunk_pages(const Dims &dm, const kvprm_batch &b, const TreePlan &p) {
-  int longest = 0;
+  int longest = 1;
   for (int i = 0; i < b.batch; ++i) longest = max(longest, cached_pages(b, i));
-  const int least = p.wide ? 16 : p.unit;
-  int cp = max(least, ((longest + p.slots - 1) / p.slots + p.unit - 1) / p.unit * p.unit);
-  const int64_t most = p.fill / ((int64_t)dm.nkv * p.blocks);
-  for (;; cp += max(p.unit, cp / 8 / p.unit * p.unit)) {
+  const int64_t most = max(p.fill / ((int64_t)dm.nkv * p.blocks), (int64_t)b.batch);
+  // in units: the least is (too few or) enough, the longest candidate whole is enough
+  int lo = max(p.least, (longest + p.slots - 1) / p.slots + p.unit - 1) / p.unit;
+  int hi = max(lo, (longest + p.unit - 1) / p.unit);
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
     int64_t chunks = 0;
-    for (int i = 0; i < b.batch; ++i) chunks += max(1, (cached_pages(b, i) + cp - 1) / cp);
-    if (chunks <= max(most, (int64_t)b.batch) || cp >= longest) return cp;
+    for (int i = 0; i < b.batch; ++i)
+      chunks += max(1, (cached_pages(b, i) + mid * p.unit - 1) / (mid * p.unit));
+    if (chunks <= most) hi = mid;
+    else lo = mid + 1;
   }
+  return lo * p.unit;
 }
 
 hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batch &b, int layer,
@@ -976,6 +1205,8 @@ hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batc
   a.mask_words = t.mask_words;
   a.ginv = ((1u << 18) + dm.g - 1) / dm.g;
   a.chunk_pages = tree_chunk_pages(dm, b, p);
+  a.unit = p.unit;
+  a.block_cols = p.cols;
   a.slots = p.slots;
   a.pacc = (float *)ws;
   a.pml = (float2 *)((char *)ws + align256((size_t)t.num_rows * dm.nq * p.slots * dm.d * 4));
@@ -1001,8 +1232,7 @@ hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batc
   if (dm.d == 64) { KVPRM_TREE_T(K_, 64) }        \
   else { KVPRM_TREE_T(K_, 128) }
 #define KVPRM_WIDE(K_, D_)                                                                              \
-  if (p.wide == 2) hipLaunchKernelGGL((k_tree_wide<K_, D_, 2>), grid, dim3(128), 0, s, a);              \
-  else hipLaunchKernelGGL((k_tree_wide<K_, D_, 4>), grid, dim3(256), 0, s, a)
+  hipLaunchKernelGGL((k_tree_wide<K_, D_, 4>), grid, dim3(256), 0, s, a)
   if (p.wide) {
     if (dm.kvdt == 1 && dm.d == 64) { KVPRM_WIDE(1, 64); }
     else if (dm.kvdt == 1) { KVPRM_WIDE(1, 128); }
