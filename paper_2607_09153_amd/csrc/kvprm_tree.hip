@@ -2,7 +2,6 @@
 // the drafted keys, by sequence, kv-head and columns) and k_tree_merge (the chunks' join).
 #include <hip/hip_runtime.h>
 #include <math.h>
-#include <stdlib.h>
 
 #include "kvprm_attn_common.h"
 #include "kvprm_internal.h"
@@ -74,14 +73,16 @@ __device__ __forceinline__ TreeSplit tree_split(const TreeArgs &a, int npages) {
 // that they share an L2.
 struct TreeItem {
   int b, j, chunk, colblock;
+  TreeRows rows;
 };
 __device__ __forceinline__ bool tree_item(const TreeArgs &a, int cols_per_block, TreeItem &it) {
   const int lane = threadIdx.x & 63;
   int id = blockIdx.x;
   for (int b0 = 0; b0 < a.B; b0 += 64) {
     int items_l = 0, cb_l = 0;
+    TreeRows r = {0, 0, 0};
     if (b0 + lane < a.B) {
-      const TreeRows r = tree_rows(a, b0 + lane);
+      r = tree_rows(a, b0 + lane);
       if (r.n > 0) {
         items_l = tree_split(a, (r.L + kPage - 1) / kPage).chunks * a.nkv;
         cb_l = (r.n * a.g + cols_per_block - 1) / cols_per_block;
@@ -108,6 +109,9 @@ __device__ __forceinline__ bool tree_item(const TreeArgs &a, int cols_per_block,
       item = full + rem - it.colblock * last;
     }
     it.b = b0 + k;
+    it.rows.L = lane_value(r.L, k);
+    it.rows.n = lane_value(r.n, k);
+    it.rows.r0 = lane_value((int)r.r0, k);
     it.chunk = item / a.nkv;
     it.j = item - it.chunk * a.nkv;
     return true;
@@ -239,7 +243,7 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
   TreeItem it;
   if (!tree_item(a, 16 * NC, it)) return;
   const int b = it.b, j = it.j, c = it.chunk;
-  const TreeRows tr = tree_rows(a, b);
+  const TreeRows tr = it.rows;
   const int L = tr.L, n = tr.n, g = a.g;
   const int cols = n * g, col0 = it.colblock * 16 * NC;
   const int npages = (L + kPage - 1) / kPage;
@@ -600,7 +604,7 @@ __device__ __forceinline__ uint32_t max_mag(uint32_t m, uint32_t x) {  // by hal
 // 8 + 4 h.. of one page are one operand). The drafted keys are stages of their own behind the last
 // chunk's pages, laid out as a page pair.
 template <int KVT, int D, int W>
-__global__ __launch_bounds__(64 * W, 2) void k_tree_wide(TreeArgs a) {
+__global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs a) {
   typedef uint16_t T;
   constexpr int KS = D / 16, NT = D / 32, TC = 2 * D;  // k steps, output tiles, 16-byte groups of a bf16 tile
   constexpr int SC = KVT == 1 ? 2 * TC : TC;           // 16-byte groups of a pair in memory
@@ -615,7 +619,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_tree_wide(TreeArgs a) {
   TreeItem it;
   if (!tree_item(a, a.block_cols, it)) return;
   const int b = it.b, j = it.j, c = it.chunk;
-  const TreeRows tr = tree_rows(a, b);
+  const TreeRows tr = it.rows;
   const int L = tr.L, n = tr.n, g = a.g;
   const int npages = (L + kPage - 1) / kPage;
   const TreeSplit sp = tree_split(a, npages);
@@ -1056,89 +1060,101 @@ __global__ __launch_bounds__(64 * W, 2) void k_tree_wide(TreeArgs a) {
   if (nc > 1 && h == 0) a.pml[at] = make_float2(m + 8.f, l * 0.00390625f);
 }
 
-// Joins the chunks of one (drafted token, q-head), one wave each: weights 2^(m - M) from one load
+// Joins the chunks of drafted tokens' q-heads, N of them to a wave: weights 2^(m - M) from one load
 // per lane (at most 64 chunks), then the chunk sums in order, two chunks at a time (one per half of the
-// wave, 16 or 8 bytes a lane) and four such pairs in flight.
-template <int D, typename T>
+// wave, 16 or 8 bytes a lane) and four such pairs in flight. N = 2 where that keeps the grid in one round
+// (the wave is one chain of memory round trips, whatever it does beside).
+template <int D, int N, typename T>
 __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a) {
   const int b = blockIdx.y, lane = threadIdx.x & 63, half = lane >> 5;
-  const int item = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (threadIdx.x >> 6));
+  const int item = N * __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (threadIdx.x >> 6));
   const TreeRows tr = tree_rows(a, b);
-  const int t = item / a.nq, head = item - t * a.nq;
-  const int nc = tree_split(a, (tr.L + kPage - 1) / kPage).chunks;
-  if (t >= tr.n || nc == 1) return;
-  const int64_t row = tr.r0 + t, at = (row * a.nq + head) * a.slots;
+  const int nc = tree_split(a, (tr.L + kPage - 1) / kPage).chunks, items = tr.n * a.nq;
+  if (item >= items || nc == 1) return;
   constexpr int E = D / 32;
   typedef float vec __attribute__((ext_vector_type(E)));
-  const vec *p = (const vec *)(a.pacc + at * D) + (lane & 31);
-  const float2 ml = lane < nc ? a.pml[at + lane] : make_float2(-INFINITY, 0.f);
-  vec x[4];
+  const vec *p[N];
+  float2 ml[N];
+  vec x[N][4];
 #pragma unroll
-  for (int u = 0; u < 4; ++u) x[u] = p[(size_t)min(2 * u + half, nc - 1) * 32];
-  const float M = wmax(ml.x);
-  const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
-  const float l = wsum(f * ml.y);
-  vec v = {};
-  for (int i = 0; i < nc; i += 8) {
+  for (int z = 0; z < N; ++z) {
+    const int64_t at = (tr.r0 * a.nq + min(item + z, items - 1)) * a.slots;
+    p[z] = (const vec *)(a.pacc + at * D) + (lane & 31);
+    ml[z] = lane < nc ? a.pml[at + lane] : make_float2(-INFINITY, 0.f);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int k = i + 2 * u;
-      const float w0 = lane_value(f, min(k, 63)), w1 = lane_value(f, min(k + 1, 63));  // (0 past the last)
-      const float w = half ? w1 : w0;
-      if (k + half < nc) v += w * x[u];
-      x[u] = p[(size_t)min(k + 8 + half, nc - 1) * 32];
+    for (int u = 0; u < 4; ++u) x[z][u] = p[z][(size_t)min(2 * u + half, nc - 1) * 32];
+  }
+#pragma unroll
+  for (int z = 0; z < N; ++z) {
+    const float M = wmax(ml[z].x);
+    const float f = ml[z].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[z].x - M);
+    const float l = wsum(f * ml[z].y);
+    vec v = {};
+    for (int i = 0; i < nc; i += 8) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int k = i + 2 * u;
+        const float w0 = lane_value(f, min(k, 63)), w1 = lane_value(f, min(k + 1, 63));
+        const float w = half ? w1 : w0;
+        if (k + half < nc) v += w * x[z][u];
+        if (i + 8 < nc) x[z][u] = p[z][(size_t)min(k + 8 + half, nc - 1) * 32];
+      }
     }
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const uint32_t u = __float_as_uint(v[e]);
-    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    v[e] = (__uint_as_float(r[0]) + __uint_as_float(r[1])) * inv;
-  }
-  if (half) return;
-  T *o = (T *)a.o + row * a.os + (int64_t)head * D + lane * E;
-  if constexpr (sizeof(T) == 4) {
-    *(vec *)o = v;
-  } else {
-    uint32_t y[E / 2], lo;
+    for (int e = 0; e < E; ++e) {
+      const uint32_t u = __float_as_uint(v[e]);
+      const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+      v[e] = (__uint_as_float(r[0]) + __uint_as_float(r[1])) * inv;
+    }
+    if (half || item + z >= items) continue;
+    const int t = (item + z) / a.nq, head = item + z - t * a.nq;
+    T *o = (T *)a.o + (tr.r0 + t) * a.os + (int64_t)head * D + lane * E;
+    if constexpr (sizeof(T) == 4) {
+      *(vec *)o = v;
+    } else {
+      uint32_t y[E / 2], lo;
 #pragma unroll
-    for (int e = 0; e < E; e += 2) split2(v[e], v[e + 1], y[e / 2], lo);
-    if constexpr (E == 4) *(uint2 *)o = make_uint2(y[0], y[1]);
-    else *(uint32_t *)o = y[0];
+      for (int e = 0; e < E; e += 2) split2(v[e], v[e + 1], y[e / 2], lo);
+      if constexpr (E == 4) *(uint2 *)o = make_uint2(y[0], y[1]);
+      else *(uint32_t *)o = y[0];
+    }
   }
 }
 
 // ------------------------------------------------------------------------------- launch
 
 struct TreePlan {
-  int wide;    // waves of a k_tree_wide block, 0 = k_tree
+  bool wide;   // k_tree_wide
   int nc;      // column tiles of a k_tree block
   int cols;    // columns of a block
   int blocks;  // column blocks of the longest draft
-  int fill;    // blocks that fill the chip
+  int fill;    // (chunk, kv-head) pairs that fill the chip
   int unit;    // pages that chunks are multiples of
   int least;   // pages of the shortest chunk that is worth a block
   int slots;   // chunk slots
 };
 
-// Kernel by the longest draft's columns. Chunk slots: what fills the chip eight times over if the
-// batch's candidates were all as long as the table.
+constexpr int kWideWaves = 4;
+
+// Kernel by the longest draft's columns. The blocks that are resident at once (fill x column blocks): two
+// of k_tree_wide on a compute unit (three at d_h = 64), two of k_tree. Column blocks are
+// counted by the average draft, num_rows / batch, since a candidate's missing ones are no blocks. Chunk
+// slots: what fills the chip eight times over if the batch's candidates were all as long as the table.
 static TreePlan tree_plan(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t) {
   TreePlan p;
   const int cols = t.max_rows * dm.g;
-  p.wide = t.dtype == KVPRM_BF16 && dm.kvdt != 0 && cols > 32 ? 4 : 0;
-  if (getenv("TW")) p.wide = atoi(getenv("TW"));
+  p.wide = t.dtype == KVPRM_BF16 && dm.kvdt != 0 && cols > 32;
   p.nc = cols <= 16 ? 1 : 2;
-  p.cols = p.wide ? 32 * p.wide : 16 * p.nc;
+  p.cols = p.wide ? 32 * kWideWaves : 16 * p.nc;
   p.blocks = (cols + p.cols - 1) / p.cols;
-  if (p.wide) p.cols = ((cols + p.blocks - 1) / p.blocks + 31) / 32 * 32;  // spread evenly
-  p.fill = p.wide ? 2048 / p.wide : 512;
-  if (getenv("TF")) p.fill = atoi(getenv("TF"));
+  if (p.wide) p.cols = ((cols + p.blocks - 1) / p.blocks + 31) / 32 * 32;  // (spread evenly)
+  // average column blocks of a candidate, in 16ths
+  const int64_t avg = max((int64_t)16, min((int64_t)p.blocks * 16, t.num_rows * dm.g * 16 / b.batch / p.cols + 8));
+  p.fill = (int)max((int64_t)1, (p.wide && dm.d == 64 ? 768 : 512) * 16 / avg);
   p.unit = p.wide ? 2 : 2 * kTreeWaves;
   p.least = p.wide ? 16 : p.unit;
-  if (getenv("TL")) p.least = atoi(getenv("TL"));
-  const int64_t items = (int64_t)b.batch * dm.nkv * p.blocks;
+  const int64_t items = (int64_t)b.batch * dm.nkv;
   int64_t slots = (8 * p.fill + items - 1) / items;
   slots = min(slots, (int64_t)(b.max_pages + p.least - 1) / p.least);
   p.slots = (int)max((int64_t)1, min(slots, (int64_t)64));
@@ -1163,7 +1179,7 @@ static int cached_pages(const kvprm_batch &b, int i) {
 static int tree_chunk_pages(const Dims &dm, const kvprm_batch &b, const TreePlan &p) {
   int longest = 1;
   for (int i = 0; i < b.batch; ++i) longest = max(longest, cached_pages(b, i));
-  const int64_t most = max(p.fill / ((int64_t)dm.nkv * p.blocks), (int64_t)b.batch);
+  const int64_t most = max((int64_t)p.fill / dm.nkv, (int64_t)b.batch);
   // in units: the least is (too few or) enough, the longest candidate whole is enough
   int lo = max(p.least, (longest + p.slots - 1) / p.slots + p.unit - 1) / p.unit;
   int hi = max(lo, (longest + p.unit - 1) / p.unit);
@@ -1232,7 +1248,7 @@ hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batc
   if (dm.d == 64) { KVPRM_TREE_T(K_, 64) }        \
   else { KVPRM_TREE_T(K_, 128) }
 #define KVPRM_WIDE(K_, D_)                                                                              \
-  hipLaunchKernelGGL((k_tree_wide<K_, D_, 4>), grid, dim3(256), 0, s, a)
+  hipLaunchKernelGGL((k_tree_wide<K_, D_, kWideWaves>), grid, dim3(64 * kWideWaves), 0, s, a)
   if (p.wide) {
     if (dm.kvdt == 1 && dm.d == 64) { KVPRM_WIDE(1, 64); }
     else if (dm.kvdt == 1) { KVPRM_WIDE(1, 128); }
@@ -1248,12 +1264,18 @@ hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batc
 #undef KVPRM_TREE
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || chunks == 1) return e;
-  const dim3 mgrid((unsigned)(((int64_t)t.max_rows * dm.nq + 3) / 4), b.batch);
-#define KVPRM_MERGE(D_)                                                                       \
-  if (bf16) hipLaunchKernelGGL((k_tree_merge<D_, uint16_t>), mgrid, dim3(256), 0, s, a);      \
-  else hipLaunchKernelGGL((k_tree_merge<D_, float>), mgrid, dim3(256), 0, s, a)
-  if (dm.d == 64) { KVPRM_MERGE(64); }
-  else { KVPRM_MERGE(128); }
+  // (8192 waves are resident at once)
+  const int n = min((int64_t)b.batch * t.max_rows, t.num_rows) * dm.nq > 8192 ? 2 : 1;
+  const dim3 mgrid((unsigned)(((int64_t)t.max_rows * dm.nq + 4 * n - 1) / (4 * n)), b.batch);
+#define KVPRM_MERGE_T(D_, N_)                                                                     \
+  if (bf16) hipLaunchKernelGGL((k_tree_merge<D_, N_, uint16_t>), mgrid, dim3(256), 0, s, a);      \
+  else hipLaunchKernelGGL((k_tree_merge<D_, N_, float>), mgrid, dim3(256), 0, s, a)
+#define KVPRM_MERGE(D_)                    \
+  if (n == 1) { KVPRM_MERGE_T(D_, 1); }    \
+  else { KVPRM_MERGE_T(D_, 2); }
+  if (dm.d == 64) { KVPRM_MERGE(64) }
+  else { KVPRM_MERGE(128) }
+#undef KVPRM_MERGE_T
 #undef KVPRM_MERGE
   return hipGetLastError();
 }
