@@ -85,9 +85,10 @@ struct Vec<uint16_t, 1> {
 // the rotated ones. The angle's turns are reduced in 64 bits, p * f - round(p * f), since p f reaches
 // 10^5 turns and more; the rest, at most half a turn, is exact enough in 32.
 // V = 16 bytes where widths, strides and addresses allow, else one element.
-// 16 heads of queries and 8 of keys of 128 dims, bf16, 8192 rows (100 MB moved): 22.6 us, 4.45 TB/s, and 18 where the caches
-// hold the rows already (non-temporal loads and stores: 20.7 there). 4093 rows of 36 heads of 64, fp32,
-// adjacent pairs (75 MB): 14 us, 5.4 TB/s. One row for each of 16 sequences: 7.3 us, the launch.
+// 16 heads of queries and 8 of keys of 128 dims, bf16, 8192 rows (100 MB moved): 22.6 us, 4.45 TB/s, and 18
+// where the caches hold the rows already (non-temporal loads and stores: 20.7 there). Two or four units of a
+// thread in flight, loaded before the table is formed: 5 to 8% slower. 4093 rows of 36 heads of 64, fp32,
+// adjacent pairs (75 MB): 14 us, 5.4 TB/s. One row for each of 16 sequences: 7 us, the launch.
 template <typename T, int V, bool HALF>
 __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
   __shared__ float2 cs[kRotaryCs];

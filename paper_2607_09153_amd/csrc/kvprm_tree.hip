@@ -28,6 +28,7 @@ struct TreeArgs {
   int chunk_pages;         // most cached pages of a chunk (a multiple of unit)
   int block_cols;          // columns of a k_tree_wide block, a multiple of 32
   int unit;                // pages that chunks are multiples of: a step of every wave of the block
+  int draft_tokens, draft_pages;  // so many drafted tokens (or a part) take a block as long as so many pages
   int chunks;              // chunks of the grid: a candidate has no more
   int slots;               // chunk slots of a (row, q-head) in the workspace (at least chunks)
   float *pacc;             // [row][q-head][slot][D] chunk sums
@@ -52,16 +53,25 @@ __device__ __forceinline__ TreeRows tree_rows(const TreeArgs &a, int b) {
   return r;
 }
 
-// A candidate's npages cached pages in chunks of equal size (to a unit), as few as have at most
-// chunk_pages each.
+// A candidate's cached pages in chunks of equal size (to a unit), as few as have at most chunk_pages
+// each. The last chunk also takes the drafted tokens and has as many pages fewer as these take time, none
+// if need be; a cache of one chunk keeps them in it.
 struct TreeSplit {
   int chunks, pages;  // pages of each chunk but the last
 };
-__device__ __forceinline__ TreeSplit tree_split(const TreeArgs &a, int npages) {
-  const int most = max(1, min(a.chunks, (npages + a.chunk_pages - 1) / a.chunk_pages));
-  TreeSplit s;
-  s.pages = max(1, (npages + most * a.unit - 1) / (most * a.unit)) * a.unit;
-  s.chunks = max(1, (npages + s.pages - 1) / s.pages);
+__host__ __device__ inline int draft_chunks(int npages, int extra, int pages) {  // chunks of at most `pages`
+  const int cached = (npages + pages - 1) / pages;
+  return cached <= 1 ? 1 : min(cached + 1, (npages + extra + pages - 1) / pages);
+}
+__device__ __forceinline__ TreeSplit tree_split(const TreeArgs &a, const TreeRows &r) {
+  const int npages = (r.L + kPage - 1) / kPage;
+  const int extra = (r.n + a.draft_tokens - 1) / a.draft_tokens * a.draft_pages;
+  const int most = min(a.chunks, draft_chunks(npages, extra, a.chunk_pages));
+  TreeSplit s = {1, npages};
+  if (most > 1) {
+    s.pages = (npages + extra + most * a.unit - 1) / (most * a.unit) * a.unit;
+    s.chunks = draft_chunks(npages, extra, s.pages);
+  }
   return s;
 }
 
@@ -84,7 +94,7 @@ __device__ __forceinline__ bool tree_item(const TreeArgs &a, int cols_per_block,
     if (b0 + lane < a.B) {
       r = tree_rows(a, b0 + lane);
       if (r.n > 0) {
-        items_l = tree_split(a, (r.L + kPage - 1) / kPage).chunks * a.nkv;
+        items_l = tree_split(a, r).chunks * a.nkv;
         cb_l = (r.n * a.g + cols_per_block - 1) / cols_per_block;
       }
     }
@@ -247,9 +257,9 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
   const int L = tr.L, n = tr.n, g = a.g;
   const int cols = n * g, col0 = it.colblock * 16 * NC;
   const int npages = (L + kPage - 1) / kPage;
-  const TreeSplit sp = tree_split(a, npages);
+  const TreeSplit sp = tree_split(a, tr);
   const int nc = sp.chunks;
-  const int p0 = c * sp.pages, np = min(sp.pages, npages - p0);
+  const int p0 = c * sp.pages, np = max(0, min(sp.pages, npages - p0));
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, cn = lane & 15, cq = lane >> 4;
   const float rs = kLog2e / sqrtf((float)D);
@@ -434,11 +444,11 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
   }
 
   // the drafted keys, 16 at a time, in fp32 (T^2 products beside T L: the fp32 matrix instructions
-  // need no split); wave w takes tiles w, w + W, ...
+  // need no split); wave w takes column tile w % NC and every W / NC-th tile of keys
   if (c == nc - 1) {
     const T *kd = (const T *)a.k + tr.r0 * a.ks + (int64_t)j * D;
     const T *vd = (const T *)a.v + tr.r0 * a.vs + (int64_t)j * D;
-    for (int t0 = 16 * w; t0 < n; t0 += 16 * W) {
+    for (int t0 = 16 * (w / NC); t0 < n; t0 += 16 * (W / NC)) {
       float kf[D / 4], vf[NDB][4];
       const T *kr = kd + (int64_t)min(t0 + cn, n - 1) * a.ks;
 #pragma unroll
@@ -464,6 +474,7 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
       }
 #pragma unroll
       for (int ct = 0; ct < NC; ++ct) {
+        if (ct != w % NC) continue;
         float qf[D / 4], p[4];
         query32<D>(qrow(ct), cq, present[ct], qf);
         bool ok[4];
@@ -622,9 +633,9 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
   const TreeRows tr = it.rows;
   const int L = tr.L, n = tr.n, g = a.g;
   const int npages = (L + kPage - 1) / kPage;
-  const TreeSplit sp = tree_split(a, npages);
+  const TreeSplit sp = tree_split(a, tr);
   const int nc = sp.chunks;
-  const int p0 = c * sp.pages, np = min(sp.pages, npages - p0);
+  const int p0 = c * sp.pages, np = max(0, min(sp.pages, npages - p0));
   const int tid = threadIdx.x, lane = tid & 63, cn = lane & 31, h = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int cols = n * g, col0 = it.colblock * a.block_cols + w * 32, col = col0 + cn;
@@ -1069,7 +1080,7 @@ __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a) {
   const int b = blockIdx.y, lane = threadIdx.x & 63, half = lane >> 5;
   const int item = N * __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (threadIdx.x >> 6));
   const TreeRows tr = tree_rows(a, b);
-  const int nc = tree_split(a, (tr.L + kPage - 1) / kPage).chunks, items = tr.n * a.nq;
+  const int nc = tree_split(a, tr).chunks, items = tr.n * a.nq;
   if (item >= items || nc == 1) return;
   constexpr int E = D / 32;
   typedef float vec __attribute__((ext_vector_type(E)));
@@ -1131,11 +1142,14 @@ struct TreePlan {
   int blocks;  // column blocks of the longest draft
   int fill;    // (chunk, kv-head) pairs that fill the chip
   int unit;    // pages that chunks are multiples of
+  int draft_tokens, draft_pages;
   int least;   // pages of the shortest chunk that is worth a block
   int slots;   // chunk slots
 };
 
 constexpr int kWideWaves = 4;
+
+static int draft_extra(const TreePlan &p, int n) { return (n + p.draft_tokens - 1) / p.draft_tokens * p.draft_pages; }
 
 // Kernel by the longest draft's columns. The blocks that are resident at once (fill x column blocks): two
 // of k_tree_wide on a compute unit (three at d_h = 64), two of k_tree. Column blocks are
@@ -1148,15 +1162,19 @@ static TreePlan tree_plan(const Dims &dm, const kvprm_batch &b, const kvprm_tree
   p.nc = cols <= 16 ? 1 : 2;
   p.cols = p.wide ? 32 * kWideWaves : 16 * p.nc;
   p.blocks = (cols + p.cols - 1) / p.cols;
-  if (p.wide) p.cols = ((cols + p.blocks - 1) / p.blocks + 31) / 32 * 32;  // (spread evenly)
+  // spread evenly, unless the average draft needs fewer blocks than the longest
+  if (p.wide && t.num_rows * dm.g > (int64_t)b.batch * (p.blocks - 1) * p.cols)
+    p.cols = ((cols + p.blocks - 1) / p.blocks + 31) / 32 * 32;
   // average column blocks of a candidate, in 16ths
   const int64_t avg = max((int64_t)16, min((int64_t)p.blocks * 16, t.num_rows * dm.g * 16 / b.batch / p.cols + 8));
   p.fill = (int)max((int64_t)1, (p.wide && dm.d == 64 ? 768 : 512) * 16 / avg);
   p.unit = p.wide ? 2 : 2 * kTreeWaves;
   p.least = p.wide ? 16 : p.unit;
+  p.draft_tokens = p.wide ? 32 : 64;
+  p.draft_pages = p.wide ? 4 : p.unit;
   const int64_t items = (int64_t)b.batch * dm.nkv;
   int64_t slots = (8 * p.fill + items - 1) / items;
-  slots = min(slots, (int64_t)(b.max_pages + p.least - 1) / p.least);
+  slots = min(slots, (int64_t)draft_chunks(b.max_pages, draft_extra(p, t.max_rows), p.least));
   p.slots = (int)max((int64_t)1, min(slots, (int64_t)64));
   return p;
 }
@@ -1176,9 +1194,11 @@ static int cached_pages(const kvprm_batch &b, int i) {
 
 // Most pages of a chunk: the fewest (multiples of p.unit, at least p.least) whose chunks leave the grid
 // within p.fill blocks and each candidate within its slots.
-static int tree_chunk_pages(const Dims &dm, const kvprm_batch &b, const TreePlan &p) {
+static int tree_chunk_pages(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t, const TreePlan &p) {
   int longest = 1;
   for (int i = 0; i < b.batch; ++i) longest = max(longest, cached_pages(b, i));
+  longest += draft_extra(p, t.max_rows);
+  const int extra = draft_extra(p, (int)(t.num_rows / b.batch));
   const int64_t most = max((int64_t)p.fill / dm.nkv, (int64_t)b.batch);
   // in units: the least is (too few or) enough, the longest candidate whole is enough
   int lo = max(p.least, (longest + p.slots - 1) / p.slots + p.unit - 1) / p.unit;
@@ -1187,7 +1207,7 @@ static int tree_chunk_pages(const Dims &dm, const kvprm_batch &b, const TreePlan
     const int mid = (lo + hi) / 2;
     int64_t chunks = 0;
     for (int i = 0; i < b.batch; ++i)
-      chunks += max(1, (cached_pages(b, i) + mid * p.unit - 1) / (mid * p.unit));
+      chunks += draft_chunks(cached_pages(b, i), extra, mid * p.unit);
     if (chunks <= most) hi = mid;
     else lo = mid + 1;
   }
@@ -1220,8 +1240,9 @@ hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batc
   a.mask = t.mask;
   a.mask_words = t.mask_words;
   a.ginv = ((1u << 18) + dm.g - 1) / dm.g;
-  a.chunk_pages = tree_chunk_pages(dm, b, p);
+  a.chunk_pages = tree_chunk_pages(dm, b, t, p);
   a.unit = p.unit;
+  a.draft_tokens = p.draft_tokens, a.draft_pages = p.draft_pages;
   a.block_cols = p.cols;
   a.slots = p.slots;
   a.pacc = (float *)ws;
@@ -1229,7 +1250,7 @@ hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batc
   int chunks = 1;
   int64_t items = 0;  // chunks of all candidates
   for (int i = 0; i < b.batch; ++i) {
-    const int nc = max(1, (cached_pages(b, i) + a.chunk_pages - 1) / a.chunk_pages);
+    const int nc = draft_chunks(cached_pages(b, i), draft_extra(p, t.max_rows), a.chunk_pages);
     chunks = max(chunks, nc);
     items += nc;
   }
