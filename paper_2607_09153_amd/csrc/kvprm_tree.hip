@@ -622,6 +622,8 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
   constexpr int NLC = (SC + 64 * W - 1) / (64 * W);    // of these per thread, K or V
   constexpr int SEG = kTreeSegStages;
   constexpr bool HALF = KVT == 2;  // values and weights in fp16
+  // Pairs that half of the waves can move: the first half of them moves keys, the others values.
+  constexpr bool ROLES = 2 * SC <= 64 * W;
   __shared__ uint4 kb[2][2 * TC], vb[2][2 * TC];
   __shared__ int id_s[2 * SEG + 12];                    // page ids of a segment, and their scales
   __shared__ float ksc_s[KVT == 2 ? 2 * SEG + 12 : 1], vsc_s[KVT == 2 ? 2 * SEG + 12 : 1];
@@ -671,7 +673,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
     const int ia = lane_value(id_l, i & 63), ib = lane_value(id_l, (i & 63) + 1);
 #pragma unroll
     for (int k = 0; k < NLC; ++k) {
-      // this wave's first group; pairs of fewer groups than threads are read twice
+      // this wave's first group
       const int i0 = (k * 64 * W + w * 64) % SC;
       const char *t = pool + ((size_t)(i0 >= SC / 2 ? ib : ia) * a.nkv + j) * TILE + (i0 % (SC / 2)) * 16;
       r.g[k] = *(const uint4 *)(t + (uint32_t)(lane * 16));
@@ -732,6 +734,12 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
               make_uint2(fp8x2_to_half2<false>(y[e]), fp8x2_to_half2<true>(y[e]));
       }
     }
+  };
+  const int role = ROLES ? w / (W / 2) : 0;
+  auto load_own = [&](int s, Half &r) { load_half(role ? a.vp : a.kp, s, kid_l, r); };
+  auto store_own = [&](int s, const Half &r) {
+    if (role) store_values(s, r);
+    else store_keys(s, r);
   };
   // 32 drafted tokens from t0 on as a page pair in buffer 0 (in fp16: one exponent for all their values).
   auto store_draft = [&](int t0) {
@@ -975,6 +983,14 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
     // matrix cores form the scores of stage s + 1. In flight beyond that: keys of the next two stages, and
     // values.
     Half k0, k1, v0, v1;
+    if constexpr (ROLES) {
+      load_own(s0, k0);
+      load_own(s0 + 1, k1);
+      store_own(s0, k0);
+      load_own(s0 + 2 - role, k0);
+      store_own(s0 + 1, k1);
+      load_own(s0 + 3 - role, k1);
+    } else {
     load_keys(s0, k0);
     load_values(s0, v0);
     load_keys(s0 + 1, k1);
@@ -985,6 +1001,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
     store_keys(s0 + 1, k1);
     load_values(s0 + 2, v0);
     load_keys(s0 + 3, k1);
+    }
     __syncthreads();
     floatx16 sv;
     if (busy) {
@@ -997,6 +1014,11 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
     auto step = [&](int s, Half &kr, Half &vr) {
       // (key buffer s & 1 is free: its scores were formed a step ago)
       auto stage = [&] {
+        if constexpr (ROLES) {
+          store_own(s + 2 - role, kr);
+          load_own(s + 4 - role, kr);
+          return;
+        }
         store_keys(s + 2, kr);
         store_values(s + 1, vr);
         load_keys(s + 4, kr);
