@@ -625,8 +625,10 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
   // Pairs that half of the waves can move: the first half of them moves keys, the others values.
   constexpr bool ROLES = 2 * SC <= 64 * W;
   __shared__ uint4 kb[2][2 * TC], vb[2][2 * TC];
-  __shared__ int id_s[2 * SEG + 12];                    // page ids of a segment, and their scales
-  __shared__ float ksc_s[KVT == 2 ? 2 * SEG + 12 : 1], vsc_s[KVT == 2 ? 2 * SEG + 12 : 1];
+  __shared__ int id_s[2 * SEG + 12];                    // page ids of a segment
+  __shared__ float ksc_s[KVT == 2 ? 2 * SEG + 12 : 1];  // key scales / sqrt(d), log2 units
+  __shared__ float vsc_s[KVT == 2 ? 2 * SEG + 12 : 1];  // value scales: factor and exponent
+  __shared__ int vex_s[KVT == 2 ? 2 * SEG + 12 : 1];
   __shared__ uint32_t mag_s;  // largest magnitude of the drafted values of a stage
   __shared__ int bad_s;
   TreeItem it;
@@ -886,29 +888,18 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
         for (int t = 0; t < NT; ++t) acc[t] = mfma32(vo[x][t], pl[x], acc[t]);
     }
   };
-  // Scales of stage s's keys and values (s < 0: drafted tokens); a page's value scale as a factor in
-  // [2^-3, 2^3] and a unit, which is kept from page to page while that allows.
+  // Scales of stage s's keys and values (s < 0: drafted tokens).
   struct Scales {
     float ka, kc, va, vc;
     int ua, uc;
   };
-  int last = 0;
   auto scales = [&](int s) {
     Scales r = {rs, rs, 1.f, 1.f, 0, 0};
     if (KVT == 2 && s >= 0) {
       const int i = 2 * (s - s0);
-      r.ka = ksc_s[i] * rs, r.kc = ksc_s[i + 1] * rs;
-      auto one = [&](float v, float &f) {
-        f = ldexpf(v, -last);
-        if (!(f >= 0.125f && f <= 8.f) && v > 0.f && v < INFINITY) {
-          last = (int)(__float_as_uint(v) >> 23) - 127;
-          f = ldexpf(v, -last);
-        }
-        last = __builtin_amdgcn_readfirstlane(last);  // (the same in every lane)
-        return last;
-      };
-      r.ua = one(vsc_s[i], r.va);
-      r.uc = one(vsc_s[i + 1], r.vc);
+      r.ka = ksc_s[i], r.kc = ksc_s[i + 1];
+      r.va = vsc_s[i], r.vc = vsc_s[i + 1];
+      r.ua = __builtin_amdgcn_readfirstlane(vex_s[i]), r.uc = __builtin_amdgcn_readfirstlane(vex_s[i + 1]);
     }
     if (HALF && s < 0) r.ua = r.uc = __builtin_amdgcn_readfirstlane(half_exponent(mag_s));
     return r;
@@ -969,13 +960,25 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
   for (s0 = 0; s0 < ncache; s0 += SEG) {
     se = min(ncache, s0 + SEG);
     if (s0 > 0) __syncthreads();
+    const int id0 = min(max(a.page_table[(size_t)b * a.max_pages + p0 + 2 * s0], 0), a.num_pages - 1);
     // (12 more than the segment's: the loads run five stages past its end)
     for (int i = tid; i < min(2 * (se - s0) + 12, 2 * SEG + 12); i += 64 * W) {
       const int id = min(max(a.page_table[(size_t)b * a.max_pages + p0 + min(2 * s0 + i, np - 1)], 0), a.num_pages - 1);
       id_s[i] = id;
       if (KVT == 2) {
-        ksc_s[i] = a.ksc[(size_t)id * a.nkv + j];
-        vsc_s[i] = a.vsc[(size_t)id * a.nkv + j];
+        ksc_s[i] = a.ksc[(size_t)id * a.nkv + j] * rs;
+        // A value scale is a factor on the page's weights and a power of two, the segment's first page's
+        // where that leaves a factor in [2^-3, 2^3], since acc moves whenever it changes.
+        const float v = a.vsc[(size_t)id * a.nkv + j], v0 = a.vsc[(size_t)id0 * a.nkv + j];
+        auto exponent = [](float x) { return x > 0.f && x < INFINITY ? (int)(__float_as_uint(x) >> 23) - 127 : 0; };
+        int e = exponent(v0);
+        float f = ldexpf(v, -e);
+        if (!(f >= 0.125f && f <= 8.f) && v > 0.f && v < INFINITY) {
+          e = exponent(v);
+          f = ldexpf(v, -e);
+        }
+        vsc_s[i] = f;
+        vex_s[i] = e;
       }
     }
     __syncthreads();
