@@ -1,5 +1,6 @@
-// Attention of drafted tokens over the paged cache for gfx950: k_tree (chunks of cached pages and
-// the drafted keys, by sequence, kv-head and columns) and k_tree_merge (the chunks' join).
+// Attention of drafted tokens over the paged cache for gfx950: k_tree and k_tree_wide (chunks of cached pages
+// and the drafted keys, by sequence, kv-head and columns; few columns and many) and k_tree_merge (the chunks'
+// join).
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -37,7 +38,7 @@ struct TreeArgs {
 
 constexpr int kTreeWaves = 4;
 constexpr int kTreeSegStages = 128;  // page pairs whose ids (and scales) a k_tree_wide block holds at a time
-constexpr int kTreeSeg = 64 * kTreeWaves;  // pages whose ids a block's lanes hold at a time
+constexpr int kTreeSeg = 64 * kTreeWaves;  // pages whose ids a k_tree block's lanes hold at a time
 
 // The rows of one candidate, kept inside the arrays whatever `start` holds.
 struct TreeRows {
@@ -242,7 +243,10 @@ struct Terms<float> {
 // A block's four waves take page pairs in turn and join their softmax states in LDS, so that a chunk is
 // one partial result.
 // A page pair (32 tokens) is one step: S = K Q^T, a running softmax in registers, O^T += V^T P^T, all
-// on the matrix cores with the cache's tiles as they lie in memory (see kvprm_attn.hip).
+// on the matrix cores with the cache's tiles as they lie in memory (see kvprm_attn.hip), the next pair's loads
+// in flight. Bound by memory on long caches: 8 of 16384 to 32768 tokens, 4 kv-heads of 128 dims, bf16, 28
+// columns (410 MB): 90 us, 4.5 TB/s. On short ones by the chain of loads, products and join: 1103 tokens,
+// 16 drafted, 8 kv-heads: 11 us, and 4 for k_tree_merge.
 template <int KVT, int D, int NC, typename T>
 __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
   constexpr int NKB = D / 32, NDB = D / 16, W = kTreeWaves;
@@ -594,7 +598,7 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
 // Exponent that bf16 values of the largest magnitude `mag` (bits) are divided by on their way to fp16:
 // it comes to lie in [2^14, 2^15). Values down to 2^-28 of it keep all their bits, smaller ones become 0.
 __device__ __forceinline__ int half_exponent(uint32_t mag) {
-  return mag == 0 ? 0 : max((int)(mag >> 7) - 141, -112);
+  return max((int)(mag >> 7) - 141, -112);
 }
 // Two bf16 values divided by 2^(bias / 128 - 112) as fp16; `bias` in both halves.
 __device__ __forceinline__ uint32_t bf16x2_to_half2(uint32_t x, uint32_t bias) {
@@ -608,12 +612,19 @@ __device__ __forceinline__ uint32_t max_mag(uint32_t m, uint32_t x) {  // by hal
 }
 
 // The same for drafts of many columns (bf16 rows): here the waves share the pages and split the
-// columns, 32 each. A stage is a page pair (32 tokens) in LDS as bf16 tiles in the stored order (fp8
-// tiles are widened on their way, exactly), double buffered, the next pair's loads in flight while one is
-// computed. 32x32x16 products: S = K Q^T (a lane holds tokens 8 i + 4 h + e, h = lane / 32, of
-// column lane % 32), softmax, O^T += V^T P^T with P in two bf16 terms, tokens in S's order (8 slots 4 h..,
-// 8 + 4 h.. of one page are one operand). The drafted keys are stages of their own behind the last
-// chunk's pages, laid out as a page pair.
+// columns, 32 each. A stage is a page pair (32 tokens) in LDS as 16-bit tiles in the stored order, double
+// buffered, the next pairs' loads in flight while one is computed. 32x32x16 products: S = K Q^T (a lane holds
+// tokens 8 i + 4 h + e, h = lane / 32, of column lane % 32), softmax, O^T += V^T P^T, tokens in S's order
+// (8 slots 4 h.., 8 + 4 h.. of one page are one operand). bf16 caches: P in two bf16 terms (16 bits; one
+// term would add an error the size of the result's own rounding). fp8 caches: keys widened to bf16, values to
+// fp16, exactly, and P in fp16 (11 bits), half the products: 8 caches of 16384 to 32768 tokens, 4 kv-heads of
+// 128 dims, 64 drafted tokens of 7 query heads each: 264 us, 700 TFLOP/s, and 285 in two bf16 terms before
+// later steps; from bf16 caches 330 us, 560 TFLOP/s (fp16 values from those too, with an exponent per tile: 357
+// and more).
+// Bound by vector instructions (about 115 a stage and wave at D = 128, bf16, 160 at D = 64, fp8, beside 24 and 8
+// products) and by how far the two or three waves of a SIMD overlap them with products: a ring of four stages
+// with half the barriers, wave priorities and waves in two groups taking turns all measured the same.
+// The drafted keys are stages of their own behind the last chunk's pages, laid out as a page pair.
 template <int KVT, int D, int W>
 __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs a) {
   typedef uint16_t T;
@@ -630,6 +641,10 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
   __shared__ float vsc_s[KVT == 2 ? 2 * SEG + 12 : 1];  // value scales: factor and exponent
   __shared__ int vex_s[KVT == 2 ? 2 * SEG + 12 : 1];
   __shared__ uint32_t mag_s;  // largest magnitude of the drafted values of a stage
+  // Largest unit so far. Others stay within 2^-kUnits of it: acc moves to each, and would overflow in one
+  // far below. (What a unit kept higher loses is below 2^-(kUnits + 20) of the largest values.)
+  constexpr int kUnits = 24, kNoUnit = -1000;
+  __shared__ int base_s;
   __shared__ int bad_s;
   TreeItem it;
   if (!tree_item(a, a.block_cols, it)) return;
@@ -743,6 +758,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
     if (role) store_values(s, r);
     else store_keys(s, r);
   };
+  auto draft_unit = [&] { return max(half_exponent(mag_s), base_s - kUnits); };
   // 32 drafted tokens from t0 on as a page pair in buffer 0 (in fp16: one exponent for all their values).
   auto store_draft = [&](int t0) {
     constexpr int ND = (2 * TC + 64 * W - 1) / (64 * W);
@@ -776,7 +792,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
       mag = lanes_max(max(mag & 0xFFFFu, mag >> 16));
       if (lane == 0) atomicMax(&mag_s, mag);
       __syncthreads();
-      bias = (uint32_t)(112 + half_exponent(mag_s)) * 0x00800080u;
+      bias = (uint32_t)(112 + draft_unit()) * 0x00800080u;
     }
 #pragma unroll
     for (int k = 0; k < ND; ++k) {
@@ -901,7 +917,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
       r.va = vsc_s[i], r.vc = vsc_s[i + 1];
       r.ua = __builtin_amdgcn_readfirstlane(vex_s[i]), r.uc = __builtin_amdgcn_readfirstlane(vex_s[i + 1]);
     }
-    if (HALF && s < 0) r.ua = r.uc = __builtin_amdgcn_readfirstlane(half_exponent(mag_s));
+    if (HALF && s < 0) r.ua = r.uc = __builtin_amdgcn_readfirstlane(draft_unit());
     return r;
   };
   // A pair of which only the tokens of `ok` (bit r: this lane's r-th) count: the candidate's last cached
@@ -957,27 +973,31 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
     for (int e = 0; e < 16; ++e) ok |= (bits >> (8 * (e >> 2) + 4 * h + (e & 3)) & 1u) << e;
     return ok;
   };
+  if (tid == 0) base_s = kNoUnit, mag_s = 0;
   for (s0 = 0; s0 < ncache; s0 += SEG) {
     se = min(ncache, s0 + SEG);
-    if (s0 > 0) __syncthreads();
-    const int id0 = min(max(a.page_table[(size_t)b * a.max_pages + p0 + 2 * s0], 0), a.num_pages - 1);
+    __syncthreads();
     // (12 more than the segment's: the loads run five stages past its end)
     for (int i = tid; i < min(2 * (se - s0) + 12, 2 * SEG + 12); i += 64 * W) {
       const int id = min(max(a.page_table[(size_t)b * a.max_pages + p0 + min(2 * s0 + i, np - 1)], 0), a.num_pages - 1);
       id_s[i] = id;
       if (KVT == 2) {
         ksc_s[i] = a.ksc[(size_t)id * a.nkv + j] * rs;
-        // A value scale is a factor on the page's weights and a power of two, the segment's first page's
-        // where that leaves a factor in [2^-3, 2^3], since acc moves whenever it changes.
-        const float v = a.vsc[(size_t)id * a.nkv + j], v0 = a.vsc[(size_t)id0 * a.nkv + j];
-        auto exponent = [](float x) { return x > 0.f && x < INFINITY ? (int)(__float_as_uint(x) >> 23) - 127 : 0; };
-        int e = exponent(v0);
-        float f = ldexpf(v, -e);
-        if (!(f >= 0.125f && f <= 8.f) && v > 0.f && v < INFINITY) {
-          e = exponent(v);
-          f = ldexpf(v, -e);
-        }
-        vsc_s[i] = f;
+        const float v = a.vsc[(size_t)id * a.nkv + j];
+        vsc_s[i] = v;
+        if (v > 0.f && v < INFINITY) atomicMax(&base_s, (int)(__float_as_uint(v) >> 23) - 127);
+      }
+    }
+    if (KVT == 2) {
+      // A value scale is a factor on the page's weights and a power of two, the largest unit where that leaves
+      // a factor in [2^-3, 2), since acc moves whenever the unit changes.
+      __syncthreads();
+      const int base = base_s;
+      for (int i = tid; i < min(2 * (se - s0) + 12, 2 * SEG + 12); i += 64 * W) {
+        const float v = vsc_s[i];
+        int e = v > 0.f && v < INFINITY ? (int)(__float_as_uint(v) >> 23) - 127 : kNoUnit;
+        e = e < base - 3 && e != kNoUnit ? max(e, base - kUnits) : max(base, -126);
+        vsc_s[i] = ldexpf(v, -e);
         vex_s[i] = e;
       }
     }
@@ -994,16 +1014,16 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
       store_own(s0 + 1, k1);
       load_own(s0 + 3 - role, k1);
     } else {
-    load_keys(s0, k0);
-    load_values(s0, v0);
-    load_keys(s0 + 1, k1);
-    load_values(s0 + 1, v1);
-    store_keys(s0, k0);
-    store_values(s0, v0);
-    load_keys(s0 + 2, k0);
-    store_keys(s0 + 1, k1);
-    load_values(s0 + 2, v0);
-    load_keys(s0 + 3, k1);
+      load_keys(s0, k0);
+      load_values(s0, v0);
+      load_keys(s0 + 1, k1);
+      load_values(s0 + 1, v1);
+      store_keys(s0, k0);
+      store_values(s0, v0);
+      load_keys(s0 + 2, k0);
+      store_keys(s0 + 1, k1);
+      load_values(s0 + 2, v0);
+      load_keys(s0 + 3, k1);
     }
     __syncthreads();
     floatx16 sv;
@@ -1060,7 +1080,10 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
   if (c == nc - 1) {
     for (int t0 = 0; t0 < n; t0 += 32) {
       __syncthreads();
-      if (tid == 0) bad_s = 0, mag_s = 0;
+      if (tid == 0) {
+        if (t0 > 0) base_s = draft_unit() > base_s ? draft_unit() : base_s;
+        bad_s = 0, mag_s = 0;
+      }
       __syncthreads();
       store_draft(t0);
       __syncthreads();
@@ -1099,7 +1122,8 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
 // Joins the chunks of drafted tokens' q-heads, N of them to a wave: weights 2^(m - M) from one load
 // per lane (at most 64 chunks), then the chunk sums in order, two chunks at a time (one per half of the
 // wave, 16 or 8 bytes a lane) and four such pairs in flight. N = 2 where that keeps the grid in one round
-// (the wave is one chain of memory round trips, whatever it does beside).
+// (the wave is one chain of memory round trips, whatever it does beside): 14336 q-heads of 16 chunks of 128
+// dims, 118 MB read, in 8.4 us; 512 of 10 chunks in 3.2.
 template <int D, int N, typename T>
 __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a) {
   const int b = blockIdx.y, lane = threadIdx.x & 63, half = lane >> 5;
@@ -1176,10 +1200,19 @@ constexpr int kWideWaves = 4;
 
 static int draft_extra(const TreePlan &p, int n) { return (n + p.draft_tokens - 1) / p.draft_tokens * p.draft_pages; }
 
-// Kernel by the longest draft's columns. The blocks that are resident at once (fill x column blocks): two
-// of k_tree_wide on a compute unit (three at d_h = 64), two of k_tree. Column blocks are
-// counted by the average draft, num_rows / batch, since a candidate's missing ones are no blocks. Chunk
-// slots: what fills the chip eight times over if the batch's candidates were all as long as the table.
+// Kernel by the longest draft's columns: k_tree up to 32, which a wave holds at once. At 17 to 32 columns it took
+// 13.7 us where k_tree_wide took 16.5 (1103 tokens, 32 columns), 25.7 and 29.6 (24 fp8 caches of 4800, 32
+// columns), 91 and 88 (8 caches of 16384 to 32768, 28 columns); at 33 to 64, where it reads the pages twice, 42.9
+// and 33.9 (the 24 caches, 48 columns), 108 and 96 (the 8, 56 columns).
+// Chunks leave as many blocks as are resident at once: two of k_tree_wide on a compute unit (three at
+// d_h = 64), two of k_tree. Fewer or more both lose (k_tree_wide, 24 ragged fp8 caches, d_h = 64: 56 us at 680
+// blocks, 54 at 768, 61 at 1024; 8 long bf16 caches, d_h = 128: 403 us at 400, 330 at 512, 394 at 600). Column
+// blocks are counted by the average draft, num_rows / batch, since a candidate's missing ones are no
+// blocks. A k_tree_wide chunk has 16 pages or more: 1200 tokens of 24 candidates take 24 us with least chunks
+// of 8 or 16, 28 with 32. Drafted tokens count as pages of the last chunk (4 for 32 tokens of
+// k_tree_wide, 8 for 64 of k_tree): 13.6 us instead of 15.6 for 1103 tokens, 338 instead of 344 on the long
+// caches; 2 to 16 pages differ by less than 2%. Chunk slots: what fills the chip eight times over if the
+// batch's candidates were all as long as the table.
 static TreePlan tree_plan(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t) {
   TreePlan p;
   const int cols = t.max_rows * dm.g;
@@ -1187,7 +1220,8 @@ static TreePlan tree_plan(const Dims &dm, const kvprm_batch &b, const kvprm_tree
   p.nc = cols <= 16 ? 1 : 2;
   p.cols = p.wide ? 32 * kWideWaves : 16 * p.nc;
   p.blocks = (cols + p.cols - 1) / p.cols;
-  // spread evenly, unless the average draft needs fewer blocks than the longest
+  // Spread evenly, unless the average draft needs fewer blocks than the longest: 24 drafts of 1 to 48 tokens of
+  // 4 query heads took 55 us in blocks of 128 columns and 68 in blocks of 96.
   if (p.wide && t.num_rows * dm.g > (int64_t)b.batch * (p.blocks - 1) * p.cols)
     p.cols = ((cols + p.blocks - 1) / p.blocks + 31) / 32 * 32;
   // average column blocks of a candidate, in 16ths
