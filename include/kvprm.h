@@ -464,7 +464,8 @@ kvprm_status kvprm_workspace_size_tree(kvprm_handle h, const kvprm_batch *batch,
  * does not attend to never reach its output, whatever they hold (infinities, NaN). Scores, the softmax and the
  * sums are fp32; F32 rows keep 24 bits of q and of the probabilities, BF16 rows 16 bits of the
  * probabilities (11 over fp8 caches where max_rows times the q-heads of a kv-head exceeds 32). fp8 scales must
- * not be negative. The cache is not written. Rows that no candidate owns are left as they are.
+ * not be negative. The cache is not written. o must not overlap q, k or v.
+ * Rows that no candidate owns are left as they are.
  * Conventions as for kvprm_attention; the prefix-sharing hint is not read. */
 kvprm_status kvprm_attention_tree(kvprm_handle h, const kvprm_kv_cache *cache,
                                   const kvprm_batch *batch, int32_t layer, const kvprm_tree *tree,

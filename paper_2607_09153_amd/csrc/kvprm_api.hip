@@ -7,6 +7,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <exception>
 #include <mutex>
 #include <new>
 #include <string>
@@ -927,30 +928,34 @@ static kvprm_status check_kv_rows(const kvprm_handle h, const kvprm_kv_cache *ca
 static kvprm_status check_written_debug(const kvprm_handle h, const kvprm_kv_cache *c, const kvprm_batch *b,
                                         const kvprm_kv_rows *r, hipStream_t s, const char *fn) {
   if (!h->debug) return KVPRM_OK;
-  std::vector<int32_t> len(b->batch), start(b->batch + 1), pt((size_t)b->batch * b->max_pages);
-  if (hipMemcpyAsync(len.data(), b->lengths, len.size() * 4, hipMemcpyDeviceToHost, s) != hipSuccess ||
-      hipMemcpyAsync(start.data(), r->start, start.size() * 4, hipMemcpyDeviceToHost, s) != hipSuccess ||
-      hipMemcpyAsync(pt.data(), b->page_table, pt.size() * 4, hipMemcpyDeviceToHost, s) != hipSuccess ||
-      hipStreamSynchronize(s) != hipSuccess)
-    return fail(KVPRM_E_HIP, "%s: debug copy of the page table failed", fn);
-  const int cap = b->max_pages * kPage;
-  std::vector<int32_t> owner((size_t)c->num_pages, -1);
-  for (int i = 0; i < b->batch; ++i) {
-    const int64_t n = (int64_t)start[i + 1] - start[i];
-    if (start[i] < 0 || n < 0 || n > r->max_rows)
-      return fail(KVPRM_E_INVALID, "%s: start[%d..%d] = %d, %d", fn, i, i + 1, start[i], start[i + 1]);
-    if (len[i] < 0 || len[i] + n > cap)
-      return fail(KVPRM_E_INVALID, "%s: candidate %d: %d tokens and %lld rows exceed %d", fn, i, len[i],
-                  (long long)n, cap);
-    for (int k = len[i] / kPage; n > 0 && k * kPage < len[i] + n; ++k) {
-      const int32_t id = pt[(size_t)i * b->max_pages + k];
-      if (id < 0 || id >= c->num_pages)
-        return fail(KVPRM_E_INVALID, "%s: page_table[%d][%d] = %d outside [0, %d)", fn, i, k, id,
-                    c->num_pages);
-      if (owner[id] >= 0)
-        return fail(KVPRM_E_INVALID, "%s: page %d gets rows of candidates %d and %d", fn, id, owner[id], i);
-      owner[id] = i;
+  try {
+    std::vector<int32_t> len(b->batch), start(b->batch + 1), pt((size_t)b->batch * b->max_pages);
+    if (hipMemcpyAsync(len.data(), b->lengths, len.size() * 4, hipMemcpyDeviceToHost, s) != hipSuccess ||
+        hipMemcpyAsync(start.data(), r->start, start.size() * 4, hipMemcpyDeviceToHost, s) != hipSuccess ||
+        hipMemcpyAsync(pt.data(), b->page_table, pt.size() * 4, hipMemcpyDeviceToHost, s) != hipSuccess ||
+        hipStreamSynchronize(s) != hipSuccess)
+      return fail(KVPRM_E_HIP, "%s: debug copy of the page table failed", fn);
+    const int cap = b->max_pages * kPage;
+    std::vector<int32_t> owner((size_t)c->num_pages, -1);
+    for (int i = 0; i < b->batch; ++i) {
+      const int64_t n = (int64_t)start[i + 1] - start[i];
+      if (start[i] < 0 || n < 0 || n > r->max_rows)
+        return fail(KVPRM_E_INVALID, "%s: start[%d..%d] = %d, %d", fn, i, i + 1, start[i], start[i + 1]);
+      if (len[i] < 0 || len[i] + n > cap)
+        return fail(KVPRM_E_INVALID, "%s: candidate %d: %d tokens and %lld rows exceed %d", fn, i, len[i],
+                    (long long)n, cap);
+      for (int k = len[i] / kPage; n > 0 && k * kPage < len[i] + n; ++k) {
+        const int32_t id = pt[(size_t)i * b->max_pages + k];
+        if (id < 0 || id >= c->num_pages)
+          return fail(KVPRM_E_INVALID, "%s: page_table[%d][%d] = %d outside [0, %d)", fn, i, k, id,
+                      c->num_pages);
+        if (owner[id] >= 0)
+          return fail(KVPRM_E_INVALID, "%s: page %d gets rows of candidates %d and %d", fn, id, owner[id], i);
+        owner[id] = i;
+      }
     }
+  } catch (const std::exception &e) {  // (no memory for the copies)
+    return fail(KVPRM_E_INVALID, "%s: debug check: %s", fn, e.what());
   }
   return KVPRM_OK;
 }

@@ -186,8 +186,6 @@ hipError_t launch_rotary(const kvprm_rope &rp, const double *turn, bool bf16, in
   a.units = a.nrot + (a.d - rp.rotary_dim) / V;
   a.uinv = (uint32_t)(((1ull << 32) + a.units - 1) / a.units);
   a.hinv = (uint32_t)(((1ull << 32) + a.heads - 1) / a.heads);
-  a.rows = rows;
-  a.pos = pos;
   a.mag = (float)rp.magnitude;
   a.smag = transpose ? -a.mag : a.mag;
   for (int i = 0; i < a.half; ++i) a.turn[i] = turn[i];
@@ -198,16 +196,26 @@ hipError_t launch_rotary(const kvprm_rope &rp, const double *turn, bool bf16, in
   while (rpb < 16 && rpb * 2 * a.half <= kRotaryCs && rows > rpb * 1024 && rpb * per_row < 1024)
     rpb *= 2;
   a.rpb = (int)rpb;
-  const dim3 grid((unsigned)((rows + rpb - 1) / rpb));
+  const int64_t most = rpb << 23;  // rows of a launch: 2^31 threads
+  for (int64_t r0 = 0; r0 < rows; r0 += most) {
+    a.rows = min(most, rows - r0);
+    a.pos = pos + r0;
+    for (int i = 0; i < 2; ++i) {
+      const kvprm_rope_heads &q = parts[i < num_parts ? i : 0];
+      a.p[i].src = (const char *)q.src + r0 * q.src_stride * eb;
+      a.p[i].dst = (char *)q.dst + r0 * q.dst_stride * eb;
+    }
+    const dim3 grid((unsigned)((a.rows + rpb - 1) / rpb));
 #define KVPRM_ROT(T_, V_)                                                             \
   if (half) hipLaunchKernelGGL((k_rotary<T_, V_, true>), grid, dim3(256), 0, s, a);   \
   else hipLaunchKernelGGL((k_rotary<T_, V_, false>), grid, dim3(256), 0, s, a)
-  if (bf16) {
-    if (wide) { KVPRM_ROT(uint16_t, 8); }
-    else { KVPRM_ROT(uint16_t, 1); }
-  } else {
-    if (wide) { KVPRM_ROT(float, 4); }
-    else { KVPRM_ROT(float, 1); }
+    if (bf16) {
+      if (wide) { KVPRM_ROT(uint16_t, 8); }
+      else { KVPRM_ROT(uint16_t, 1); }
+    } else {
+      if (wide) { KVPRM_ROT(float, 4); }
+      else { KVPRM_ROT(float, 1); }
+    }
   }
 #undef KVPRM_ROT
   return hipGetLastError();

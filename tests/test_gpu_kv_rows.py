@@ -288,3 +288,37 @@ def test_write_then_read(cdt):
             x = rows[part][sum(counts[:b]):sum(counts[:b + 1])].double().numpy()
             # (below e4m3's normal range, 2^-6 of the scale, half a step is 2^-10 of it)
             assert np.all(np.abs(v - x) <= half * np.abs(x) + (0 if cdt != "fp8" else 2.0 ** -10 * c.scale[part].max()))
+
+
+def test_write_debug_refusals(monkeypatch):
+    """KVPRM_DEBUG=1: what would be dropped, and a page that would get rows twice, is refused on the host;
+    nothing is written. A good call passes."""
+    _say("debug")
+    monkeypatch.setenv("KVPRM_DEBUG", "1")
+    counts = [6, 20]
+
+    def call(table=None, lengths=None, start=None):
+        c = Cache("fp8", 64, [10, 20], counts, seed=8)
+        if table is not None:
+            c.table[table[0], table[1]] = table[2] if len(table) == 3 else c.table[table[3], table[4]]
+            c.upload()
+        if lengths is not None:
+            c.dlen.copy_(torch.tensor(lengths, dtype=torch.int32))
+        before = [t.clone() for t in c.pool + c.sc]
+        rows = [t.cuda() for t in _rows(26, 64, "bf16", 9)]
+        ds = torch.tensor([0, 6, 26] if start is None else start, dtype=torch.int32).cuda()
+        r = c.m.make_kv_rows(rows[0].data_ptr(), rows[1].data_ptr(), "bf16", NKV * 64, NKV * 64, 26, ds.data_ptr(), 20)
+        refused = None
+        try:
+            c.m.kvprm_write_kv(c.h, c.cache, c.batch, LAYER, r, torch.cuda.current_stream().cuda_stream)
+        except RuntimeError as e:
+            refused = str(e)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(before, c.pool + c.sc)) == (refused is not None)
+        return refused
+
+    assert call() is None
+    for bad in (dict(table=(0, 0, -1)), dict(table=(1, 2, 1 << 20)), dict(table=(1, 1, None, 0, 0)),
+                dict(table=(1, 2, None, 1, 1)), dict(lengths=[10, 60]), dict(lengths=[-1, 20]), dict(start=[0, 6, 27]),
+                dict(start=[-1, 6, 26]), dict(start=[0, 6, 5])):
+        assert "kvprm_write_kv" in call(**bad)
