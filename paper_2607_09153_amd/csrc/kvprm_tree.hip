@@ -1200,7 +1200,8 @@ constexpr int kWideWaves = 4;
 
 static int draft_extra(const TreePlan &p, int n) { return (n + p.draft_tokens - 1) / p.draft_tokens * p.draft_pages; }
 
-// Kernel by the longest draft's columns: k_tree up to 32, which a wave holds at once. At 17 to 32 columns it took
+// Kernel by the longest draft's columns where the chip is full (launch_tree has the rule for fewer blocks): k_tree up
+// to 32, which a wave holds at once. At 17 to 32 columns it took
 // 13.7 us where k_tree_wide took 16.5 (1103 tokens, 32 columns), 25.7 and 29.6 (24 fp8 caches of 4800, 32
 // columns), 91 and 88 (8 caches of 16384 to 32768, 28 columns); at 33 to 64, where it reads the pages twice, 42.9
 // and 33.9 (the 24 caches, 48 columns), 108 and 96 (the 8, 56 columns).
@@ -1213,10 +1214,10 @@ static int draft_extra(const TreePlan &p, int n) { return (n + p.draft_tokens - 
 // k_tree_wide, 8 for 64 of k_tree): 13.6 us instead of 15.6 for 1103 tokens, 338 instead of 344 on the long
 // caches; 2 to 16 pages differ by less than 2%. Chunk slots: what fills the chip eight times over if the
 // batch's candidates were all as long as the table.
-static TreePlan tree_plan(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t) {
+static TreePlan tree_plan(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t, bool wide) {
   TreePlan p;
   const int cols = t.max_rows * dm.g;
-  p.wide = t.dtype == KVPRM_BF16 && dm.kvdt != 0 && cols > 32;
+  p.wide = wide;
   p.nc = cols <= 16 ? 1 : 2;
   p.cols = p.wide ? 32 * kWideWaves : 16 * p.nc;
   p.blocks = (cols + p.cols - 1) / p.cols;
@@ -1227,7 +1228,7 @@ static TreePlan tree_plan(const Dims &dm, const kvprm_batch &b, const kvprm_tree
   // average column blocks of a candidate, in 16ths
   const int64_t avg = max((int64_t)16, min((int64_t)p.blocks * 16, t.num_rows * dm.g * 16 / b.batch / p.cols + 8));
   p.fill = (int)max((int64_t)1, (p.wide && dm.d == 64 ? 768 : 512) * 16 / avg);
-  p.unit = p.wide ? 2 : 2 * kTreeWaves;
+  p.unit = p.wide ? 2 : dm.kvdt == 0 ? kTreeWaves : 2 * kTreeWaves;
   p.least = p.wide ? 16 : p.unit;
   p.draft_tokens = p.wide ? 32 : 64;
   p.draft_pages = p.wide ? 4 : p.unit;
@@ -1240,10 +1241,15 @@ static TreePlan tree_plan(const Dims &dm, const kvprm_batch &b, const kvprm_tree
 
 static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
+static bool may_be_wide(const Dims &dm, const kvprm_tree &t) {
+  return t.dtype == KVPRM_BF16 && dm.kvdt != 0 && t.max_rows * dm.g > 32;
+}
+
 size_t tree_ws_bytes(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t) {
-  const TreePlan p = tree_plan(dm, b, t);
-  if (p.slots == 1) return 256;
-  const size_t parts = (size_t)t.num_rows * dm.nq * p.slots;
+  int slots = tree_plan(dm, b, t, false).slots;
+  if (may_be_wide(dm, t)) slots = max(slots, tree_plan(dm, b, t, true).slots);
+  if (slots == 1) return 256;
+  const size_t parts = (size_t)t.num_rows * dm.nq * slots;
   return align256(parts * dm.d * 4) + align256(parts * 8);
 }
 
@@ -1275,7 +1281,25 @@ static int tree_chunk_pages(const Dims &dm, const kvprm_batch &b, const kvprm_tr
 
 hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batch &b, int layer,
                        const kvprm_tree &t, void *ws, hipStream_t s) {
-  const TreePlan p = tree_plan(dm, b, t);
+  TreePlan p = tree_plan(dm, b, t, false);
+  int chunk_pages = tree_chunk_pages(dm, b, t, p);
+  auto chunks_of = [&](int i) { return draft_chunks(cached_pages(b, i), draft_extra(p, t.max_rows), chunk_pages); };
+  int64_t items = 0;  // chunks of all candidates
+  for (int i = 0; i < b.batch; ++i) items += chunks_of(i);
+  // Blocks of 16 columns (short chains, pages read once per block from the caches) while they leave the chip's
+  // waves unfilled. Instead of 32 columns, up to 768 blocks: 1103 tokens, 32 columns (160 blocks) 14.0 -> 12.2 us,
+  // 2 x 2500 (672 blocks) 24.8 -> 21.3, but 16 x 4000 (1024 blocks) 67.7 -> 73.4. Instead of k_tree_wide, up to
+  // 512: 1103 tokens, 64 columns (320 blocks) 17.7 -> 14.7, 300 tokens, 128 columns (256) 19.1 -> 13.0, 4 x 700
+  // fp8 tokens, 64 columns 16.4 -> 10.9, but 2500 tokens, 64 columns (over 512) 18.7 -> 21.0.
+  const int64_t blocks16 = items * dm.nkv * ((t.max_rows * dm.g + 15) / 16);
+  if (may_be_wide(dm, t) && blocks16 > 512) {
+    p = tree_plan(dm, b, t, true);
+    chunk_pages = tree_chunk_pages(dm, b, t, p);
+  } else if (blocks16 <= 768) {
+    p.nc = 1;
+    p.cols = 16;
+    p.blocks = (t.max_rows * dm.g + 15) / 16;
+  }
   const size_t tiles = (size_t)c.num_pages * dm.nkv;
   const size_t bytes = tiles * kPage * dm.d * (dm.kvdt == 0 ? 4 : dm.kvdt == 1 ? 2 : 1);
   TreeArgs a;
@@ -1299,7 +1323,7 @@ hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batc
   a.mask = t.mask;
   a.mask_words = t.mask_words;
   a.ginv = ((1u << 18) + dm.g - 1) / dm.g;
-  a.chunk_pages = tree_chunk_pages(dm, b, t, p);
+  a.chunk_pages = chunk_pages;
   a.unit = p.unit;
   a.draft_tokens = p.draft_tokens, a.draft_pages = p.draft_pages;
   a.block_cols = p.cols;
@@ -1307,11 +1331,10 @@ hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batc
   a.pacc = (float *)ws;
   a.pml = (float2 *)((char *)ws + align256((size_t)t.num_rows * dm.nq * p.slots * dm.d * 4));
   int chunks = 1;
-  int64_t items = 0;  // chunks of all candidates
+  items = 0;
   for (int i = 0; i < b.batch; ++i) {
-    const int nc = draft_chunks(cached_pages(b, i), draft_extra(p, t.max_rows), a.chunk_pages);
-    chunks = max(chunks, nc);
-    items += nc;
+    chunks = max(chunks, chunks_of(i));
+    items += chunks_of(i);
   }
   a.chunks = chunks;
   const dim3 grid((unsigned)(items * dm.nkv * p.blocks));
