@@ -533,7 +533,7 @@ __global__ __launch_bounds__(256) void k_read_kv(RowArgs a) {
   const int p0 = a.first ? a.first[b] : 0;  // position of the first row
   const int from = max(p0, 0), to = (int)min((int64_t)L, (int64_t)p0 + n);
   const int page = from / kPage + slotpage;
-  if (n <= 0 || page * kPage >= to || from >= to) return;
+  if (n <= 0 || from >= to || page * kPage >= to) return;
   const int id = a.page_table[(size_t)b * a.max_pages + page];
   if (id < 0 || id >= a.num_pages) return;
   const size_t tile = (size_t)id * a.nkv + j;
@@ -574,7 +574,7 @@ __global__ __launch_bounds__(256) void k_read_kv(RowArgs a) {
 #pragma unroll
     for (int i = 0; i < RL; ++i) {
       const int pos = page * kPage + at.slot(p, i);
-      const int64_t row = (int64_t)r0 + (pos - p0);
+      const int64_t row = (int64_t)r0 + pos - p0;
       if (pos < from || pos >= to || row < 0 || row >= a.num_rows) continue;
       uint4 y;
       Vec<S, VS>::store((S *)&y, x[i]);
@@ -644,9 +644,11 @@ hipError_t launch_read_kv(const Dims &dm, const kvprm_kv_cache &c, const kvprm_b
   a.first = first;
   const bool bf16 = r.dtype == KVPRM_BF16;
   const int parts = (r.k ? 1 : 0) + (r.v ? 1 : 0);
-  const int64_t rows = min((int64_t)a.max_rows * b.batch, r.num_rows);
+  const int most = a.max_rows;  // positions of a candidate that hold tokens
+  a.max_rows = r.max_rows;      // (rows of positions below 0 come on top of them)
+  const int64_t rows = min((int64_t)most * b.batch, r.num_rows);
   a.once = rows * dm.nkv * dm.d * parts * (bf16 ? 2 : 4) >= kOnceBytes;
-  const int pages = min(pages_of(a.max_rows), b.max_pages);
+  const int pages = min(pages_of(most), b.max_pages);
   const dim3 grid((unsigned)(((int64_t)pages * parts * dm.nkv + 3) / 4), b.batch);
   KVPRM_ROWS(k_read_kv)
   return hipGetLastError();

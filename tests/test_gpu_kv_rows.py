@@ -268,6 +268,14 @@ def test_read_leaves_other_rows():
     assert np.array_equal(np.flatnonzero(lost), np.concatenate([np.arange(36, 52), np.arange(53, 69)]))
 
 
+def test_read_far_outside():
+    """More rows than the page table has slots, most of them at positions below 0 or past the cache."""
+    _say("read far outside")
+    c = Cache("bf16", 64, [20, 33, 0, 16], [0] * 4, seed=11)
+    _read(c, "bf16", [300, 200, 90, 400], first=[-250, -190, -50, -399])
+    _read(c, "bf16", [300, 2, 90, 4], first=[-2 ** 31, 2 ** 31 - 1, 2 ** 31 - 16, 15])
+
+
 @pytest.mark.parametrize("cdt", ["f32", "bf16", "fp8"])
 def test_write_then_read(cdt):
     """What fp32 rows become in the cache comes back within half a step of its type (fp8: of the
