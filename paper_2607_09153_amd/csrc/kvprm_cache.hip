@@ -88,7 +88,8 @@ struct Vec<uint16_t, 1> {
 // 16 heads of queries and 8 of keys of 128 dims, bf16, 8192 rows (100 MB moved): 22.6 us, 4.45 TB/s, and 18
 // where the caches hold the rows already (non-temporal loads and stores: 20.7 there). Two or four units of a
 // thread in flight, loaded before the table is formed: 5 to 8% slower. 4093 rows of 36 heads of 64, fp32,
-// adjacent pairs (75 MB): 14 us, 5.4 TB/s. One row for each of 16 sequences: 7 us, the launch.
+// adjacent pairs (75 MB): 14 us, partly from the caches, and 19 from memory (4 TB/s). One row for each of 16
+// sequences: 7 us, the launch.
 template <typename T, int V, bool HALF>
 __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
   __shared__ float2 cs[kRotaryCs];

@@ -246,7 +246,7 @@ struct Terms<float> {
 // on the matrix cores with the cache's tiles as they lie in memory (see kvprm_attn.hip), the next pair's loads
 // in flight. Bound by memory on long caches: 8 of 16384 to 32768 tokens, 4 kv-heads of 128 dims, bf16, 28
 // columns (410 MB): 90 us, 4.5 TB/s. On short ones by the chain of loads, products and join: 1103 tokens,
-// 16 drafted, 8 kv-heads: 11 us, and 4 for k_tree_merge.
+// 16 drafted, 8 kv-heads, 32 columns in two blocks of 16: 8 us, and 4 for k_tree_merge.
 template <int KVT, int D, int NC, typename T>
 __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
   constexpr int NKB = D / 32, NDB = D / 16, W = kTreeWaves;
@@ -1122,8 +1122,8 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
 // Joins the chunks of drafted tokens' q-heads, N of them to a wave: weights 2^(m - M) from one load
 // per lane (at most 64 chunks), then the chunk sums in order, two chunks at a time (one per half of the
 // wave, 16 or 8 bytes a lane) and four such pairs in flight. N = 2 where that keeps the grid in one round
-// (the wave is one chain of memory round trips, whatever it does beside): 14336 q-heads of 16 chunks of 128
-// dims, 118 MB read, in 8.4 us; 512 of 10 chunks in 3.2.
+// (the wave is one chain of memory round trips, whatever it does beside): 14336 q-heads of 4 chunks of 128
+// dims, 29 MB read, in 9 us; 256 of 10 chunks in 4.
 template <int D, int N, typename T>
 __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a) {
   const int b = blockIdx.y, lane = threadIdx.x & 63, half = lane >> 5;
@@ -1200,18 +1200,18 @@ constexpr int kWideWaves = 4;
 
 static int draft_extra(const TreePlan &p, int n) { return (n + p.draft_tokens - 1) / p.draft_tokens * p.draft_pages; }
 
-// Kernel by the longest draft's columns where the chip is full (launch_tree has the rule for fewer blocks): k_tree up
-// to 32, which a wave holds at once. At 17 to 32 columns it took
-// 13.7 us where k_tree_wide took 16.5 (1103 tokens, 32 columns), 25.7 and 29.6 (24 fp8 caches of 4800, 32
-// columns), 91 and 88 (8 caches of 16384 to 32768, 28 columns); at 33 to 64, where it reads the pages twice, 42.9
-// and 33.9 (the 24 caches, 48 columns), 108 and 96 (the 8, 56 columns).
+// Kernel by the longest draft's columns where the chip is full (launch_tree has the rule for fewer blocks): k_tree
+// up to 32, which a wave holds at once. At 17 to 32 columns it took 13.7 us where k_tree_wide took 16.5 (1103
+// tokens, 32 columns), 25.7 and 29.6 (24 fp8 caches of 4800, 32 columns), 91 and 88 (8 caches of 16384 to 32768,
+// 28 columns); at 33 to 64, where it reads the pages twice, 42.9 and 33.9 (the 24 caches, 48 columns), 108 and 96
+// (the 8, 56 columns).
 // Chunks leave as many blocks as are resident at once: two of k_tree_wide on a compute unit (three at
 // d_h = 64), two of k_tree. Fewer or more both lose (k_tree_wide, 24 ragged fp8 caches, d_h = 64: 56 us at 680
 // blocks, 54 at 768, 61 at 1024; 8 long bf16 caches, d_h = 128: 403 us at 400, 330 at 512, 394 at 600). Column
 // blocks are counted by the average draft, num_rows / batch, since a candidate's missing ones are no
 // blocks. A k_tree_wide chunk has 16 pages or more: 1200 tokens of 24 candidates take 24 us with least chunks
 // of 8 or 16, 28 with 32. Drafted tokens count as pages of the last chunk (4 for 32 tokens of
-// k_tree_wide, 8 for 64 of k_tree): 13.6 us instead of 15.6 for 1103 tokens, 338 instead of 344 on the long
+// k_tree_wide, a unit for 64 of k_tree): 13.6 us instead of 15.6 for 1103 tokens, 338 instead of 344 on the long
 // caches; 2 to 16 pages differ by less than 2%. Chunk slots: what fills the chip eight times over if the
 // batch's candidates were all as long as the table.
 static TreePlan tree_plan(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t, bool wide) {
@@ -1228,6 +1228,7 @@ static TreePlan tree_plan(const Dims &dm, const kvprm_batch &b, const kvprm_tree
   // average column blocks of a candidate, in 16ths
   const int64_t avg = max((int64_t)16, min((int64_t)p.blocks * 16, t.num_rows * dm.g * 16 / b.batch / p.cols + 8));
   p.fill = (int)max((int64_t)1, (p.wide && dm.d == 64 ? 768 : 512) * 16 / avg);
+  // (fp32 caches: a wave takes pages, not pairs; units of 8 pages took 11.4 us for 4 x 512 tokens, of 4 11.0)
   p.unit = p.wide ? 2 : dm.kvdt == 0 ? kTreeWaves : 2 * kTreeWaves;
   p.least = p.wide ? 16 : p.unit;
   p.draft_tokens = p.wide ? 32 : 64;
