@@ -63,3 +63,11 @@ def test_tree_long_chunk(cdt, dtype, n):
             c.scale[1][:, page] = 2.0 ** (-100 if i < 256 or i > 280 else -7)
         c.upload()
     _check(c)
+
+
+@pytest.mark.parametrize("cdt,dtype,nq,nkv,d", [("bf16", "bf16", 32, 2, 128), ("fp8", "bf16", 32, 2, 64), ("f32", "f32", 13, 1, 64),
+                                                ("fp8", "f32", 16, 1, 128), ("bf16", "bf16", 11, 1, 64)])
+def test_tree_most_columns(cdt, dtype, nq, nkv, d):
+    """256 drafted tokens of 11 to 16 query heads per kv-head: up to 4096 columns."""
+    _say("most columns", cdt, dtype, nq, nkv, d)
+    _check(Case(cdt, dtype, nq, nkv, d, [40, 500, 0], [256, 255, 1], seed=nq))
