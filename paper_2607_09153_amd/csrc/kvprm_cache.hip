@@ -23,10 +23,19 @@ struct RotaryArgs {
   uint32_t uinv, hinv;    // ceil(2^32 / units), ceil(2^32 / heads)
   int64_t rows;
   int rpb;                // rows per block
+  bool once;              // bf16: more rows written than the L2 caches hold
   const int32_t *pos;
   float mag, smag;        // factor on cosines and sines (the sines' negated for the transpose)
   double turn[kMaxRotaryPairs];  // turns per position of each pair
 };
+
+// 16 bytes of a call that moves more than the caches hold, past them; else as usual.
+__device__ __forceinline__ void store_group(uint4 *p, const uint4 &v, bool once) {
+  typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+  if (once) __builtin_nontemporal_store(u32x4v{v.x, v.y, v.z, v.w}, (u32x4v *)p);
+  else *p = v;
+}
+__device__ __forceinline__ uint4 load_group(const uint4 *p, bool once) { return once ? ld_stream(p) : *p; }
 
 // A vector of V elements of T, widened and back (rounded to nearest even).
 template <typename T, int V>
@@ -37,14 +46,14 @@ struct Vec<float, 4> {
     const float4 x = *(const float4 *)p;
     v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
   }
-  static __device__ __forceinline__ void store(float *p, const float *v) {
+  static __device__ __forceinline__ void store(float *p, const float *v, bool = false) {
     *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]);
   }
 };
 template <>
 struct Vec<float, 1> {
   static __device__ __forceinline__ void load(const float *p, float *v) { v[0] = *p; }
-  static __device__ __forceinline__ void store(float *p, const float *v) { *p = v[0]; }
+  static __device__ __forceinline__ void store(float *p, const float *v, bool = false) { *p = v[0]; }
 };
 __device__ __forceinline__ uint32_t bf16x2(float a, float b) {
   typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
@@ -63,9 +72,9 @@ struct Vec<uint16_t, 8> {
       v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
     }
   }
-  static __device__ __forceinline__ void store(uint16_t *p, const float *v) {
-    *(uint4 *)p = make_uint4(bf16x2(v[0], v[1]), bf16x2(v[2], v[3]), bf16x2(v[4], v[5]),
-                             bf16x2(v[6], v[7]));
+  static __device__ __forceinline__ void store(uint16_t *p, const float *v, bool once = false) {
+    store_group((uint4 *)p, make_uint4(bf16x2(v[0], v[1]), bf16x2(v[2], v[3]), bf16x2(v[4], v[5]),
+                                       bf16x2(v[6], v[7])), once);
   }
 };
 template <>
@@ -73,7 +82,7 @@ struct Vec<uint16_t, 1> {
   static __device__ __forceinline__ void load(const uint16_t *p, float *v) {
     v[0] = __uint_as_float((uint32_t)*p << 16);
   }
-  static __device__ __forceinline__ void store(uint16_t *p, const float *v) {
+  static __device__ __forceinline__ void store(uint16_t *p, const float *v, bool = false) {
     *p = (uint16_t)bf16x2(v[0], 0.f);
   }
 };
@@ -85,9 +94,10 @@ struct Vec<uint16_t, 1> {
 // the rotated ones. The angle's turns are reduced in 64 bits, p * f - round(p * f), since p f reaches
 // 10^5 turns and more; the rest, at most half a turn, is exact enough in 32.
 // V = 16 bytes where widths, strides and addresses allow, else one element.
-// 16 heads of queries and 8 of keys of 128 dims, bf16, 8192 rows (100 MB moved): 22.6 us, 4.45 TB/s, and 18
-// where the caches hold the rows already (non-temporal loads and stores: 20.7 there). Two or four units of a
-// thread in flight, loaded before the table is formed: 5 to 8% slower. 4093 rows of 36 heads of 64, fp32,
+// 16 heads of queries and 8 of keys of 128 dims, bf16, 8192 rows (100 MB moved): 21.2 us, 4.75 TB/s, with
+// non-temporal stores (22.6 with ordinary ones; loads too: 20.7 where the caches hold the rows already and this
+// takes 18; fp32 rows lose by them, 14.1 and 14.9 us below). Two or four units of a thread in flight, loaded
+// before the table is formed: 5 to 8% slower. 4093 rows of 36 heads of 64, fp32,
 // adjacent pairs (75 MB): 14 us, partly from the caches, and 19 from memory (4 TB/s). One row for each of 16
 // sequences: 7 us, the launch.
 template <typename T, int V, bool HALF>
@@ -120,7 +130,7 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
       const int e = 2 * a.half + ((int)u - a.nrot) * V;
       float x[V];
       Vec<T, V>::load(src + e, x);
-      Vec<T, V>::store(dst + e, x);
+      Vec<T, V>::store(dst + e, x, a.once);
     } else if (HALF) {
       const int e = (int)u * V;
       float x[V], y[V];
@@ -133,8 +143,8 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
         x[k] = xa * w.x - xb * w.y;
         y[k] = xb * w.x + xa * w.y;
       }
-      Vec<T, V>::store(dst + e, x);
-      Vec<T, V>::store(dst + a.half + e, y);
+      Vec<T, V>::store(dst + e, x, a.once);
+      Vec<T, V>::store(dst + a.half + e, y, a.once);
     } else {
       // (one element at a time: a unit is a pair)
       constexpr int W = V == 1 ? 2 : V;
@@ -154,14 +164,16 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
         x[k + 1] = xb * w.x + xa * w.y;
       }
       if (V == 1) {
-        Vec<T, 1>::store(dst + e, x);
-        Vec<T, 1>::store(dst + e + 1, x + 1);
+        Vec<T, 1>::store(dst + e, x, a.once);
+        Vec<T, 1>::store(dst + e + 1, x + 1, a.once);
       } else {
-        Vec<T, V>::store(dst + e, x);
+        Vec<T, V>::store(dst + e, x, a.once);
       }
     }
   }
 }
+
+constexpr int64_t kL2Bytes = (int64_t)32 << 20;  // eight XCDs' L2 caches
 
 hipError_t launch_rotary(const kvprm_rope &rp, const double *turn, bool bf16, int64_t rows,
                          const int32_t *pos, const kvprm_rope_heads *parts, int num_parts,
@@ -197,6 +209,7 @@ hipError_t launch_rotary(const kvprm_rope &rp, const double *turn, bool bf16, in
   while (rpb < 16 && rpb * 2 * a.half <= kRotaryCs && rows > rpb * 1024 && rpb * per_row < 1024)
     rpb *= 2;
   a.rpb = (int)rpb;
+  a.once = rows * a.heads * a.d * eb >= kL2Bytes;
   const int64_t most = rpb << 23;  // rows of a launch: 2^31 threads
   for (int64_t r0 = 0; r0 < rows; r0 += most) {
     a.rows = min(most, rows - r0);
@@ -504,14 +517,6 @@ __global__ __launch_bounds__(256) void k_write_kv(RowArgs a) {
     out[gi] = w;
   }
 }
-
-// 16 bytes of a call that moves more than the caches hold, past them; else as usual.
-__device__ __forceinline__ void store_group(uint4 *p, const uint4 &v, bool once) {
-  typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
-  if (once) __builtin_nontemporal_store(u32x4v{v.x, v.y, v.z, v.w}, (u32x4v *)p);
-  else *p = v;
-}
-__device__ __forceinline__ uint4 load_group(const uint4 *p, bool once) { return once ? ld_stream(p) : *p; }
 
 // The reverse: one wave per (page, kv-head, part) tile, its 16-byte groups through LDS, rows of the
 // wanted positions out, 16 bytes per lane and store. Bound by memory: 16 fp8 caches of 8192 to 16384 tokens,
