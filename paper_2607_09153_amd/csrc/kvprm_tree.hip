@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "kvprm_attn_common.h"
 #include "kvprm_internal.h"
 #include "kvprm_mx_common.h"
@@ -563,7 +565,6 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
-typedef unsigned short ushortx2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ floatx16 mfma32(const uint4 &a, const uint4 &b, const floatx16 &c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
                                                  __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -584,32 +585,6 @@ __device__ __forceinline__ uint32_t fp8x2_to_half2(uint32_t word) {  // (every e
   const halfx2 v = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(word, 1.0f, HIGH);
   return __builtin_bit_cast(uint32_t, v);
 }
-// The largest of 64 lanes' values (unsigned), as a scalar.
-__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
-  auto step = [](uint32_t x, uint32_t y) { return x > y ? x : y; };
-  v = step(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false));  // as in lane_scan
-  v = step(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false));
-  v = step(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false));
-  v = step(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false));
-  v = step(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));
-  v = step(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false));
-  return __builtin_amdgcn_readlane(v, 63);
-}
-// Exponent that bf16 values of the largest magnitude `mag` (bits) are divided by on their way to fp16:
-// it comes to lie in [2^14, 2^15). Values down to 2^-28 of it keep all their bits, smaller ones become 0.
-__device__ __forceinline__ int half_exponent(uint32_t mag) {
-  return max((int)(mag >> 7) - 141, -112);
-}
-// Two bf16 values divided by 2^(bias / 128 - 112) as fp16; `bias` in both halves.
-__device__ __forceinline__ uint32_t bf16x2_to_half2(uint32_t x, uint32_t bias) {
-  const ushortx2 m = __builtin_bit_cast(ushortx2, x & 0x7FFF7FFFu);
-  const ushortx2 r = __builtin_elementwise_sub_sat(m, __builtin_bit_cast(ushortx2, bias)) << 3;
-  return (x & 0x80008000u) | __builtin_bit_cast(uint32_t, r);
-}
-__device__ __forceinline__ uint32_t max_mag(uint32_t m, uint32_t x) {  // by halves
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushortx2, m),
-                                                                __builtin_bit_cast(ushortx2, x & 0x7FFF7FFFu)));
-}
 
 // The same for drafts of many columns (bf16 rows): here the waves share the pages and split the
 // columns, 32 each. A stage is a page pair (32 tokens) in LDS as 16-bit tiles in the stored order, double
@@ -620,7 +595,9 @@ __device__ __forceinline__ uint32_t max_mag(uint32_t m, uint32_t x) {  // by hal
 // fp16, exactly, and P in fp16 (11 bits), half the products: 8 caches of 16384 to 32768 tokens, 4 kv-heads of
 // 128 dims, 64 drafted tokens of 7 query heads each: 264 us, 700 TFLOP/s, and 285 in two bf16 terms before
 // later steps; from bf16 caches 330 us, 560 TFLOP/s (fp16 values from those too, with an exponent per tile: 357
-// and more).
+// and more). Drafted values stay bf16 over fp8 caches too (two-term weights): as fp16 they would need an exponent
+// that all of them share, and the largest of them would push others out of fp16's range, those also that a token
+// sees without seeing the largest.
 // Bound by vector instructions (about 115 a stage and wave at D = 128, bf16, 160 at D = 64, fp8, beside 24 and 8
 // products) and by how far the two or three waves of a SIMD overlap them with products: a ring of four stages
 // with half the barriers, wave priorities and waves in two groups taking turns all measured the same.
@@ -640,7 +617,6 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
   __shared__ float ksc_s[KVT == 2 ? 2 * SEG + 12 : 1];  // key scales / sqrt(d), log2 units
   __shared__ float vsc_s[KVT == 2 ? 2 * SEG + 12 : 1];  // value scales: factor and exponent
   __shared__ int vex_s[KVT == 2 ? 2 * SEG + 12 : 1];
-  __shared__ uint32_t mag_s;  // largest magnitude of the drafted values of a stage
   // Largest unit so far. Others stay within 2^-kUnits of it: acc moves to each, and would overflow in one
   // far below. (What a unit kept higher loses is below 2^-(kUnits + 20) of the largest values.)
   constexpr int kUnits = 24, kNoUnit = -1000;
@@ -758,14 +734,12 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
     if (role) store_values(s, r);
     else store_keys(s, r);
   };
-  auto draft_unit = [&] { return max(half_exponent(mag_s), base_s - kUnits); };
-  // 32 drafted tokens from t0 on as a page pair in buffer 0 (in fp16: one exponent for all their values).
+  // 32 drafted tokens from t0 on as a page pair in buffer 0, all in bf16.
   auto store_draft = [&](int t0) {
     constexpr int ND = (2 * TC + 64 * W - 1) / (64 * W);
     uint4 *kt = kb[0];
     uint16_t *vt = (uint16_t *)vb[0];
     uint4 rv[ND];
-    uint32_t mag = 0;
     bool bad = false;
 #pragma unroll
     for (int k = 0; k < ND; ++k) {
@@ -783,17 +757,9 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
         // infinities and NaN leave the product (see below)
         if ((x[y] & 0x7F80u) == 0x7F80u) bad = true, x[y] &= 0xFFFF0000u;
         if ((x[y] & 0x7F800000u) == 0x7F800000u) bad = true, x[y] &= 0xFFFFu;
-        mag = max_mag(mag, x[y]);
       }
     }
     if (bad) bad_s = 1;
-    uint32_t bias = 0;
-    if (HALF) {
-      mag = lanes_max(max(mag & 0xFFFFu, mag >> 16));
-      if (lane == 0) atomicMax(&mag_s, mag);
-      __syncthreads();
-      bias = (uint32_t)(112 + draft_unit()) * 0x00800080u;
-    }
 #pragma unroll
     for (int k = 0; k < ND; ++k) {
       const int i = k * 64 * W + tid, t = i / (D / 8), e = 8 * (i % (D / 8)), sl = t & 15;
@@ -803,7 +769,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
       for (int y = 0; y < 8; ++y) {
         const int mm = e + y;
         vt[((t >> 4) * 2 * TC + value_at(mm >> 5, mm & 31, sl >> 2)) * 4 + (sl & 3)] =
-            (uint16_t)((HALF ? bf16x2_to_half2(x[y >> 1], bias) : x[y >> 1]) >> (16 * (y & 1)));
+            (uint16_t)(x[y >> 1] >> (16 * (y & 1)));
       }
     }
   };
@@ -864,16 +830,18 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
         for (int e = 0; e < 16; ++e) acc[t][e] *= alpha;
     }
   };
-  // P's operands by page: fp16 values take the weights in fp16 (times their pages' scales va, vc), bf16
+  // P's operands by page: fp16 values (H) take the weights in fp16 (times their pages' scales va, vc), bf16
   // values in two bf16 terms.
-  auto operands = [&](const float (&p)[16], float va, float vc, uint4 (&ph)[2], uint4 (&pl)[2]) {
+  typedef std::integral_constant<bool, HALF> Cached;
+  typedef std::integral_constant<bool, false> Drafted;
+  auto operands = [&](auto H, const float (&p)[16], float va, float vc, uint4 (&ph)[2], uint4 (&pl)[2]) {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       uint32_t hi[4], lo[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float y0 = p[8 * x + 2 * e], y1 = p[8 * x + 2 * e + 1];
-        if (HALF) {
+        if constexpr (decltype(H)::value) {
           const float f = x ? vc : va;
           hi[e] = half2(y0 * f, y1 * f);
           lo[e] = 0;
@@ -892,14 +860,14 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
       for (int t = 0; t < NT; ++t) vo[x][t] = vb[buf][x * TC + t * 64 + lane];
   };
   // (ua, uc: the units that the two pages' products come in)
-  auto products = [&](const uint4 (&vo)[2][NT], const uint4 (&ph)[2], const uint4 (&pl)[2], int ua, int uc) {
+  auto products = [&](auto H, const uint4 (&vo)[2][NT], const uint4 (&ph)[2], const uint4 (&pl)[2], int ua, int uc) {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       to_unit(x ? uc : ua);
 #pragma unroll
       for (int t = 0; t < NT; ++t)
-        acc[t] = HALF ? mfma32h(vo[x][t], ph[x], acc[t]) : mfma32(vo[x][t], ph[x], acc[t]);
-      if (!HALF)
+        acc[t] = decltype(H)::value ? mfma32h(vo[x][t], ph[x], acc[t]) : mfma32(vo[x][t], ph[x], acc[t]);
+      if (!decltype(H)::value)
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[t] = mfma32(vo[x][t], pl[x], acc[t]);
     }
@@ -917,12 +885,11 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
       r.va = vsc_s[i], r.vc = vsc_s[i + 1];
       r.ua = __builtin_amdgcn_readfirstlane(vex_s[i]), r.uc = __builtin_amdgcn_readfirstlane(vex_s[i + 1]);
     }
-    if (HALF && s < 0) r.ua = r.uc = __builtin_amdgcn_readfirstlane(draft_unit());
     return r;
   };
   // A pair of which only the tokens of `ok` (bit r: this lane's r-th) count: the candidate's last cached
   // one (stage s), or (s < 0) the drafted tokens from d0 on.
-  auto compute_masked = [&](int s, int buf, uint32_t ok, int d0) {
+  auto compute_masked = [&](auto H, int s, int buf, uint32_t ok, int d0) {
     floatx16 sv;
     uint4 ko[KS], vo[2][NT];
     keys(buf & 1, ko);
@@ -940,9 +907,9 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
       l += p[e];
     }
     uint4 ph[2], pl[2];
-    operands(p, sc.va, sc.vc, ph, pl);
+    operands(H, p, sc.va, sc.vc, ph, pl);
     values(buf & 1, vo);
-    products(vo, ph, pl, sc.ua, sc.uc);
+    products(H, vo, ph, pl, sc.ua, sc.uc);
     if (s < 0 && bad_s) {
       // Infinities and NaN among the drafted values: 0 times them would reach the columns that do not
       // attend to them, so they are added column by column.
@@ -973,7 +940,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
     for (int e = 0; e < 16; ++e) ok |= (bits >> (8 * (e >> 2) + 4 * h + (e & 3)) & 1u) << e;
     return ok;
   };
-  if (tid == 0) base_s = kNoUnit, mag_s = 0;
+  if (tid == 0) base_s = kNoUnit;
   for (s0 = 0; s0 < ncache; s0 += SEG) {
     se = min(ncache, s0 + SEG);
     __syncthreads();
@@ -1060,9 +1027,9 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
         keys((s + 1) & 1, ko);
         scores(ko, sv);
         stage();
-        operands(p, sc.va, sc.vc, ph, pl);
+        operands(Cached(), p, sc.va, sc.vc, ph, pl);
         values(s & 1, vo);
-        products(vo, ph, pl, sc.ua, sc.uc);
+        products(Cached(), vo, ph, pl, sc.ua, sc.uc);
       } else {
         stage();
       }
@@ -1075,15 +1042,12 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
     }
     if (s < end) step(s, k0, v1);
     if (end < se && busy)  // the candidate's last pair (in its buffers since the steps before)
-      compute_masked(end, end, own_bits((1u << (L - (p0 + 2 * end) * kPage)) - 1u), -1);
+      compute_masked(Cached(), end, end, own_bits((1u << (L - (p0 + 2 * end) * kPage)) - 1u), -1);
   }
   if (c == nc - 1) {
     for (int t0 = 0; t0 < n; t0 += 32) {
       __syncthreads();
-      if (tid == 0) {
-        if (t0 > 0) base_s = draft_unit() > base_s ? draft_unit() : base_s;
-        bad_s = 0, mag_s = 0;
-      }
+      if (tid == 0) bad_s = 0;
       __syncthreads();
       store_draft(t0);
       __syncthreads();
@@ -1093,7 +1057,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
       if (a.mask) bits = a.mask[(tr.r0 + tok) * a.mask_words + (t0 >> 5)];
       else bits = own >= 31 ? ~0u : own < 0 ? 0u : (2u << own) - 1u;
       if (n - t0 < 32) bits &= (1u << (n - t0)) - 1u;
-      compute_masked(-1, 0, own_bits(bits), t0);
+      compute_masked(Drafted(), -1, 0, own_bits(bits), t0);
     }
   }
   if (!present) return;

@@ -1,0 +1,63 @@
+"""kvprm_attention_tree where a row's own keys and values bound its result, whatever the others hold.
+
+Tolerance of a row: the weights p of what it attends to are rounded to 16 bits (two bf16 terms) or, over fp8 caches
+with more than 32 columns, 11 (fp16), and are off by 2e-5 through the scores (test_gpu_tree.py), so that o = sum p v /
+sum p is off by at most (2^-16 or 2^-11, and 2e-5) sum p |v| / sum p; the bf16 result adds its own half step, 2^-8 |o|."""
+import numpy as np
+import pytest
+
+from oracle import growing_cache as gc
+
+from test_gpu_tree import LAYER, Case, _say
+from test_gpu_tree_full import _sizes
+
+pytestmark = pytest.mark.gpu
+
+
+def _set_bits(c):
+    """The case's mask words from its `sees`, and everything back on the device."""
+    c.bits[:] = 0
+    for b, s in enumerate(c.sees):
+        for j in range(len(s)):
+            c.bits[c.start[b]:c.start[b] + len(s), j // 32] |= s[:, j].astype(np.uint32) << np.uint32(j % 32)
+    c.upload()
+
+
+def _check_rows(c, eps, got=None, scores=1.0):
+    """eps: the weights' rounding; scores: the size of the scores, with which their error grows."""
+    got, want = c.run() if got is None else got, c.want()
+    nq, nkv, d = c.shape
+    y = got[:c.rows, :nq * d].double().numpy()
+    assert np.array_equal(np.isnan(y), np.isnan(want))
+    assert np.array_equal(np.isinf(y), np.isinf(want)) and np.array_equal(y[np.isinf(want)], want[np.isinf(want)])
+    for b, (n, t) in enumerate(zip(c.lengths, c.counts)):
+        if t == 0:
+            continue
+        rows = slice(c.start[b], c.start[b] + t)
+        x = c.qkv[rows].double().numpy()
+        q, k, v = (x[:, i * d:j * d].reshape(t, j - i, d) for i, j in ((0, nq), (nq, nq + nkv), (nq + nkv, nq + 2 * nkv)))
+        ck, cv = (gc.cached(c.tok[p][LAYER], c.scale[p][LAYER], c.cdt, c.table[b], n) for p in (0, 1))
+        v, cv = (np.where(np.isfinite(z), np.abs(z), 0) for z in (v, cv))
+        size = gc.tree_attention(q, k, v, ck, cv, c.sees[b]).reshape(t, nq * d)
+        w, fine = want[rows], np.isfinite(want[rows])
+        tol = (eps + 2e-5 * scores) * size + (2.0 ** -8 * np.abs(w) if c.dtype == "bf16" else 0)
+        off = np.argwhere(fine & ~(np.abs(np.where(fine, y[rows] - w, 0)) <= tol))
+        assert not len(off), (b, off[:3], y[rows][tuple(off[0])], w[tuple(off[0])], tol[tuple(off[0])])
+
+
+@pytest.mark.parametrize("cdt,eps", [("fp8", 2.0 ** -11), ("bf16", 2.0 ** -16)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_tree_large_values_where_masked(cdt, eps, d):
+    """Drafted values of 2^100 and 2^110 that other tokens do not attend to, among values near 1 that they do: in the
+    same 32 tokens, and in earlier ones."""
+    _say("large values where masked", cdt, d)
+    nq, nkv = 8, 2
+    c = Case(cdt, "bf16", nq, nkv, d, *_sizes(60), seed=d)
+    vs = slice((nq + nkv) * d, (nq + 2 * nkv) * d)
+    for b, n in enumerate(c.counts):
+        for t, f in ((1, 2.0 ** 100), (n - 2, 2.0 ** 110)):
+            if n >= 8:
+                c.qkv[c.start[b] + t, vs] *= f
+                c.sees[b][:, t] = np.arange(n) == t
+    _set_bits(c)
+    _check_rows(c, eps)
