@@ -465,7 +465,7 @@ kvprm_status kvprm_workspace_size_tree(kvprm_handle h, const kvprm_batch *batch,
  * sums are fp32; F32 rows keep 24 bits of q and of the probabilities, BF16 rows 16 bits of the
  * probabilities. Over fp8 caches, where max_rows times the q-heads of a kv-head exceeds 32 and the batch fills the
  * chip, those of cached tokens keep 11 bits down to 2^-19 of a row's largest, and have an error of at most 2^-30 of it
- * below. fp8 scales must not be negative. The cache is not written. o must not overlap q, k or v.
+ * below; pages whose value scale lies more than 2^80 below the candidate's largest lose bits. fp8 scales must not be negative. The cache is not written. o must not overlap q, k or v.
  * Rows that no candidate owns are left as they are.
  * Conventions as for kvprm_attention; the prefix-sharing hint is not read. */
 kvprm_status kvprm_attention_tree(kvprm_handle h, const kvprm_kv_cache *cache,

@@ -617,9 +617,10 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
   __shared__ float ksc_s[KVT == 2 ? 2 * SEG + 12 : 1];  // key scales / sqrt(d), log2 units
   __shared__ float vsc_s[KVT == 2 ? 2 * SEG + 12 : 1];  // value scales: factor and exponent
   __shared__ int vex_s[KVT == 2 ? 2 * SEG + 12 : 1];
-  // Largest unit so far. Others stay within 2^-kUnits of it: acc moves to each, and would overflow in one
-  // far below. (What a unit kept higher loses is below 2^-(kUnits + 20) of the largest values.)
-  constexpr int kUnits = 24, kNoUnit = -1000;
+  // Largest unit so far. Others stay within 2^-kUnits of it: acc, which holds up to 2^40 (2^18 tokens' weights below
+  // 2^13 times codes), moves to each, and would overflow in one further below. (What a unit kept higher loses is below
+  // 2^-(kUnits + 20) of the largest values; at 24 that was all of a page of small values whose tokens had the weight.)
+  constexpr int kUnits = 80, kNoUnit = -1000;
   __shared__ int base_s;
   __shared__ int bad_s;
   TreeItem it;

@@ -61,3 +61,22 @@ def test_tree_large_values_where_masked(cdt, eps, d):
                 c.sees[b][:, t] = np.arange(n) == t
     _set_bits(c)
     _check_rows(c, eps)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_tree_small_pages_beside_large_ones(d):
+    """Pages of values near 2^-60 beside one of values near 1 whose tokens have weights below 2^-200."""
+    _say("small pages", d)
+    nq, nkv = 8, 2
+    c = Case("fp8", "bf16", nq, nkv, d, *_sizes(60), seed=d + 1, masked="chain")
+    c.qkv[:, :nq * d] = c.qkv[:, :nq * d].abs()
+    c.qkv[:, (nq + nkv) * d:] *= 2.0 ** -60
+    c.scale[1][:] *= 2.0 ** -60
+    for b, n in enumerate(c.lengths):
+        if n >= 32:
+            page = c.table[b, (n // 16) // 2]
+            c.scale[1][:, page] *= 2.0 ** 60
+            c.tok[0][:, page] = gc.to_e4m3(np.array(-256.0))
+            c.scale[0][:, page] = 0.125
+    c.upload()
+    _check_rows(c, 2.0 ** -11)
