@@ -816,12 +816,14 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
     const auto t = __builtin_amdgcn_permlane32_swap(u, u, false, false);
     return fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
   };
-  // The weights are 2^(score - m). m lies 8 below the largest score when it was set and moves when one
-  // comes to lie more than 12 above it, which leaves out most of the rescaling: the weights stay below
-  // 2^12, and those that fp16 holds with fewer bits, below 2^-14, are 2^-22 of the largest or less.
-  auto new_max = [&](float mx) {
-    if (__any(mx > m + 12.f)) {
-      const float mn = fmaxf(m, mx - 8.f);
+  // The weights are 2^(score - m), and m moves only once a score lies more than a limit above it, which leaves out
+  // most of the rescaling. bf16 weights: m lies 12 above the largest score when it is set and moves when one passes
+  // it; the weights stay below 1, so that values near fp32's largest stay finite. fp16 weights (H): m lies 8 below
+  // and moves when a score comes to lie more than 12 above it; the weights stay below 2^12, and those that fp16
+  // holds with fewer bits, below 2^-14, are 2^-22 of the largest or less.
+  auto new_max = [&](auto H, float mx) {
+    if (__any(mx > (decltype(H)::value ? m + 12.f : m))) {
+      const float mn = fmaxf(m, decltype(H)::value ? mx - 8.f : mx + 12.f);
       const float alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
       m = mn;
       l *= alpha;
@@ -898,7 +900,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
     const Scales sc = scales(s);
 #pragma unroll
     for (int e = 0; e < 16; ++e) sv[e] = ok >> e & 1 ? sv[e] : -INFINITY;
-    new_max(largest(sv, sc.ka, sc.kc));
+    new_max(H, largest(sv, sc.ka, sc.kc));
     const float ms = m == -INFINITY ? 0.f : m;
     float p[16];
 #pragma unroll
@@ -1017,7 +1019,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
       };
       if (busy) {
         const Scales sc = scales(s);
-        new_max(largest(sv, sc.ka, sc.kc));
+        new_max(Cached(), largest(sv, sc.ka, sc.kc));
         float p[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -1044,6 +1046,15 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
     if (s < end) step(s, k0, v1);
     if (end < se && busy)  // the candidate's last pair (in its buffers since the steps before)
       compute_masked(Cached(), end, end, own_bits((1u << (L - (p0 + 2 * end) * kPage)) - 1u), -1);
+  }
+  if (HALF) {  // from here on as over bf16 caches: weights below 1, acc in units of 1
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[t][e] = ldexpf(acc[t][e], unit - 12);
+    unit = 0;
+    m += 12.f;
+    l *= 0x1p-12f;
   }
   if (c == nc - 1) {
     for (int t0 = 0; t0 < n; t0 += 32) {
@@ -1076,12 +1087,11 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
       const int d = 32 * t + 8 * i + 4 * h;
       float v[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e)  // (parts: without the weights' 2^8)
-        v[e] = nc == 1 ? ldexpf(acc[t][4 * i + e] * inv, unit) : ldexpf(acc[t][4 * i + e], unit - 8);
+      for (int e = 0; e < 4; ++e) v[e] = nc == 1 ? acc[t][4 * i + e] * inv : acc[t][4 * i + e];
       if (nc == 1) store4((T *)a.o + row * a.os + (int64_t)head * D + d, v);
       else store4(a.pacc + at * D + d, v);
     }
-  if (nc > 1 && h == 0) a.pml[at] = make_float2(m + 8.f, l * 0.00390625f);
+  if (nc > 1 && h == 0) a.pml[at] = make_float2(m, l);
 }
 
 // Joins the chunks of drafted tokens' q-heads, N of them to a wave: weights 2^(m - M) from one load

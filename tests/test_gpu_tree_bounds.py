@@ -80,3 +80,20 @@ def test_tree_small_pages_beside_large_ones(d):
             c.scale[0][:, page] = 0.125
     c.upload()
     _check_rows(c, 2.0 ** -11)
+
+
+@pytest.mark.parametrize("cdt,eps", [("bf16", 2.0 ** -16), ("fp8", 2.0 ** -11)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_tree_values_near_the_largest(cdt, eps, d):
+    """Cached and drafted values of 2^119 and more."""
+    _say("values near the largest", cdt, d)
+    nq, nkv = 8, 2
+    c = Case(cdt, "bf16", nq, nkv, d, *_sizes(60), seed=d + 2)
+    c.qkv[:, (nq + nkv) * d:(nq + 2 * nkv) * d] *= 2.0 ** 119
+    if cdt == "fp8":
+        c.scale[1][:] *= 2.0 ** 119
+    else:
+        x = (c.tok[1].astype(np.uint32) << 16).view(np.float32) * np.float32(2.0 ** 119)
+        c.tok[1] = gc.to_bf16(x)
+    c.upload()
+    _check_rows(c, eps)
