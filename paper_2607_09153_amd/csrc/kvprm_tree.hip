@@ -1020,10 +1020,11 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
       if (busy) {
         const Scales sc = scales(s);
         new_max(Cached(), largest(sv, sc.ka, sc.kc));
+        const float ms = KVT == 1 && m == -INFINITY ? 0.f : m;  // (all scores -inf so far; fp8 keys are finite)
         float p[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(fmaf(sv[e], e < 8 ? sc.ka : sc.kc, -m));
+          p[e] = __builtin_amdgcn_exp2f(fmaf(sv[e], e < 8 ? sc.ka : sc.kc, -ms));
           l += p[e];
         }
         uint4 ph[2], pl[2], ko[KS], vo[2][NT];

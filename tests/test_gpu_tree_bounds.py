@@ -97,3 +97,22 @@ def test_tree_values_near_the_largest(cdt, eps, d):
         c.tok[1] = gc.to_bf16(x)
     c.upload()
     _check_rows(c, eps)
+
+
+@pytest.mark.parametrize("counts", [None, 4])
+@pytest.mark.parametrize("d", [64, 128])
+def test_tree_scores_of_minus_infinity(counts, d):
+    """The first cached keys, 40 of them, and every second drafted one give scores of minus infinity: weights of 0."""
+    _say("scores of minus infinity", counts, d)
+    nq, nkv = 8, 2
+    sizes = _sizes(60) if counts is None else ([700, 100, 0], [counts] * 3)
+    c = Case("bf16", "bf16", nq, nkv, d, *sizes, seed=d + 4, masked="chain")
+    c.qkv[:, :nq * d] = c.qkv[:, :nq * d].abs() + 0.125
+    c.qkv[1::2, nq * d:(nq + nkv) * d] = -float("inf")
+    for b, n in enumerate(c.lengths):
+        c.qkv[c.start[b]:c.start[b] + 1, nq * d:(nq + nkv) * d] = 0.5  # (the first drafted key is finite)
+        for t in range(min(n, 40)):
+            c.tok[0][:, c.table[b, t // 16], :, t % 16] = 0xFF80
+    c.upload()
+    assert np.isfinite(c.want()).all()
+    _check_rows(c, 2.0 ** -16)
