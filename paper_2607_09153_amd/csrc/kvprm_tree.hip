@@ -240,6 +240,45 @@ struct Terms<float> {
   static constexpr int Q = 3, P = 3;
 };
 
+// Infinities among cached bf16 values. A weight is a sum of bf16 terms, of which the lower ones may be 0 or negative,
+// so that its product with an infinity can be NaN where the definition has the infinity. Sums that ended as NaN
+// therefore look up which infinities their dim holds: a wave reads the value tiles of its pages once more, at the
+// memory's rate but for the tiles that hold something not finite. (Where all sums are finite this costs their test.)
+template <int N>
+struct Special {
+  uint64_t plus = 0, minus = 0, nan = 0;  // bit y: the dim of this lane's y-th sum
+  // The first `slots` slots of a bf16 value tile (see kvprm_kv_cache); dim(y): dim of the y-th sum.
+  template <int D, typename F>
+  __device__ __forceinline__ void look(const uint16_t *tile, int slots, int lane, F dim) {
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      const uint4 x = ((const uint4 *)tile)[i * 64 + lane];
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) any = any || (w[e] & 0x7F80u) == 0x7F80u || (w[e] & 0x7F800000u) == 0x7F800000u;
+    }
+    if (!__any(any)) return;
+#pragma unroll 1
+    for (int y = 0; y < N; ++y) {
+      const int m = dim(y);
+#pragma unroll 1
+      for (int s = 0; s < slots; ++s) {
+        const uint32_t v = tile[((((m >> 5) * 4 + (s >> 2)) * 16 + (m & 15)) * 2 + (m >> 4 & 1)) * 4 + (s & 3)];
+        if ((v & 0x7F80u) != 0x7F80u) continue;
+        const uint64_t bit = (uint64_t)1 << y;
+        if (v & 0x7Fu) nan |= bit;
+        else if (v >> 15) minus |= bit;
+        else plus |= bit;
+      }
+    }
+  }
+  __device__ __forceinline__ float mend(float sum, int y) const {  // the y-th sum
+    const bool p = plus >> y & 1, q = minus >> y & 1;
+    return sum == sum || (nan >> y & 1) || p == q ? sum : p ? INFINITY : -INFINITY;
+  }
+};
+
 // o = softmax(q K^T / sqrt(d)) V for NC tiles of 16 columns (drafted token, q-head of the kv-head's
 // group), over one chunk of a candidate's cached pages; the last chunk also takes the drafted keys.
 // A block's four waves take page pairs in turn and join their softmax states in LDS, so that a chunk is
@@ -446,6 +485,31 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
         if (i + 1 < mine) compute(i + 1, r1);
         __builtin_amdgcn_sched_barrier(0);
       }
+    }
+  }
+
+  if constexpr (KVT == 1) {
+    float z[4] = {0.f, 0.f, 0.f, 0.f};  // NaN where a sum is not finite
+#pragma unroll
+    for (int ct = 0; ct < NC; ++ct)
+#pragma unroll
+      for (int nb = 0; nb < NDB; ++nb)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] = fmaf(st[ct].acc[nb][e], 0.f, z[e]);
+    if (__any((z[0] + z[1]) + (z[2] + z[3]) != 0.f)) {
+      Special<NDB * 4> sp;
+      for (int i = 0; i < np; ++i) {
+        if ((i >> 1) % W != w) continue;  // (a segment is a multiple of W pairs)
+        const int id = min(max(a.page_table[(size_t)b * a.max_pages + p0 + i], 0), a.num_pages - 1);
+        sp.template look<D>((const uint16_t *)(a.vp + ((size_t)id * a.nkv + j) * TILE), min(kPage, L - (p0 + i) * kPage),
+                            lane, [&](int y) { return 16 * (y >> 2) + 4 * cq + (y & 3); });
+      }
+#pragma unroll
+      for (int ct = 0; ct < NC; ++ct)
+#pragma unroll
+        for (int nb = 0; nb < NDB; ++nb)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) st[ct].acc[nb][e] = sp.mend(st[ct].acc[nb][e], 4 * nb + e);
     }
   }
 
@@ -1047,6 +1111,25 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
     if (s < end) step(s, k0, v1);
     if (end < se && busy)  // the candidate's last pair (in its buffers since the steps before)
       compute_masked(Cached(), end, end, own_bits((1u << (L - (p0 + 2 * end) * kPage)) - 1u), -1);
+  }
+  if (KVT == 1) {
+    float z[4] = {0.f, 0.f, 0.f, 0.f};  // NaN where a sum is not finite
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) z[e & 3] = fmaf(acc[t][e], 0.f, z[e & 3]);
+    if (__any((z[0] + z[1]) + (z[2] + z[3]) != 0.f)) {
+      Special<NT * 16> sp;
+      for (int i = 0; i < np; ++i) {
+        const int id = min(max(a.page_table[(size_t)b * a.max_pages + p0 + i], 0), a.num_pages - 1);
+        sp.template look<D>((const uint16_t *)a.vp + ((size_t)id * a.nkv + j) * (kPage * D), min(kPage, L - (p0 + i) * kPage),
+                            lane, [&](int y) { return 8 * (y >> 2) + 4 * h + (y & 3); });
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[t][e] = sp.mend(acc[t][e], 16 * t + e);
+    }
   }
   if (HALF) {  // from here on as over bf16 caches: weights below 1, acc in units of 1
 #pragma unroll

@@ -99,6 +99,35 @@ def test_tree_values_near_the_largest(cdt, eps, d):
     _check_rows(c, eps)
 
 
+@pytest.mark.parametrize("dtype,counts", [("bf16", None), ("bf16", 5), ("f32", 9), ("bf16", 40)])
+@pytest.mark.parametrize("cdt", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_tree_cached_infinities(cdt, dtype, counts, d):
+    """Infinities and NaN among the cached values reach every token as the definition says; those of drafted values
+    meet them. Several chunks, the cache's last page among those that hold them; slots past the length hold NaN."""
+    _say("cached infinities", cdt, dtype, counts, d)
+    nq, nkv = 8, 2
+    sizes = _sizes(60) if counts is None else ([2000, 33, 7, 300], [counts, 2, 8, counts])
+    c = Case(cdt, dtype, nq, nkv, d, *sizes, seed=d + 3)
+    word = {"bf16": (0x7F80, 0xFF80, 0x7FC0), "f32": (0x7F800000, 0xFF800000, 0x7FC00000)}[cdt]
+    rng = np.random.default_rng(d)
+    for b, n in enumerate(c.lengths):
+        for i in range(6 if n >= 5 and b % 3 != 1 else 0):
+            t = n - 1 if i == 0 else int(rng.integers(0, n))
+            # one sign to a dim, most of the time; a NaN now and then
+            dims = rng.integers(0, d, size=4)
+            kind = 2 if rng.random() < 0.1 else None
+            for m in dims:
+                c.tok[1][:, c.table[b, t // 16], :, t % 16, m] = word[int(m) % 2 if kind is None else kind]
+        if b % 4 == 0 and c.counts[b] >= 2:
+            c.qkv[c.start[b], (nq + nkv) * d + 5:(nq + nkv) * d + d] = float("inf")
+    c.upload()
+    want = c.want()
+    assert np.isinf(want).any() and np.isnan(want).any() and np.isfinite(want).any()
+    assert (want == np.inf).any() and (want == -np.inf).any()
+    _check_rows(c, 2.0 ** -16)
+
+
 @pytest.mark.parametrize("counts", [None, 4])
 @pytest.mark.parametrize("d", [64, 128])
 def test_tree_scores_of_minus_infinity(counts, d):
