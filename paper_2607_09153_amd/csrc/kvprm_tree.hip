@@ -1257,6 +1257,10 @@ struct TreePlan {
 
 constexpr int kWideWaves = 4;
 
+// Drafted tokens there can be (an array may have rows to spare).
+static int64_t draft_rows(const kvprm_batch &b, const kvprm_tree &t) {
+  return min((int64_t)b.batch * t.max_rows, t.num_rows);
+}
 static int draft_extra(const TreePlan &p, int n) { return (n + p.draft_tokens - 1) / p.draft_tokens * p.draft_pages; }
 
 // Kernel by the longest draft's columns where the chip is full (launch_tree has the rule for fewer blocks): k_tree
@@ -1267,7 +1271,7 @@ static int draft_extra(const TreePlan &p, int n) { return (n + p.draft_tokens - 
 // Chunks leave as many blocks as are resident at once: two of k_tree_wide on a compute unit (three at
 // d_h = 64), two of k_tree. Fewer or more both lose (k_tree_wide, 24 ragged fp8 caches, d_h = 64: 56 us at 680
 // blocks, 54 at 768, 61 at 1024; 8 long bf16 caches, d_h = 128: 403 us at 400, 330 at 512, 394 at 600). Column
-// blocks are counted by the average draft, num_rows / batch, since a candidate's missing ones are no
+// blocks are counted by the average draft, draft_rows / batch, since a candidate's missing ones are no
 // blocks. A k_tree_wide chunk has 16 pages or more: 1200 tokens of 24 candidates take 24 us with least chunks
 // of 8 or 16, 28 with 32. Drafted tokens count as pages of the last chunk (4 for 32 tokens of
 // k_tree_wide, a unit for 64 of k_tree): 13.6 us instead of 15.6 for 1103 tokens, 338 instead of 344 on the long
@@ -1282,10 +1286,11 @@ static TreePlan tree_plan(const Dims &dm, const kvprm_batch &b, const kvprm_tree
   p.blocks = (cols + p.cols - 1) / p.cols;
   // Spread evenly, unless the average draft needs fewer blocks than the longest: 24 drafts of 1 to 48 tokens of
   // 4 query heads took 55 us in blocks of 128 columns and 68 in blocks of 96.
-  if (p.wide && t.num_rows * dm.g > (int64_t)b.batch * (p.blocks - 1) * p.cols)
+  const int64_t rows = draft_rows(b, t);
+  if (p.wide && rows * dm.g > (int64_t)b.batch * (p.blocks - 1) * p.cols)
     p.cols = ((cols + p.blocks - 1) / p.blocks + 31) / 32 * 32;
   // average column blocks of a candidate, in 16ths
-  const int64_t avg = max((int64_t)16, min((int64_t)p.blocks * 16, t.num_rows * dm.g * 16 / b.batch / p.cols + 8));
+  const int64_t avg = max((int64_t)16, min((int64_t)p.blocks * 16, rows * dm.g * 16 / b.batch / p.cols + 8));
   p.fill = (int)max((int64_t)1, (p.wide && dm.d == 64 ? 768 : 512) * 16 / avg);
   // (fp32 caches: a wave takes pages, not pairs; units of 8 pages took 11.4 us for 4 x 512 tokens, of 4 11.0)
   p.unit = p.wide ? 2 : dm.kvdt == 0 ? kTreeWaves : 2 * kTreeWaves;
@@ -1323,7 +1328,7 @@ static int tree_chunk_pages(const Dims &dm, const kvprm_batch &b, const kvprm_tr
   int longest = 1;
   for (int i = 0; i < b.batch; ++i) longest = max(longest, cached_pages(b, i));
   longest += draft_extra(p, t.max_rows);
-  const int extra = draft_extra(p, (int)(t.num_rows / b.batch));
+  const int extra = draft_extra(p, (int)(draft_rows(b, t) / b.batch));
   const int64_t most = max((int64_t)p.fill / dm.nkv, (int64_t)b.batch);
   // in units: the least is (too few or) enough, the longest candidate whole is enough
   int lo = max(p.least, (longest + p.slots - 1) / p.slots + p.unit - 1) / p.unit;
@@ -1428,7 +1433,7 @@ hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batc
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || chunks == 1) return e;
   // (8192 waves are resident at once)
-  const int n = min((int64_t)b.batch * t.max_rows, t.num_rows) * dm.nq > 8192 ? 2 : 1;
+  const int n = draft_rows(b, t) * dm.nq > 8192 ? 2 : 1;
   const dim3 mgrid((unsigned)(((int64_t)t.max_rows * dm.nq + 4 * n - 1) / (4 * n)), b.batch);
 #define KVPRM_MERGE_T(D_, N_)                                                                     \
   if (bf16) hipLaunchKernelGGL((k_tree_merge<D_, N_, uint16_t>), mgrid, dim3(256), 0, s, a);      \

@@ -145,3 +145,16 @@ def test_tree_scores_of_minus_infinity(counts, d):
     c.upload()
     assert np.isfinite(c.want()).all()
     _check_rows(c, 2.0 ** -16)
+
+
+@pytest.mark.parametrize("cdt,n", [("bf16", 16), ("bf16", 64), ("fp8", 64), ("f32", 16)])
+def test_tree_padded_rows(cdt, n):
+    """Arrays with rows to spare: the same bits as without them."""
+    _say("padded rows", cdt, n)
+    c = Case(cdt, "f32" if cdt == "f32" else "bf16", 16, 8, 128, [300] * 24, [n] * 24, seed=n, masked="chain",
+             spare_rows=6000)
+    c.o = c.o.new_full((c.rows + 6000, c.o.shape[1]), 7.0)
+    got = c.run(tree=c.tree(num_rows=c.rows))
+    c.o.fill_(7.0)
+    padded = c.run(tree=c.tree(num_rows=c.rows + 6000))
+    assert bool((got == padded).all())
