@@ -453,8 +453,9 @@ typedef struct {
   int32_t mask_words;         /* >= ceil(max_rows / 32) with a mask */
 } kvprm_tree;
 
-/* Bytes of device workspace kvprm_attention_tree needs (from the batch's size and max_pages, and the
- * tree's num_rows, max_rows and dtype alone). */
+/* Bytes of device workspace that serve kvprm_attention_tree for this call and every one of at most this
+ * batch's size and max_pages and this tree's num_rows and max_rows, with the same dtype (on which alone it
+ * depends). */
 kvprm_status kvprm_workspace_size_tree(kvprm_handle h, const kvprm_batch *batch,
                                        const kvprm_tree *tree, size_t *bytes);
 

@@ -1038,7 +1038,7 @@ kvprm_status kvprm_attention_tree(kvprm_handle h, const kvprm_kv_cache *cache, c
   if ((st = check_rows(t->o, t->o_stride, nq, t->dtype, "o", fn)) != KVPRM_OK) return st;
   if (t->mask && t->mask_words < (t->max_rows + 31) / 32)
     return fail(KVPRM_E_INVALID, "%s: mask_words %d below %d", fn, t->mask_words, (t->max_rows + 31) / 32);
-  const size_t need = tree_ws_bytes(h->dm, *b, *t);
+  const size_t need = tree_ws_need(h->dm, *b, *t);
   if (!workspace || ws_bytes < need)
     return fail(KVPRM_E_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need,
                 workspace ? ws_bytes : (size_t)0);

@@ -246,7 +246,8 @@ hipError_t launch_read_kv(const Dims &dm, const kvprm_kv_cache &c, const kvprm_b
                           const kvprm_kv_rows &r, const int32_t *first, hipStream_t s);
 // attention of drafted tokens (kvprm_tree.hip)
 constexpr int kMaxTreeRows = 256;
-size_t tree_ws_bytes(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t);
+size_t tree_ws_need(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t);   // of this call
+size_t tree_ws_bytes(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t);  // of this one and all smaller ones
 hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batch &b, int layer,
                        const kvprm_tree &t, void *ws, hipStream_t s);
 hipError_t launch_head(const Dims &dm, const Plan &p, const Workspace &w, const void *final_norm,

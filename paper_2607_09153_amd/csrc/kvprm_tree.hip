@@ -34,6 +34,7 @@ struct TreeArgs {
   int draft_tokens, draft_pages;  // so many drafted tokens (or a part) take a block as long as so many pages
   int chunks;              // chunks of the grid: a candidate has no more
   int slots;               // chunk slots of a (row, q-head) in the workspace (at least chunks)
+  int part_rows;           // workspace rows of a candidate; 0: as the arrays' rows
   float *pacc;             // [row][q-head][slot][D] chunk sums
   float2 *pml;             // [row][q-head][slot] chunk maximum (log2 units) and sum
 };
@@ -54,6 +55,11 @@ __device__ __forceinline__ TreeRows tree_rows(const TreeArgs &a, int b) {
   r.r0 = s0;
   r.n = s0 < 0 || s0 >= a.num_rows ? 0 : (int)min((int64_t)min(s1 - s0, a.max_rows), a.num_rows - s0);
   return r;
+}
+
+// The workspace row of a candidate's first token.
+__device__ __forceinline__ int part_row(const TreeArgs &a, int b, const TreeRows &r) {
+  return a.part_rows ? b * a.part_rows : (int)r.r0;
 }
 
 // A candidate's cached pages in chunks of equal size (to a unit), as few as have at most chunk_pages
@@ -600,7 +606,7 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
       l += f[x] * ml.y;
     }
     const int64_t row = tr.r0 + tok[ct];
-    const int64_t at = (row * a.nq + head[ct]) * a.slots + c;
+    const int64_t at = ((int64_t)(part_row(a, b, tr) + tok[ct]) * a.nq + head[ct]) * a.slots + c;
 #pragma unroll
     for (int k = 0; k < NDB / W; ++k) {
       const int nb = w * (NDB / W) + k;
@@ -698,10 +704,21 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
   const int p0 = c * sp.pages, np = max(0, min(sp.pages, npages - p0));
   const int tid = threadIdx.x, lane = tid & 63, cn = lane & 31, h = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int cols = n * g, col0 = it.colblock * a.block_cols + w * 32, col = col0 + cn;
-  const bool busy = col0 < cols && w * 32 < a.block_cols, present = busy && col < cols;
-  const int tok = present ? (int)(((uint32_t)col * a.ginv) >> 18) : 0;
-  const int head = j * g + (present ? col - tok * g : 0);
+  const int cols = n * g, col0 = it.colblock * a.block_cols + w * 32;
+  const bool busy = col0 < cols && w * 32 < a.block_cols;
+  struct Column {  // a lane's column: drafted token and q-head
+    bool present;
+    int tok, head;
+  };
+  auto column = [&](int lane) {
+    const int col = col0 + (lane & 31);
+    Column r = {busy && col < cols, 0, j * g};
+    if (r.present) {
+      r.tok = (int)(((uint32_t)col * a.ginv) >> 18);
+      r.head += col - r.tok * g;
+    }
+    return r;
+  };
   const float rs = kLog2e / sqrtf((float)D);
   const int ncache = (np + 1) >> 1;                    // stages of cached pages
   const int nfull = max(0, L - p0 * kPage) >> 5;       // of these, the first without a slot at or past L
@@ -710,11 +727,12 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
 
   uint4 qo[KS];
   {
-    const T *q = (const T *)a.q + (tr.r0 + tok) * a.qs + (int64_t)head * D;
+    const Column my = column(lane);
+    const T *q = (const T *)a.q + (tr.r0 + my.tok) * a.qs + (int64_t)my.head * D;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       const uint4 v = *(const uint4 *)(q + 16 * ks + 8 * h);
-      qo[ks] = present ? v : make_uint4(0, 0, 0, 0);
+      qo[ks] = my.present ? v : make_uint4(0, 0, 0, 0);
     }
   }
   // A stage's keys or values in registers, as 16-byte groups in memory order. (No branch around loads,
@@ -1140,6 +1158,9 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
     m += 12.f;
     l *= 0x1p-12f;
   }
+  // (the column once more, from the lane's number: held over the loop it would take registers that are not there)
+  const Column my = column(__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)));
+  const int tok = my.tok, head = my.head;
   if (c == nc - 1) {
     for (int t0 = 0; t0 < n; t0 += 32) {
       __syncthreads();
@@ -1156,13 +1177,13 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
       compute_masked(Drafted(), -1, 0, own_bits(bits), t0);
     }
   }
-  if (!present) return;
+  if (!my.present) return;
   {
     const uint32_t u = __float_as_uint(l);
     const auto t = __builtin_amdgcn_permlane32_swap(u, u, false, false);
     l = __uint_as_float(t[0]) + __uint_as_float(t[1]);
   }
-  const int64_t row = tr.r0 + tok, at = (row * a.nq + head) * a.slots + c;
+  const int64_t row = tr.r0 + tok, at = ((int64_t)(part_row(a, b, tr) + tok) * a.nq + head) * a.slots + c;
   const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int t = 0; t < NT; ++t)
@@ -1197,7 +1218,7 @@ __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a) {
   vec x[N][4];
 #pragma unroll
   for (int z = 0; z < N; ++z) {
-    const int64_t at = (tr.r0 * a.nq + min(item + z, items - 1)) * a.slots;
+    const int64_t at = ((int64_t)part_row(a, b, tr) * a.nq + min(item + z, items - 1)) * a.slots;
     p[z] = (const vec *)(a.pacc + at * D) + (lane & 31);
     ml[z] = lane < nc ? a.pml[at + lane] : make_float2(-INFINITY, 0.f);
 #pragma unroll
@@ -1277,6 +1298,7 @@ static int draft_extra(const TreePlan &p, int n) { return (n + p.draft_tokens - 
 // k_tree_wide, a unit for 64 of k_tree): 13.6 us instead of 15.6 for 1103 tokens, 338 instead of 344 on the long
 // caches; 2 to 16 pages differ by less than 2%. Chunk slots: what fills the chip eight times over if the
 // batch's candidates were all as long as the table.
+static int full_chip(const Dims &dm, bool wide) { return wide && dm.d == 64 ? 768 : 512; }
 static TreePlan tree_plan(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t, bool wide) {
   TreePlan p;
   const int cols = t.max_rows * dm.g;
@@ -1291,7 +1313,7 @@ static TreePlan tree_plan(const Dims &dm, const kvprm_batch &b, const kvprm_tree
     p.cols = ((cols + p.blocks - 1) / p.blocks + 31) / 32 * 32;
   // average column blocks of a candidate, in 16ths
   const int64_t avg = max((int64_t)16, min((int64_t)p.blocks * 16, rows * dm.g * 16 / b.batch / p.cols + 8));
-  p.fill = (int)max((int64_t)1, (p.wide && dm.d == 64 ? 768 : 512) * 16 / avg);
+  p.fill = (int)max((int64_t)1, full_chip(dm, p.wide) * 16 / avg);
   // (fp32 caches: a wave takes pages, not pairs; units of 8 pages took 11.4 us for 4 x 512 tokens, of 4 11.0)
   p.unit = p.wide ? 2 : dm.kvdt == 0 ? kTreeWaves : 2 * kTreeWaves;
   p.least = p.wide ? 16 : p.unit;
@@ -1310,12 +1332,34 @@ static bool may_be_wide(const Dims &dm, const kvprm_tree &t) {
   return t.dtype == KVPRM_BF16 && dm.kvdt != 0 && t.max_rows * dm.g > 32;
 }
 
-size_t tree_ws_bytes(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t) {
+static size_t parts_bytes(const Dims &dm, int64_t parts) {  // parts: (row, slot) pairs
+  return align256((size_t)parts * dm.nq * dm.d * 4) + align256((size_t)parts * dm.nq * 8);
+}
+
+// What one call takes.
+size_t tree_ws_need(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t) {
   int slots = tree_plan(dm, b, t, false).slots;
   if (may_be_wide(dm, t)) slots = max(slots, tree_plan(dm, b, t, true).slots);
-  if (slots == 1) return 256;
-  const size_t parts = (size_t)t.num_rows * dm.nq * slots;
-  return align256(parts * dm.d * 4) + align256(parts * 8);
+  return slots == 1 ? 256 : parts_bytes(dm, draft_rows(b, t) * slots);
+}
+
+// What the largest call of at most so many candidates, pages, rows and rows per candidate takes, so that a workspace
+// sized once serves smaller batches, whose chip is filled by more chunks. With r = draft_rows, B candidates and n
+// kv-heads a plan has slots < 8 fill / (B n) + 1 and fill <= full 16 / avg, where avg >= 16 and avg >= r g 16 / (B cols):
+// r slots <= r + 8 full / n min(r / B, cols / g), which grows with all four; nor are there more slots than
+// chunks.
+size_t tree_ws_bytes(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t) {
+  const int64_t rows = draft_rows(b, t);
+  int64_t parts = 0;
+  for (int wide = 0; wide <= may_be_wide(dm, t); ++wide) {
+    const TreePlan p = tree_plan(dm, b, t, wide);
+    const int64_t chunks = min((int64_t)64, (int64_t)draft_chunks(b.max_pages, draft_extra(p, t.max_rows), p.least));
+    const int64_t columns = wide ? 32 * kWideWaves : 32;
+    const int64_t filled = 8 * (int64_t)full_chip(dm, wide) * min(t.max_rows * (int64_t)dm.g, columns);
+    const int64_t per = dm.nkv * dm.g;
+    if (chunks > 1) parts = max(parts, min(rows * chunks, rows + (filled + per - 1) / per));
+  }
+  return max((size_t)256, parts_bytes(dm, parts));
 }
 
 static int cached_pages(const kvprm_batch &b, int i) {
@@ -1394,7 +1438,8 @@ hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batc
   a.block_cols = p.cols;
   a.slots = p.slots;
   a.pacc = (float *)ws;
-  a.pml = (float2 *)((char *)ws + align256((size_t)t.num_rows * dm.nq * p.slots * dm.d * 4));
+  a.part_rows = draft_rows(b, t) < t.num_rows ? t.max_rows : 0;
+  a.pml = (float2 *)((char *)ws + align256((size_t)draft_rows(b, t) * dm.nq * p.slots * dm.d * 4));
   int chunks = 1;
   items = 0;
   for (int i = 0; i < b.batch; ++i) {
