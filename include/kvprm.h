@@ -416,7 +416,8 @@ typedef struct {
  * scales) of `cache` are WRITTEN; other slots and pages keep their bytes, but for this:
  * an fp8 tile's scale becomes the smallest power of two s >= 2^-100 with 448 s >= |x| for every
  * new x of the tile, at least its present scale (rounded up to a power of two) if the page holds
- * earlier tokens, whose codes are then rounded to the new scale where it changes. A power of two
+ * earlier tokens, whose codes are then rounded to the new scale where it changes (present scales are positive, up
+ * to 2^126). A power of two
  * costs no significant bit on either way, so that a code is rounded again only where it leaves e4m3's
  * normal range. Infinities and NaN are stored as NaN in fp8 (and do not enter the scale).
  * Rows past max_pages * 16 tokens, with a row number outside [0, num_rows) or whose page id is outside

@@ -440,7 +440,7 @@ __global__ __launch_bounds__(256) void k_write_kv(RowArgs a) {
         }
     int e = scale_exponent(wmax(m));
     if (old > 0) e = max(e, ceil_exponent(before));
-    e = min(e, 120);
+    e = min(e, 126);  // (new values need 2^120 at most; the inverse of 2^126 is a normal number)
     const float scale = exp2i(e), inv = exp2i(-e);
     if (old > 0 && scale != before) {
       grew = true;
