@@ -390,9 +390,10 @@ typedef struct {
  * tensors of `rows` rows, p = positions[row] (device int32, any value): pair (a, b) becomes
  * (a cos - b sin, b cos + a sin) with angle p f_i. transpose != 0 applies magnitude * R^T, the
  * gradient of the rotation (sines negated). Angles are formed in 64 bits, products in 32, each
- * result is rounded once. dst may be src (same stride); otherwise the rows written must not be
- * rows read. KVPRM_E_INVALID: a null or misaligned pointer (element size), a stride below the
- * row, overlapping src and dst, values outside the ranges above. rows = 0 does nothing. */
+ * result is rounded once. A tensor's dst may be its src (same stride); otherwise no row written may share a byte
+ * with a row read or written of either tensor (rows side by side in one buffer, of equal strides, do not).
+ * KVPRM_E_INVALID: a null or misaligned pointer (element size), a stride below the row, rows that overlap,
+ * or rows of unequal strides between each other, values outside the ranges above. rows = 0 does nothing. */
 kvprm_status kvprm_rotary(const kvprm_rope *rope, kvprm_dtype dtype, int64_t rows,
                           const int32_t *positions, const kvprm_rope_heads *parts,
                           int32_t num_parts, int32_t transpose, void *stream);

@@ -828,6 +828,18 @@ static void rope_turns(const kvprm_rope &r, double *turn) {
   }
 }
 
+// Whether rows of `wa` bytes every `sa` from a on and rows of `wb` bytes every `sb` from b on share a byte. Rows that
+// lie next to each other (columns of one buffer) do not; interleaved rows of unequal strides are taken to.
+static bool rows_meet(uintptr_t a, uintptr_t sa, uintptr_t wa, uintptr_t b, uintptr_t sb, uintptr_t wb,
+                      int64_t rows) {
+  const uintptr_t na = (uintptr_t)(rows - 1) * sa + wa, nb = (uintptr_t)(rows - 1) * sb + wb;
+  if (a >= b + nb || b >= a + na) return false;
+  if (rows == 1 || sa != sb) return true;
+  // where the later one's rows begin between two of the earlier one's
+  const uintptr_t off = (a > b ? a - b : b - a) % sa;
+  return off < (a > b ? wb : wa) || off + (a > b ? wa : wb) > sa;
+}
+
 kvprm_status kvprm_rotary(const kvprm_rope *rope, kvprm_dtype dtype, int64_t rows,
                           const int32_t *positions, const kvprm_rope_heads *parts,
                           int32_t num_parts, int32_t transpose, void *stream) {
@@ -872,20 +884,23 @@ kvprm_status kvprm_rotary(const kvprm_rope *rope, kvprm_dtype dtype, int64_t row
     if (!p.src || !p.dst) return fail(KVPRM_E_INVALID, "%s: null tensor %d", fn, i);
     if (((uintptr_t)p.src | (uintptr_t)p.dst) % eb != 0)
       return fail(KVPRM_E_INVALID, "%s: tensor %d not aligned to its elements", fn, i);
-    if (p.src == p.dst && p.src_stride == p.dst_stride) continue;
-    // rows written next to rows read (other columns of one buffer) are no overlap
-    const uintptr_t a = (uintptr_t)p.src, b = (uintptr_t)p.dst;
-    const uintptr_t na = (uintptr_t)(((rows - 1) * p.src_stride + width) * eb);
-    const uintptr_t nb = (uintptr_t)(((rows - 1) * p.dst_stride + width) * eb);
-    if (a < b + nb && b < a + na) {
-      const uintptr_t step = (uintptr_t)(p.src_stride * eb), w = (uintptr_t)(width * eb);
-      const uintptr_t off = (a > b ? a - b : b - a) % step;
-      if (p.src_stride != p.dst_stride || off < w || step - off < w)
-        return fail(KVPRM_E_INVALID, "%s: src and dst of tensor %d overlap", fn, i);
-    }
   }
   if (rows == 0) return ok();
   if (!positions) return fail(KVPRM_E_INVALID, "%s: null positions", fn);
+  if ((uintptr_t)positions % sizeof(int32_t) != 0)
+    return fail(KVPRM_E_INVALID, "%s: positions not aligned to its elements", fn);
+  // what is written: no row read but the tensor's own in place, and no row of the other tensor's result
+  for (int i = 0; i < num_parts; ++i)
+    for (int j = 0; j < num_parts; ++j) {
+      const kvprm_rope_heads &w = parts[i], &p = parts[j];
+      const uintptr_t ww = (uintptr_t)(w.heads * r.head_dim * eb), wp = (uintptr_t)(p.heads * r.head_dim * eb);
+      const uintptr_t sw = (uintptr_t)(w.dst_stride * eb);
+      const bool in_place = i == j && w.src == w.dst && (rows == 1 || w.src_stride == w.dst_stride);
+      if (!in_place && rows_meet((uintptr_t)w.dst, sw, ww, (uintptr_t)p.src, (uintptr_t)(p.src_stride * eb), wp, rows))
+        return fail(KVPRM_E_INVALID, "%s: dst of tensor %d and src of tensor %d overlap", fn, i, j);
+      if (i < j && rows_meet((uintptr_t)w.dst, sw, ww, (uintptr_t)p.dst, (uintptr_t)(p.dst_stride * eb), wp, rows))
+        return fail(KVPRM_E_INVALID, "%s: dst of tensors %d and %d overlap", fn, i, j);
+    }
   double turn[kMaxRotaryPairs];
   rope_turns(r, turn);
   HIP_TRY(launch_rotary(r, turn, dtype == KVPRM_BF16, rows, positions, parts, num_parts, transpose != 0,
