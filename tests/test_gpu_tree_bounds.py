@@ -158,3 +158,54 @@ def test_tree_padded_rows(cdt, n):
     c.o.fill_(7.0)
     padded = c.run(tree=c.tree(num_rows=c.rows + 6000))
     assert bool((got == padded).all())
+
+
+@pytest.mark.parametrize("cdt,dtype,eps", [("bf16", "bf16", 2.0 ** -16), ("bf16", "f32", 2.0 ** -16), ("f32", "bf16", 2.0 ** -16),
+                                           ("f32", "f32", 2.0 ** -16), ("fp8", "bf16", 2.0 ** -11)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("masked", ["tree", "any"])
+def test_tree_weights(cdt, dtype, eps, d, masked):
+    """The weights' bits on a batch that fills the chip."""
+    _say("weights", cdt, dtype, d, masked)
+    _check_rows(Case(cdt, dtype, 8, 2, d, *_sizes(60), seed=d + 5, masked=masked), eps)
+
+
+@pytest.mark.parametrize("cdt,dtype", [("bf16", "bf16"), ("fp8", "bf16"), ("fp8", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [3, 8])
+def test_tree_weights_of_few_columns(cdt, dtype, d, n):
+    """Up to 32 columns: 16 bits whatever the cache."""
+    _say("weights of few columns", cdt, dtype, d, n)
+    _check_rows(Case(cdt, dtype, 8, 2, d, [700, 0, 33, 5000], [n, n, 1, n], seed=d + n), 2.0 ** -16)
+
+
+@pytest.mark.parametrize("cdt,dtype,eps", [("bf16", "bf16", 2.0 ** -16), ("fp8", "bf16", 2.0 ** -11), ("f32", "f32", 2.0 ** -16)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("counts", [None, 3])
+def test_tree_rising_scores(cdt, dtype, eps, d, counts):
+    """Scores that rise along the cache to several hundred, the largest among the last drafted keys: the running
+    maximum moves again and again."""
+    if cdt == "fp8" and counts:
+        eps = 2.0 ** -16
+    _say("rising scores", cdt, dtype, d, counts)
+    nq, nkv = 8, 2
+    sizes = _sizes(60) if counts is None else ([700, 0, 3000], [counts] * 3)
+    c = Case(cdt, dtype, nq, nkv, d, *sizes, seed=d + 6, masked="chain")
+    c.qkv[:, :nq * d] = c.qkv[:, :nq * d] + 3.0
+    rng = np.random.default_rng(d)
+    for b, n in enumerate(c.lengths):
+        for p in range(-(-n // 16)):
+            t = np.minimum(np.arange(16 * p, 16 * p + 16), n)
+            x = (t[:, None] / max(n, 1) * 9 + rng.normal(size=(16, d)) * 0.1).astype(np.float32)
+            page = c.table[b, p]
+            if cdt == "fp8":
+                c.scale[0][:, page] = 0.03125
+                x = gc.to_e4m3(x.astype(np.float64) * 32)
+            else:
+                x = gc.to_bf16(x) if cdt == "bf16" else x.view(np.uint32)
+            c.tok[0][:, page, :, :min(16, n - 16 * p)] = x[:min(16, n - 16 * p)]
+        m = c.counts[b]
+        for t in range(m):
+            c.qkv[c.start[b] + t, nq * d:(nq + nkv) * d] += 9 + t / 8
+    c.upload()
+    _check_rows(c, eps, scores=60)
