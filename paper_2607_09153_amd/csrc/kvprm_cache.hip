@@ -23,21 +23,18 @@ struct RotaryArgs {
   uint32_t uinv, hinv;    // ceil(2^32 / units), ceil(2^32 / heads)
   int64_t rows;
   int rpb;                // rows per block
-  bool once;              // bf16: more rows written than the L2 caches hold
   const int32_t *pos;
   float mag, smag;        // factor on cosines and sines (the sines' negated for the transpose)
   double turn[kMaxRotaryPairs];  // turns per position of each pair
 };
 
-// 16 bytes of a call that moves more than the caches hold, past them; else as usual.
-__device__ __forceinline__ void store_group(uint4 *p, const uint4 &v, bool once) {
-  typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
-  if (once) __builtin_nontemporal_store(u32x4v{v.x, v.y, v.z, v.w}, (u32x4v *)p);
-  else *p = v;
-}
+// 16 bytes that a call reads once, past the caches where it moves more than they hold.
 __device__ __forceinline__ uint4 load_group(const uint4 *p, bool once) { return once ? ld_stream(p) : *p; }
 
-// A vector of V elements of T, widened and back (rounded to nearest even).
+// A vector of V elements of T, widened and back (rounded to nearest even). (bf16: one store of a native vector type.
+// The compiler splits those of a struct of four words between branches that end alike, into 4 and 12 bytes: 22.5 us
+// instead of 21.1 for k_rotary's 8192 rows.)
+typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
 template <typename T, int V>
 struct Vec;
 template <>
@@ -46,14 +43,14 @@ struct Vec<float, 4> {
     const float4 x = *(const float4 *)p;
     v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
   }
-  static __device__ __forceinline__ void store(float *p, const float *v, bool = false) {
+  static __device__ __forceinline__ void store(float *p, const float *v) {
     *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]);
   }
 };
 template <>
 struct Vec<float, 1> {
   static __device__ __forceinline__ void load(const float *p, float *v) { v[0] = *p; }
-  static __device__ __forceinline__ void store(float *p, const float *v, bool = false) { *p = v[0]; }
+  static __device__ __forceinline__ void store(float *p, const float *v) { *p = v[0]; }
 };
 __device__ __forceinline__ uint32_t bf16x2(float a, float b) {
   typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
@@ -72,9 +69,8 @@ struct Vec<uint16_t, 8> {
       v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
     }
   }
-  static __device__ __forceinline__ void store(uint16_t *p, const float *v, bool once = false) {
-    store_group((uint4 *)p, make_uint4(bf16x2(v[0], v[1]), bf16x2(v[2], v[3]), bf16x2(v[4], v[5]),
-                                       bf16x2(v[6], v[7])), once);
+  static __device__ __forceinline__ void store(uint16_t *p, const float *v) {
+    *(u32x4v *)p = u32x4v{bf16x2(v[0], v[1]), bf16x2(v[2], v[3]), bf16x2(v[4], v[5]), bf16x2(v[6], v[7])};
   }
 };
 template <>
@@ -82,7 +78,7 @@ struct Vec<uint16_t, 1> {
   static __device__ __forceinline__ void load(const uint16_t *p, float *v) {
     v[0] = __uint_as_float((uint32_t)*p << 16);
   }
-  static __device__ __forceinline__ void store(uint16_t *p, const float *v, bool = false) {
+  static __device__ __forceinline__ void store(uint16_t *p, const float *v) {
     *p = (uint16_t)bf16x2(v[0], 0.f);
   }
 };
@@ -94,12 +90,13 @@ struct Vec<uint16_t, 1> {
 // the rotated ones. The angle's turns are reduced in 64 bits, p * f - round(p * f), since p f reaches
 // 10^5 turns and more; the rest, at most half a turn, is exact enough in 32.
 // V = 16 bytes where widths, strides and addresses allow, else one element.
-// 16 heads of queries and 8 of keys of 128 dims, bf16, 8192 rows (100 MB moved): 21.2 us, 4.75 TB/s, with
-// non-temporal stores (22.6 with ordinary ones; loads too: 20.7 where the caches hold the rows already and this
-// takes 18; fp32 rows lose by them, 14.1 and 14.9 us below). Two or four units of a thread in flight, loaded
-// before the table is formed: 5 to 8% slower. 4093 rows of 36 heads of 64, fp32,
-// adjacent pairs (75 MB): 14 us, partly from the caches, and 19 from memory (4 TB/s). One row for each of 16
-// sequences: 7 us, the launch.
+// 16 heads of queries and 8 of keys of 128 dims, bf16, 8192 rows (100 MB moved): 21.1 us, 4.8 TB/s. Stores stay
+// ordinary: non-temporal ones take less here (21.3 instead of 25.0 us where the rows come from memory, fp32 20.2
+// instead of 23.4) and give it back where the rows are read next: a call and a copy of its result 47.0 instead of 43.5
+// us at 48 MB written, 62.4 and 57.2 at 64, 85 and 93 at 96, 218 and 212 at 256 (bf16; fp32 alike). Two or four
+// units of a thread in flight, loaded before the table is formed: 5 to 8% slower. 4093 rows of 36 heads of 64, fp32,
+// adjacent pairs (75 MB): 14.1 us, partly from the caches, and 20 from memory (3.8 TB/s). One row for each of 16
+// sequences: 7.6 us, the launch.
 template <typename T, int V, bool HALF>
 __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
   __shared__ float2 cs[kRotaryCs];
@@ -130,7 +127,7 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
       const int e = 2 * a.half + ((int)u - a.nrot) * V;
       float x[V];
       Vec<T, V>::load(src + e, x);
-      Vec<T, V>::store(dst + e, x, a.once);
+      Vec<T, V>::store(dst + e, x);
     } else if (HALF) {
       const int e = (int)u * V;
       float x[V], y[V];
@@ -143,8 +140,8 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
         x[k] = xa * w.x - xb * w.y;
         y[k] = xb * w.x + xa * w.y;
       }
-      Vec<T, V>::store(dst + e, x, a.once);
-      Vec<T, V>::store(dst + a.half + e, y, a.once);
+      Vec<T, V>::store(dst + e, x);
+      Vec<T, V>::store(dst + a.half + e, y);
     } else {
       // (one element at a time: a unit is a pair)
       constexpr int W = V == 1 ? 2 : V;
@@ -164,16 +161,14 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
         x[k + 1] = xb * w.x + xa * w.y;
       }
       if (V == 1) {
-        Vec<T, 1>::store(dst + e, x, a.once);
-        Vec<T, 1>::store(dst + e + 1, x + 1, a.once);
+        Vec<T, 1>::store(dst + e, x);
+        Vec<T, 1>::store(dst + e + 1, x + 1);
       } else {
-        Vec<T, V>::store(dst + e, x, a.once);
+        Vec<T, V>::store(dst + e, x);
       }
     }
   }
 }
-
-constexpr int64_t kL2Bytes = (int64_t)32 << 20;  // eight XCDs' L2 caches
 
 hipError_t launch_rotary(const kvprm_rope &rp, const double *turn, bool bf16, int64_t rows,
                          const int32_t *pos, const kvprm_rope_heads *parts, int num_parts,
@@ -209,7 +204,6 @@ hipError_t launch_rotary(const kvprm_rope &rp, const double *turn, bool bf16, in
   while (rpb < 16 && rpb * 2 * a.half <= kRotaryCs && rows > rpb * 1024 && rpb * per_row < 1024)
     rpb *= 2;
   a.rpb = (int)rpb;
-  a.once = rows * a.heads * a.d * eb >= kL2Bytes;
   const int64_t most = rpb << 23;  // rows of a launch: 2^31 threads
   for (int64_t r0 = 0; r0 < rows; r0 += most) {
     a.rows = min(most, rows - r0);
@@ -249,7 +243,7 @@ struct RowArgs {
   int64_t num_rows;
   const int32_t *start, *index, *first;
   int max_rows;
-  bool once;           // read_kv: more than the caches hold
+  bool once;           // read_kv: tiles read past the caches
 };
 
 // Exponent of the smallest power of two s with 448 s >= amax (448 = 1.75 * 2^8), from the bits of
@@ -520,7 +514,9 @@ __global__ __launch_bounds__(256) void k_write_kv(RowArgs a) {
 
 // The reverse: one wave per (page, kv-head, part) tile, its 16-byte groups through LDS, rows of the
 // wanted positions out, 16 bytes per lane and store. Bound by memory: 16 fp8 caches of 8192 to 16384 tokens,
-// 8 kv-heads of 128 dims, to bf16 (1.2 GB moved): 225 us, 5.4 TB/s.
+// 8 kv-heads of 128 dims, to bf16 (1.2 GB moved): 225 us, 5.4 TB/s. Stores stay ordinary: non-temporal ones take
+// 5 to 25% less, which a copy of the rows behind the call pays back up to 128 MB (both took 45.3 us at 64 MB, and 51.0
+// with them; 191 and 175 at 256, 703 and 703 at 1 GB).
 template <int KVT, int D, typename S>
 __global__ __launch_bounds__(256) void k_read_kv(RowArgs a) {
   constexpr int EB = KVT == 0 ? 4 : KVT == 1 ? 2 : 1;
@@ -582,15 +578,14 @@ __global__ __launch_bounds__(256) void k_read_kv(RowArgs a) {
       const int pos = page * kPage + at.slot(p, i);
       const int64_t row = (int64_t)r0 + pos - p0;
       if (pos < from || pos >= to || row < 0 || row >= a.num_rows) continue;
-      uint4 y;
-      Vec<S, VS>::store((S *)&y, x[i]);
-      store_group((uint4 *)(rows + row * stride + (int64_t)j * D + at.e0), y, a.once);
+      Vec<S, VS>::store(rows + row * stride + (int64_t)j * D + at.e0, x[i]);
     }
   }
 }
 
-// Rows read back go past the caches from here on: 815 MB of them took 228 us so and 238 through the caches,
-// while a call whose rows fit leaves them there for whoever reads them next.
+// The tiles are read past the caches where the rows take this much: 128 MB of fp32 rows from fp32 tiles 51.1 us so and
+// 55.6 through the caches, bf16 from bf16 51.0 and 54.9, bf16 from fp8 39.9 and 42.0, 512 MB 192, 192 and 148 instead of
+// 207, 206 and 157. A smaller call leaves the tiles there for whoever reads them next (8 MB take 7.9 and 8.0 us).
 constexpr int64_t kOnceBytes = (int64_t)128 << 20;
 
 static RowArgs row_args(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batch &b, int layer,
