@@ -305,7 +305,8 @@ kvprm_status kvprm_score_grad(kvprm_handle h, const kvprm_kv_cache *cache,
 /* KV Steering (appendix algorithm): `steps` times, every cached key and value the candidates
  * read (slots 0..L_b-1) becomes round_bf16(kv - eta * d(-log P(+))/d kv), the gradient taken at
  * the cache as it is at that step. The pools of `cache` are WRITTEN in place. scores_before[b]
- * = P(+) before the first step, scores_after[b] = P(+) after the last (device fp32 [B]). Requirements as for kvprm_score_grad; steps >= 1. */
+ * = P(+) before the first step, scores_after[b] = P(+) after the last (device fp32 [B]).
+ * Requirements as for kvprm_score_grad; steps >= 1. */
 kvprm_status kvprm_steer(kvprm_handle h, const kvprm_kv_cache *cache, const kvprm_batch *batch,
                          const kvprm_readout_weights *weights, float eta, int32_t steps,
                          void *workspace, size_t ws_bytes, float *scores_before,
@@ -390,10 +391,11 @@ typedef struct {
  * tensors of `rows` rows, p = positions[row] (device int32, any value): pair (a, b) becomes
  * (a cos - b sin, b cos + a sin) with angle p f_i. transpose != 0 applies magnitude * R^T, the
  * gradient of the rotation (sines negated). Angles are formed in 64 bits, products in 32, each
- * result is rounded once. A tensor's dst may be its src (same stride); otherwise no row written may share a byte
- * with a row read or written of either tensor (rows side by side in one buffer, of equal strides, do not).
- * KVPRM_E_INVALID: a null or misaligned pointer (element size), a stride below the row, rows that overlap,
- * or rows of unequal strides between each other, values outside the ranges above. rows = 0 does nothing. */
+ * result is rounded once. A tensor's dst may be its src (same stride); otherwise no row written
+ * may share a byte with a row read or written of either tensor (rows side by side in one buffer,
+ * of equal strides, do not). KVPRM_E_INVALID: a null or misaligned pointer (element size), a stride
+ * below the row, rows that overlap or that lie between each other with unequal strides, values
+ * outside the ranges above. rows = 0 does nothing. */
 kvprm_status kvprm_rotary(const kvprm_rope *rope, kvprm_dtype dtype, int64_t rows,
                           const int32_t *positions, const kvprm_rope_heads *parts,
                           int32_t num_parts, int32_t transpose, void *stream);
@@ -455,9 +457,9 @@ typedef struct {
   int32_t mask_words;         /* >= ceil(max_rows / 32) with a mask */
 } kvprm_tree;
 
-/* Bytes of device workspace that serve kvprm_attention_tree for this call and every one of at most this
- * batch's size and max_pages and this tree's num_rows and max_rows, with the same dtype (on which alone it
- * depends). */
+/* Bytes of device workspace that serve kvprm_attention_tree for this call and every one of the
+ * same dtype with at most this batch's size and max_pages and this tree's num_rows and max_rows
+ * (the size depends on these alone). */
 kvprm_status kvprm_workspace_size_tree(kvprm_handle h, const kvprm_batch *batch,
                                        const kvprm_tree *tree, size_t *bytes);
 
@@ -465,13 +467,16 @@ kvprm_status kvprm_workspace_size_tree(kvprm_handle h, const kvprm_batch *batch,
  * o = softmax(q K^T / sqrt(d_h)) V over the candidate's lengths[b] cached tokens and the drafted
  * tokens of its mask. A token that attends to nothing gets zeros. Keys and values that a token
  * does not attend to never reach its output, whatever they hold (infinities, NaN); infinities
- * that it attends to reach it as they are, cached or drafted, unless their weight underflows. Scores, the softmax and the
- * sums are fp32 (weights of at most 1: only values above 2^127 / the tokens they are summed over could overflow); F32 rows keep 24 bits of q and of the probabilities, BF16 rows 16 bits of the
- * probabilities. Over fp8 caches, where max_rows times the q-heads of a kv-head exceeds 32 and the batch fills the
- * chip, those of cached tokens keep 11 bits down to 2^-19 of a row's largest, and have an error of at most 2^-30 of it
- * below; pages whose value scale lies more than 2^80 below the candidate's largest lose bits. fp8 scales must not be negative. The cache is not written. o must not overlap q, k or v.
- * Rows that no candidate owns are left as they are.
- * Conventions as for kvprm_attention; the prefix-sharing hint is not read. */
+ * that it attends to reach it as they are, cached or drafted, unless their weight underflows.
+ * Scores, the softmax and the sums are fp32, of weights of at most 1: values above 2^127 / (the
+ * tokens summed over) may overflow. F32 rows keep 24 bits of q and of the probabilities, BF16 rows
+ * 16 bits of the probabilities. Over fp8 caches, where max_rows times the q-heads of a kv-head
+ * exceeds 32 and the batch fills the chip (so that other candidates matter), those of cached
+ * tokens keep 11 bits down to 2^-19 of a row's largest and have an error of at most 2^-30 of it
+ * below, and pages whose value scale lies more than 2^80 below the candidate's largest lose bits.
+ * fp8 scales must not be negative. The cache is not written. o must not overlap q, k or v. Rows
+ * that no candidate owns are left as they are. Conventions as for kvprm_attention; the
+ * prefix-sharing hint is not read. */
 kvprm_status kvprm_attention_tree(kvprm_handle h, const kvprm_kv_cache *cache,
                                   const kvprm_batch *batch, int32_t layer, const kvprm_tree *tree,
                                   void *workspace, size_t ws_bytes, void *stream);

@@ -1015,7 +1015,7 @@ static kvprm_status check_tree(const kvprm_handle h, const kvprm_batch *b, const
   if (t->max_rows > kMaxTreeRows)
     return fail(KVPRM_E_UNSUPPORTED, "%s: at most %d drafted tokens per candidate", fn, kMaxTreeRows);
   if (t->num_rows > INT32_MAX) return fail(KVPRM_E_UNSUPPORTED, "%s: at most 2^31 - 1 rows", fn);
-  if ((int64_t)b->batch * h->dm.nkv > 65535)  // (the launch grid's third side)
+  if ((int64_t)b->batch * h->dm.nkv > 65535)  // (keeps the launch below 2^32 threads)
     return fail(KVPRM_E_UNSUPPORTED, "%s: at most 65535 kv-heads over the batch", fn);
   return KVPRM_OK;
 }

@@ -663,11 +663,10 @@ __device__ __forceinline__ uint32_t fp8x2_to_half2(uint32_t word) {  // (every e
 // (8 slots 4 h.., 8 + 4 h.. of one page are one operand). bf16 caches: P in two bf16 terms (16 bits; one
 // term would add an error the size of the result's own rounding). fp8 caches: keys widened to bf16, values to
 // fp16, exactly, and P in fp16 (11 bits), half the products: 8 caches of 16384 to 32768 tokens, 4 kv-heads of
-// 128 dims, 64 drafted tokens of 7 query heads each: 264 us, 700 TFLOP/s, and 285 in two bf16 terms before
-// later steps; from bf16 caches 330 us, 560 TFLOP/s (fp16 values from those too, with an exponent per tile: 357
-// and more). Drafted values stay bf16 over fp8 caches too (two-term weights): as fp16 they would need an exponent
-// that all of them share, and the largest of them would push others out of fp16's range, those also that a token
-// sees without seeing the largest.
+// 128 dims, 64 drafted tokens of 7 query heads each: 273 us, 675 TFLOP/s; from bf16 caches 330 us, 560 TFLOP/s (fp16
+// values from those too, with an exponent per tile: 357 and more). Drafted values stay bf16 over fp8 caches too (two-
+// term weights): as fp16 they would need an exponent that all of them share, and the largest of them would push others
+// out of fp16's range, those also that a token sees without seeing the largest.
 // Bound by vector instructions (about 115 a stage and wave at D = 128, bf16, 160 at D = 64, fp8, beside 24 and 8
 // products) and by how far the two or three waves of a SIMD overlap them with products: a ring of four stages
 // with half the barriers, wave priorities and waves in two groups taking turns all measured the same.
@@ -1284,21 +1283,27 @@ static int64_t draft_rows(const kvprm_batch &b, const kvprm_tree &t) {
 }
 static int draft_extra(const TreePlan &p, int n) { return (n + p.draft_tokens - 1) / p.draft_tokens * p.draft_pages; }
 
-// Kernel by the longest draft's columns where the chip is full (launch_tree has the rule for fewer blocks): k_tree
-// up to 32, which a wave holds at once. At 17 to 32 columns it took 13.7 us where k_tree_wide took 16.5 (1103
-// tokens, 32 columns), 25.7 and 29.6 (24 fp8 caches of 4800, 32 columns), 91 and 88 (8 caches of 16384 to 32768,
-// 28 columns); at 33 to 64, where it reads the pages twice, 42.9 and 33.9 (the 24 caches, 48 columns), 108 and 96
-// (the 8, 56 columns).
-// Chunks leave as many blocks as are resident at once: two of k_tree_wide on a compute unit (three at
-// d_h = 64), two of k_tree. Fewer or more both lose (k_tree_wide, 24 ragged fp8 caches, d_h = 64: 56 us at 680
-// blocks, 54 at 768, 61 at 1024; 8 long bf16 caches, d_h = 128: 403 us at 400, 330 at 512, 394 at 600). Column
-// blocks are counted by the average draft, draft_rows / batch, since a candidate's missing ones are no
-// blocks. A k_tree_wide chunk has 16 pages or more: 1200 tokens of 24 candidates take 24 us with least chunks
-// of 8 or 16, 28 with 32. Drafted tokens count as pages of the last chunk (4 for 32 tokens of
-// k_tree_wide, a unit for 64 of k_tree): 13.6 us instead of 15.6 for 1103 tokens, 338 instead of 344 on the long
-// caches; 2 to 16 pages differ by less than 2%. Chunk slots: what fills the chip eight times over if the
-// batch's candidates were all as long as the table.
+// Blocks that fill the chip (see tree_plan).
 static int full_chip(const Dims &dm, bool wide) { return wide && dm.d == 64 ? 768 : 512; }
+
+// Kernel by the longest draft's columns where the chip is full (launch_tree has the rule for fewer blocks): k_tree
+// up to 32, which a wave holds at once, else k_tree_wide. At 17 to 32 columns k_tree took 13.9 us and k_tree_wide 16.6
+// (1103 tokens, 32 columns; 12.0 in blocks of 16), 25.5 and 30.2 (24 fp8 caches of 4800, 32 columns), 91.0 and 88.6 (8
+// caches of 16384 to 32768, 28 columns); at 33 to 64, where k_tree reads the pages twice, 42.1 and 34.2 (the 24 caches,
+// 48 columns), 108 and 95 (the 8, 56 columns). Left at 32 columns: 16 x 4000 bf16 tokens, 67.4 us, would take 62.6 in
+// k_tree_wide.
+// Chunks leave as many blocks as the chip takes: two of k_tree_wide on a compute unit (three at d_h = 64), which are
+// resident at once. Fewer or more both lose: 24 ragged fp8 caches, d_h = 64, 52.0 us at 680 blocks, 49.6 at 768, 58.2
+// at 1024; 8 long bf16 caches, d_h = 128, 402 us at 400, 332 at 512, 399 at 600. Two of k_tree as well; they are
+// resident at once but for 32 columns at d_h = 128 and fp32 rows over bf16 caches there, whose registers leave room for
+// one block: 256, 512 and 1024 blocks take 29.2, 25.5 and 29.9 us (24 fp8 caches of 4800, 32 columns, d_h = 64), 91.3,
+// 90.8 and 108 (8 long bf16 caches, 28 columns, d_h = 128), 68.2, 76.8 and 96.8 (16 x 4096 bf16 tokens, 112
+// columns, d_h = 128, which k_tree_wide takes). Column blocks are counted by the average draft, draft_rows / batch,
+// since a candidate's missing ones are no blocks. A k_tree_wide chunk has 16 pages or more: 24 x 1200 tokens, 96
+// columns, take 25.2, 23.8 and 26.9 us with least chunks of 8, 16 and 32 pages. Drafted tokens count as pages of the
+// last chunk (4 for 32 tokens of k_tree_wide, a unit for 64 of k_tree): 12.1 us instead of 13.9 for 1103 tokens, 326
+// instead of 330 on the long caches; 2 to 8 pages are alike there. Chunk slots: what fills the chip eight times over if
+// the batch's candidates were all as long as the table.
 static TreePlan tree_plan(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t, bool wide) {
   TreePlan p;
   const int cols = t.max_rows * dm.g;
@@ -1396,10 +1401,10 @@ hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batc
   int64_t items = 0;  // chunks of all candidates
   for (int i = 0; i < b.batch; ++i) items += chunks_of(i);
   // Blocks of 16 columns (short chains, pages read once per block from the caches) while they leave the chip's
-  // waves unfilled. Instead of 32 columns, up to 768 blocks: 1103 tokens, 32 columns (160 blocks) 14.0 -> 12.2 us,
-  // 2 x 2500 (672 blocks) 24.8 -> 21.3, but 16 x 4000 (1024 blocks) 67.7 -> 73.4. Instead of k_tree_wide, up to
-  // 512: 1103 tokens, 64 columns (320 blocks) 17.7 -> 14.7, 300 tokens, 128 columns (256) 19.1 -> 13.0, 4 x 700
-  // fp8 tokens, 64 columns 16.4 -> 10.9, but 2500 tokens, 64 columns (over 512) 18.7 -> 21.0.
+  // waves unfilled. Instead of 32 columns, up to 768 blocks: 1103 tokens, 32 columns (160 blocks) 13.9 -> 12.0 us,
+  // 2 x 2500 (672 blocks) 25.0 -> 21.5, but 16 x 4000 (1024 blocks) 67.4 -> 73.4. Instead of k_tree_wide, up to
+  // 512: 1103 tokens, 64 columns (320 blocks) 17.7 -> 14.6, 300 tokens, 128 columns (256) 19.3 -> 12.8, 4 x 700
+  // fp8 tokens, 64 columns 16.1 -> 10.5, but 2500 tokens, 64 columns (over 512) 18.9 -> 20.9.
   const int64_t blocks16 = items * dm.nkv * ((t.max_rows * dm.g + 15) / 16);
   if (may_be_wide(dm, t) && blocks16 > 512) {
     p = tree_plan(dm, b, t, true);
