@@ -466,8 +466,9 @@ kvprm_status kvprm_workspace_size_tree(kvprm_handle h, const kvprm_batch *batch,
 /* Attention of drafted tokens over the cache of one layer: for every drafted token and q-head,
  * o = softmax(q K^T / sqrt(d_h)) V over the candidate's lengths[b] cached tokens and the drafted
  * tokens of its mask. A token that attends to nothing gets zeros. Keys and values that a token
- * does not attend to never reach its output, whatever they hold (infinities, NaN); infinities
- * that it attends to reach it as they are, cached or drafted, unless their weight underflows.
+ * does not attend to never reach its output, whatever they hold (infinities, NaN); infinite values
+ * that it attends to reach it as they are, cached or drafted, unless their weight underflows. A
+ * score of -infinity is a weight of 0 (F32 rows over infinite keys of a bf16 cache: NaN).
  * Scores, the softmax and the sums are fp32, of weights of at most 1: values above 2^127 / (the
  * tokens summed over) may overflow. F32 rows keep 24 bits of q and of the probabilities, BF16 rows
  * 16 bits of the probabilities. Over fp8 caches, where max_rows times the q-heads of a kv-head
