@@ -10,8 +10,8 @@
  *
  * Conventions for every entry point
  *   - All tensor pointers are DEVICE pointers unless the name ends in _host. The caller owns
- *     every buffer; the library never frees, never writes the cache (except kvprm_steer and
- *     kvprm_write_kv, which exist to update it), the page table or the weights, and never
+ *     every buffer; the library never frees, never writes the cache (except kvprm_steer,
+ *     kvprm_write_kv and the calls on its pages, which exist to update it), the page table or the weights, and never
  *     allocates device memory in any call (the caller passes a workspace sized by the matching
  *     kvprm_workspace_size* query), so every call but kvprm_create can be captured in a HIP
  *     graph (no memset nodes either; not in the KVPRM_DEBUG mode below, which synchronises).
@@ -57,11 +57,12 @@ typedef enum {
   KVPRM_E_INTERNAL = 5
 } kvprm_status;
 
-typedef enum { KVPRM_F32 = 0, KVPRM_BF16 = 1, KVPRM_FP8_E4M3 = 2 } kvprm_dtype;
+typedef enum { KVPRM_F32 = 0, KVPRM_BF16 = 1, KVPRM_FP8_E4M3 = 2, KVPRM_FP4_E2M1 = 3 } kvprm_dtype;
 
 /* Model shape. Supported: head_dim in {64, 128}; page_size == 16; num_q_heads a multiple of
- * num_kv_heads; weight_dtype F32 with kv_dtype F32, or weight_dtype BF16 with kv_dtype BF16 or
- * FP8_E4M3 (OCP E4M3FN: bias 7, max 448, no infinities). */
+ * num_kv_heads; weight_dtype F32 with kv_dtype F32, or weight_dtype BF16 with kv_dtype BF16,
+ * FP8_E4M3 (OCP E4M3FN: bias 7, max 448, no infinities) or FP4_E2M1 (OCP MXFP4: 4-bit codes with a scale for
+ * every 32 dims of a token). */
 typedef struct {
   int32_t num_layers;   /* N_L */
   int32_t hidden;       /* H, a multiple of 64 */
@@ -112,7 +113,15 @@ typedef struct {
  *            ((((m / (16 r)) * 4 + s / 4) * 16 + m % 16) * r + (m / 16) % r) * 4 + s % 4
  *            (each 16 bytes hold 4 consecutive slots of r dimensions 16 apart)
  * For FP8_E4M3 pools the stored code is multiplied by a per-(layer, page, kv-head) fp32 scale:
- *   k_scale, v_scale: [num_layers][num_pages][num_kv_heads]; NULL for other dtypes. */
+ *   k_scale, v_scale: [num_layers][num_pages][num_kv_heads]; NULL for other dtypes.
+ * FP4_E2M1 pools hold codes and scales in the tile, 8 d_h + d_h / 2 bytes (pools 16-byte aligned; 4.25 bits a value;
+ * written by kvprm_write_kv). A code (bit 3 the sign, then 0, 0.5, 1, 1.5, 2, 3, 4, 6) is multiplied by its scale, the
+ * power of two with the biased exponent byte e: 2^(e - 127), e = 0 .. 252; 255 makes the 32 values NaN (253 and
+ * 254: codes whose product passes fp32 become infinities).
+ *   K tile: the code of (slot s, dim m) in nibble m % 2 (0: the low one) of byte ((m / 32) * 16 + s) * 16 + m % 32 / 2,
+ *           its scale in byte 8 d_h + (m / 32) * 16 + s
+ *   V tile: nibble (m / 16) % 2 of byte ((s / 4) * 16 + m % 16) * (d_h / 8) + (m / 32) * 4 + s % 4, its scale in byte
+ *           8 d_h + (s / 4) * (d_h / 8) + (m / 32) * 4 + s % 4 */
 typedef struct {
   const void *k_pages;
   const void *v_pages;
@@ -334,7 +343,7 @@ typedef enum { KVPRM_KEYS = 0, KVPRM_VALUES = 1 } kvprm_kv_part;
  *      kvprm_kv_cache, in the same tile order (fp8 per-tile scales therefore keep their order
  *      and are not touched).
  * The bytes are moved unchanged (slots past a sequence's end may hold anything, NaN included).
- * dtype F32, BF16 or FP8_E4M3; head_dim 64 or 128 (KVPRM_E_UNSUPPORTED otherwise); src and dst
+ * dtype F32, BF16 or FP8_E4M3 (FP4_E2M1: KVPRM_E_UNSUPPORTED); head_dim 64 or 128 (KVPRM_E_UNSUPPORTED otherwise); src and dst
  * device pointers, 16-byte aligned, not overlapping (KVPRM_E_INVALID otherwise); num_tiles = 0
  * does nothing. Nothing is allocated; enqueued on `stream`. */
 kvprm_status kvprm_pack_kv(const void *src, void *dst, int64_t num_tiles, int32_t head_dim,
@@ -423,6 +432,10 @@ typedef struct {
  * to 2^126). A power of two
  * costs no significant bit on either way, so that a code is rounded again only where it leaves e4m3's
  * normal range. Infinities and NaN are stored as NaN in fp8 (and do not enter the scale).
+ * FP4_E2M1: the scale of 32 dims of a token is the smallest power of two s with 7 s >= |x| for all of them, 2^-100 to
+ * 2^125 (error at most s; a smaller s would not lower it, since codes 4 and 6 lie 2 s apart), codes to the nearest, ties to
+ * even. A token's bytes depend on it alone and are never changed by later ones. 32 dims that hold an
+ * infinity or NaN are stored as code 0 with scale byte 255: NaN, all of them.
  * Rows past max_pages * 16 tokens, with a row number outside [0, num_rows) or whose page id is outside
  * [0, num_pages) are dropped. No page may get rows of two candidates (checked with KVPRM_DEBUG=1).
  * The prefix-sharing hint is not read. */
@@ -430,8 +443,8 @@ kvprm_status kvprm_write_kv(kvprm_handle h, const kvprm_kv_cache *cache, const k
                             int32_t layer, const kvprm_kv_rows *rows, void *stream);
 
 /* Reads cached tokens of one layer back: row i of candidate b receives the key and value at
- * position first[b] + i (first: device [B], or NULL for 0), code times scale for fp8, rounded to
- * the rows' type. Rows of positions outside [0, lengths[b]), rows past max_rows or num_rows and rows
+ * position first[b] + i (first: device [B], or NULL for 0), code times scale for fp8 and 4 bits, rounded to
+ * the rows' type (4 bits: exact). Rows of positions outside [0, lengths[b]), rows past max_rows or num_rows and rows
  * that no candidate owns are left as they are. index must be NULL (KVPRM_E_INVALID). k or v may be
  * NULL (that part is not read). The prefix-sharing hint is not read. */
 kvprm_status kvprm_read_kv(kvprm_handle h, const kvprm_kv_cache *cache, const kvprm_batch *batch,
@@ -475,12 +488,67 @@ kvprm_status kvprm_workspace_size_tree(kvprm_handle h, const kvprm_batch *batch,
  * exceeds 32 and the batch fills the chip (so that other candidates matter), those of cached
  * tokens keep 11 bits down to 2^-19 of a row's largest and have an error of at most 2^-30 of it
  * below, and pages whose value scale lies more than 2^80 below the candidate's largest lose bits.
- * fp8 scales must not be negative. The cache is not written. o must not overlap q, k or v. Rows
+ * fp8 scales must not be negative. Over 4-bit caches the products take the stored values, which bf16 holds exactly; a
+ * token stored as NaN makes the outputs that attend to it NaN. The cache is not written. o must not overlap q, k or v. Rows
  * that no candidate owns are left as they are. Conventions as for kvprm_attention; the
  * prefix-sharing hint is not read. */
 kvprm_status kvprm_attention_tree(kvprm_handle h, const kvprm_kv_cache *cache,
                                   const kvprm_batch *batch, int32_t layer, const kvprm_tree *tree,
                                   void *workspace, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------- pages of the cache
+ * A generator that keeps several continuations of one text holds their common pages once. The calls below keep the
+ * tables of such a cache on the device, with a count of holders per page, so that a beam can be scored, pruned and
+ * forked without a host round trip. They work on caches of every type; a pool has at most 2^22 pages. */
+
+/* Rows of a page table and what they hold. Row i holds the pages of its first held[i] entries (a page that
+ * stands in several rows is shared; one that stands in one row twice is held twice); the other entries may be
+ * anything. */
+typedef struct {
+  int32_t rows;        /* 0 to 256 */
+  int32_t max_pages;   /* entries of a row, 1 to 2^20 */
+  int32_t *page_table; /* device [rows][max_pages] */
+  int32_t *lengths;    /* device [rows]: cached tokens, 0 to 16 held[i] */
+  int32_t *held;       /* device [rows]: 0 to max_pages */
+} kvprm_page_rows;
+
+/* Bytes of device workspace of kvprm_fork_pages and kvprm_compact_pages for a pool of num_pages or fewer. */
+kvprm_status kvprm_workspace_size_pages(kvprm_handle h, int32_t num_pages, size_t *bytes);
+
+/* Replaces the rows of `from` by those of `to`: new row i continues row parent[i] of `from` (any number of times;
+ * a row without a child ends here), or is an empty one (parent[i] < 0). It has its parent's tokens and holds
+ * ceil((length + room[i]) / 16) pages (room: device [to->rows], >= 0, or NULL for 0):
+ *   - its parent's full pages are shared;
+ *   - a page that the parent has partly filled goes to the parent's first child (the lowest i) if no other row holds
+ *     it (refs 1); every other child gets a copy of it, in all layers, keys and values (and fp8 scales), so that rows
+ *     can be appended to each;
+ *   - the copy and the pages for room are fresh ones: pages that nobody holds after the call's own releases, and that
+ *     are not copied in this call, by ascending id in the order of new rows and their entries. What they held before
+ *     is not cleared.
+ * refs (device [num_pages]): holders of every page before the call, those outside `from` counted too; new_refs
+ * receives them after it (pages with 0 are free). Entries of `to` past held are -1.
+ * result (device [4]) receives {status, fresh pages needed, pages there were for them, pages free afterwards}.
+ * Status 0: done. 1: too few free pages. 2: inconsistent: a parent >= from->rows, a negative room, a held or a parent's
+ * length outside its range, an entry outside [0, num_pages), a page with fewer refs than holders, a new row of more than
+ * to->max_pages pages. With status 1 or 2 nothing but `result` is written ({1, needed, there were, 0}, {2, 0, 0, 0}).
+ * `to` and `from`, refs and new_refs and all others must not overlap (KVPRM_E_INVALID). to->rows = 0 frees all rows.
+ * The pools of `cache` are WRITTEN (fresh copies). parent: device [to->rows]. */
+kvprm_status kvprm_fork_pages(kvprm_handle h, const kvprm_kv_cache *cache, const kvprm_page_rows *from,
+                              const kvprm_page_rows *to, const int32_t *parent, const int32_t *room,
+                              const int32_t *refs, int32_t *new_refs, int32_t *result, void *workspace,
+                              size_t ws_bytes, void *stream);
+
+/* Moves the live pages of a pool (refs > 0; M of them) into its first M pages: those at or past M go, in ascending
+ * order, to the free ids below M, in ascending order; the others keep their ids. Keys, values and fp8 scales of all
+ * layers are copied; what the left pages hold stays. moved (device [num_pages]) receives every page's new id (-1: it
+ * was free), new_table (device [rows][max_pages]) the rows' new entries (-1 past held), new_refs the holders.
+ * rows: every table of the pool that is to be rewritten (lengths is not read); tables kept elsewhere follow by `moved`.
+ * result (device [4]) receives {status, M, pages moved, free pages}. Status 2 (nothing else is written, {2, 0, 0,
+ * 0}): a held outside its range, an entry that names no live page, a negative count. Overlap as above. The
+ * pools of `cache` are WRITTEN. */
+kvprm_status kvprm_compact_pages(kvprm_handle h, const kvprm_kv_cache *cache, const kvprm_page_rows *rows,
+                                 int32_t *new_table, const int32_t *refs, int32_t *new_refs, int32_t *moved,
+                                 int32_t *result, void *workspace, size_t ws_bytes, void *stream);
 
 /* Diagnostic (measurement, not part of scoring): read `bytes` of device memory at `buf` once,
  * with the access pattern of the cache and weight streams (16-byte non-temporal loads, 512

@@ -17,8 +17,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libkvprm.so")
 
 KVPRM_OK, KVPRM_E_INVALID, KVPRM_E_UNSUPPORTED, KVPRM_E_WORKSPACE, KVPRM_E_HIP, KVPRM_E_INTERNAL = range(6)
-KVPRM_F32, KVPRM_BF16, KVPRM_FP8_E4M3 = 0, 1, 2
-DTYPE_CODE = {"f32": KVPRM_F32, "bf16": KVPRM_BF16, "fp8": KVPRM_FP8_E4M3}
+KVPRM_F32, KVPRM_BF16, KVPRM_FP8_E4M3, KVPRM_FP4_E2M1 = 0, 1, 2, 3
+DTYPE_CODE = {"f32": KVPRM_F32, "bf16": KVPRM_BF16, "fp8": KVPRM_FP8_E4M3, "fp4": KVPRM_FP4_E2M1}
 
 EXPORTED = ["kvprm_create", "kvprm_destroy", "kvprm_workspace_size", "kvprm_score",
             "kvprm_attention", "kvprm_attention_partials", "kvprm_pack_weight",
@@ -26,7 +26,8 @@ EXPORTED = ["kvprm_create", "kvprm_destroy", "kvprm_workspace_size", "kvprm_scor
             "kvprm_score_ex", "kvprm_workspace_size_grad", "kvprm_score_grad", "kvprm_steer",
             "kvprm_stream_read", "kvprm_score_static", "kvprm_pack_kv", "kvprm_rotary",
             "kvprm_write_kv", "kvprm_read_kv", "kvprm_workspace_size_tree",
-            "kvprm_attention_tree", "kvprm_last_error"]
+            "kvprm_attention_tree", "kvprm_workspace_size_pages", "kvprm_fork_pages",
+            "kvprm_compact_pages", "kvprm_last_error"]
 KVPRM_KEYS, KVPRM_VALUES = 0, 1
 STATIC_WORKSPACE_BYTES = 64 << 20  # KVPRM_STATIC_WORKSPACE_BYTES
 ROPE_LAYOUT = {"half": 0, "interleaved": 1}
@@ -115,6 +116,12 @@ class Tree(ctypes.Structure):
                 ("mask", ctypes.c_void_p), ("mask_words", ctypes.c_int32)]
 
 
+class PageRows(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("page_table", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+                ("held", ctypes.c_void_p)]
+
+
 class KvprmError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"kvprm status {status}: {msg}")
@@ -181,13 +188,19 @@ def _load():
                                               ctypes.POINTER(sz)]
     lib.kvprm_attention_tree.argtypes = [vp, ctypes.POINTER(KVCache), ctypes.POINTER(Batch),
                                          ctypes.c_int32, ctypes.POINTER(Tree), vp, sz, vp]
+    lib.kvprm_workspace_size_pages.argtypes = [vp, ctypes.c_int32, ctypes.POINTER(sz)]
+    lib.kvprm_fork_pages.argtypes = [vp, ctypes.POINTER(KVCache), ctypes.POINTER(PageRows),
+                                     ctypes.POINTER(PageRows), vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.kvprm_compact_pages.argtypes = [vp, ctypes.POINTER(KVCache), ctypes.POINTER(PageRows), vp, vp,
+                                        vp, vp, vp, vp, sz, vp]
     for f in ("kvprm_create", "kvprm_destroy", "kvprm_workspace_size", "kvprm_score",
               "kvprm_attention", "kvprm_attention_partials", "kvprm_pack_weight",
               "kvprm_workspace_size_lora", "kvprm_score_lora", "kvprm_workspace_size_ex",
               "kvprm_score_ex", "kvprm_workspace_size_grad", "kvprm_score_grad", "kvprm_steer",
               "kvprm_stream_read", "kvprm_score_static", "kvprm_pack_kv", "kvprm_rotary",
               "kvprm_write_kv", "kvprm_read_kv", "kvprm_workspace_size_tree",
-              "kvprm_attention_tree"):
+              "kvprm_attention_tree", "kvprm_workspace_size_pages", "kvprm_fork_pages",
+              "kvprm_compact_pages"):
         getattr(lib, f).restype = ctypes.c_int
     lib.kvprm_last_error.argtypes = []
     lib.kvprm_last_error.restype = ctypes.c_char_p
@@ -447,3 +460,30 @@ def kvprm_attention_tree(handle: int, cache: KVCache, batch: Batch, layer: int, 
                          workspace_ptr: int, ws_bytes: int, stream: int = 0) -> None:
     _check(lib.kvprm_attention_tree(handle, ctypes.byref(cache), ctypes.byref(batch), layer,
                                     ctypes.byref(tree), workspace_ptr, ws_bytes, stream or None))
+
+
+def make_page_rows(rows: int, max_pages: int, page_table_ptr: int, lengths_ptr: int, held_ptr: int) -> PageRows:
+    return PageRows(rows, max_pages, page_table_ptr or None, lengths_ptr or None, held_ptr or None)
+
+
+def kvprm_workspace_size_pages(handle: int, num_pages: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib.kvprm_workspace_size_pages(handle, num_pages, ctypes.byref(n)))
+    return n.value
+
+
+def kvprm_fork_pages(handle: int, cache: KVCache, from_rows: PageRows, to_rows: PageRows, parent_ptr: int,
+                     room_ptr: int, refs_ptr: int, new_refs_ptr: int, result_ptr: int, workspace_ptr: int,
+                     ws_bytes: int, stream: int = 0) -> None:
+    """room_ptr 0: no pages beyond the tokens'."""
+    _check(lib.kvprm_fork_pages(handle, ctypes.byref(cache), ctypes.byref(from_rows), ctypes.byref(to_rows),
+                                parent_ptr or None, room_ptr or None, refs_ptr or None, new_refs_ptr or None,
+                                result_ptr or None, workspace_ptr, ws_bytes, stream or None))
+
+
+def kvprm_compact_pages(handle: int, cache: KVCache, rows: PageRows, new_table_ptr: int, refs_ptr: int,
+                        new_refs_ptr: int, moved_ptr: int, result_ptr: int, workspace_ptr: int, ws_bytes: int,
+                        stream: int = 0) -> None:
+    _check(lib.kvprm_compact_pages(handle, ctypes.byref(cache), ctypes.byref(rows), new_table_ptr or None,
+                                   refs_ptr or None, new_refs_ptr or None, moved_ptr or None, result_ptr or None,
+                                   workspace_ptr, ws_bytes, stream or None))

@@ -73,10 +73,12 @@ kvprm_status kvprm_create(const kvprm_model_desc *d, kvprm_handle *out) {
     return fail(KVPRM_E_UNSUPPORTED, "kvprm_create: hidden, ffn_dim, n_q*d_h must be multiples of 64");
   const bool f32 = d->weight_dtype == KVPRM_F32 && d->kv_dtype == KVPRM_F32;
   const bool bf = d->weight_dtype == KVPRM_BF16 &&
-                  (d->kv_dtype == KVPRM_BF16 || d->kv_dtype == KVPRM_FP8_E4M3);
+                  (d->kv_dtype == KVPRM_BF16 || d->kv_dtype == KVPRM_FP8_E4M3 ||
+                   d->kv_dtype == KVPRM_FP4_E2M1);
   if (!f32 && !bf)
     return fail(KVPRM_E_UNSUPPORTED,
-                "kvprm_create: dtype pair must be (F32, F32), (BF16, BF16) or (BF16, FP8_E4M3)");
+                "kvprm_create: dtype pair must be (F32, F32), (BF16, BF16), (BF16, FP8_E4M3) or "
+                "(BF16, FP4_E2M1)");
   kvprm_handle h = new (std::nothrow) kvprm_handle_s;
   if (!h) return fail(KVPRM_E_INTERNAL, "kvprm_create: out of host memory");
   h->desc = *d;
@@ -91,7 +93,7 @@ kvprm_status kvprm_create(const kvprm_model_desc *d, kvprm_handle *out) {
   m.theta = d->rope_theta;
   m.eps = d->rms_eps;
   m.wdt = d->weight_dtype == KVPRM_BF16 ? 1 : 0;
-  m.kvdt = d->kv_dtype == KVPRM_F32 ? 0 : (d->kv_dtype == KVPRM_BF16 ? 1 : 2);
+  m.kvdt = d->kv_dtype == KVPRM_F32 ? 0 : d->kv_dtype == KVPRM_BF16 ? 1 : d->kv_dtype == KVPRM_FP8_E4M3 ? 2 : 3;
   const char *dbg = getenv("KVPRM_DEBUG");
   h->debug = dbg && dbg[0] && strcmp(dbg, "0") != 0;
   *out = h;
@@ -150,6 +152,8 @@ static kvprm_status check_cache(const kvprm_handle h, const kvprm_kv_cache *c, c
   if (c->num_pages < 1) return fail(KVPRM_E_INVALID, "%s: num_pages < 1", fn);
   if (h->dm.kvdt == 2 && (!c->k_scale || !c->v_scale))
     return fail(KVPRM_E_INVALID, "%s: fp8 cache needs k_scale and v_scale", fn);
+  if (h->dm.kvdt == 3 && (((uintptr_t)c->k_pages | (uintptr_t)c->v_pages) & 15) != 0)
+    return fail(KVPRM_E_INVALID, "%s: 4-bit pools not 16-byte aligned", fn);
   return KVPRM_OK;
 }
 
@@ -724,6 +728,8 @@ kvprm_status kvprm_pack_kv(const void *src, void *dst, int64_t num_tiles, int32_
   if (num_tiles < 0) return fail(KVPRM_E_INVALID, "%s: num_tiles < 0", fn);
   if (head_dim != 64 && head_dim != 128)
     return fail(KVPRM_E_UNSUPPORTED, "%s: head_dim must be 64 or 128", fn);
+  if (dtype == KVPRM_FP4_E2M1)
+    return fail(KVPRM_E_UNSUPPORTED, "%s: 4-bit tiles are written by kvprm_write_kv", fn);
   if (dtype != KVPRM_F32 && dtype != KVPRM_BF16 && dtype != KVPRM_FP8_E4M3)
     return fail(KVPRM_E_INVALID, "%s: unknown dtype %d", fn, (int)dtype);
   if (part != KVPRM_KEYS && part != KVPRM_VALUES)
@@ -1061,6 +1067,116 @@ kvprm_status kvprm_attention_tree(kvprm_handle h, const kvprm_kv_cache *cache, c
     return fail(KVPRM_E_WORKSPACE, "%s: workspace not 256-byte aligned", fn);
   if ((st = check_pages_debug(h, cache, b, (hipStream_t)stream, fn)) != KVPRM_OK) return st;
   HIP_TRY(launch_tree(h->dm, *cache, *b, layer, *t, workspace, (hipStream_t)stream), "tree attention");
+  return ok();
+}
+
+// ------------------------------------------------------------------ pages of the cache
+
+static kvprm_status check_page_rows(const kvprm_page_rows *r, bool lengths, const char *what, const char *fn) {
+  if (!r) return fail(KVPRM_E_INVALID, "%s: null %s", fn, what);
+  if (r->rows < 0) return fail(KVPRM_E_INVALID, "%s: %s: rows < 0", fn, what);
+  if (r->rows > kMaxBatch) return fail(KVPRM_E_UNSUPPORTED, "%s: %s: at most %d rows", fn, what, kMaxBatch);
+  if (r->rows == 0) return KVPRM_OK;
+  if (r->max_pages < 1) return fail(KVPRM_E_INVALID, "%s: %s: max_pages < 1", fn, what);
+  if (r->max_pages > kMaxTablePages)
+    return fail(KVPRM_E_UNSUPPORTED, "%s: %s: at most %d pages a row", fn, what, kMaxTablePages);
+  if (!r->page_table || !r->held || (lengths && !r->lengths))
+    return fail(KVPRM_E_INVALID, "%s: %s: null table, lengths or held", fn, what);
+  return KVPRM_OK;
+}
+
+// An array of `n` 32-bit words that a call reads or writes.
+struct Words {
+  const void *p;
+  int64_t n;
+  bool written;
+};
+static kvprm_status check_words(const Words *w, int n, const char *fn) {
+  for (int i = 0; i < n; ++i) {
+    if ((uintptr_t)w[i].p % sizeof(int32_t) != 0) return fail(KVPRM_E_INVALID, "%s: an array not aligned to its elements", fn);
+    for (int k = 0; k < i; ++k) {
+      const uintptr_t a = (uintptr_t)w[i].p, b = (uintptr_t)w[k].p;
+      if (!a || !b || (!w[i].written && !w[k].written)) continue;
+      if (a < b + (uintptr_t)w[k].n * 4 && b < a + (uintptr_t)w[i].n * 4)
+        return fail(KVPRM_E_INVALID, "%s: an array that is written overlaps another", fn);
+    }
+  }
+  return KVPRM_OK;
+}
+
+static kvprm_status check_pool(const kvprm_handle h, const kvprm_kv_cache *c, const char *fn) {
+  kvprm_status st = check_cache(h, c, fn);
+  if (st != KVPRM_OK) return st;
+  if ((((uintptr_t)c->k_pages | (uintptr_t)c->v_pages) & 15) != 0)
+    return fail(KVPRM_E_INVALID, "%s: pools not 16-byte aligned", fn);
+  if (c->num_pages > max_pool_pages())
+    return fail(KVPRM_E_UNSUPPORTED, "%s: at most %lld pages", fn, (long long)max_pool_pages());
+  return KVPRM_OK;
+}
+
+static kvprm_status check_pages_ws(int64_t num_pages, const void *ws, size_t n, const char *fn) {
+  const size_t need = pages_ws_bytes(num_pages);
+  if (!ws || n < need)
+    return fail(KVPRM_E_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, ws ? n : (size_t)0);
+  if (((uintptr_t)ws & 255) != 0) return fail(KVPRM_E_WORKSPACE, "%s: workspace not 256-byte aligned", fn);
+  return KVPRM_OK;
+}
+
+kvprm_status kvprm_workspace_size_pages(kvprm_handle h, int32_t num_pages, size_t *bytes) {
+  const char *fn = "kvprm_workspace_size_pages";
+  if (!h || !bytes) return fail(KVPRM_E_INVALID, "%s: null argument", fn);
+  if (num_pages < 1) return fail(KVPRM_E_INVALID, "%s: num_pages < 1", fn);
+  if (num_pages > max_pool_pages())
+    return fail(KVPRM_E_UNSUPPORTED, "%s: at most %lld pages", fn, (long long)max_pool_pages());
+  *bytes = pages_ws_bytes(num_pages);
+  return ok();
+}
+
+kvprm_status kvprm_fork_pages(kvprm_handle h, const kvprm_kv_cache *cache, const kvprm_page_rows *from,
+                              const kvprm_page_rows *to, const int32_t *parent, const int32_t *room,
+                              const int32_t *refs, int32_t *new_refs, int32_t *result, void *workspace,
+                              size_t ws_bytes, void *stream) {
+  const char *fn = "kvprm_fork_pages";
+  if (!h) return fail(KVPRM_E_INVALID, "%s: null handle", fn);
+  kvprm_status st = check_pool(h, cache, fn);
+  if (st != KVPRM_OK) return st;
+  if ((st = check_page_rows(from, true, "from", fn)) != KVPRM_OK) return st;
+  if ((st = check_page_rows(to, true, "to", fn)) != KVPRM_OK) return st;
+  if ((to->rows > 0 && !parent) || !refs || !new_refs || !result)
+    return fail(KVPRM_E_INVALID, "%s: null parent, refs, new_refs or result", fn);
+  const int64_t n = from->rows, m = to->rows;
+  const Words w[] = {{n ? from->page_table : nullptr, n * from->max_pages, false}, {n ? from->lengths : nullptr, n, false},
+                     {n ? from->held : nullptr, n, false}, {m ? parent : nullptr, m, false}, {m ? room : nullptr, m, false},
+                     {refs, cache->num_pages, false}, {new_refs, cache->num_pages, true}, {result, 4, true},
+                     {m ? to->page_table : nullptr, m * to->max_pages, true}, {m ? to->lengths : nullptr, m, true},
+                     {m ? to->held : nullptr, m, true}, {workspace, (int64_t)(pages_ws_bytes(cache->num_pages) / 4), true}};
+  if ((st = check_words(w, sizeof w / sizeof *w, fn)) != KVPRM_OK) return st;
+  if ((st = check_pages_ws(cache->num_pages, workspace, ws_bytes, fn)) != KVPRM_OK) return st;
+  HIP_TRY(launch_fork_pages(h->dm, *cache, *from, *to, parent, room, refs, new_refs, result, workspace,
+                            (hipStream_t)stream),
+          "fork pages");
+  return ok();
+}
+
+kvprm_status kvprm_compact_pages(kvprm_handle h, const kvprm_kv_cache *cache, const kvprm_page_rows *rows,
+                                 int32_t *new_table, const int32_t *refs, int32_t *new_refs, int32_t *moved,
+                                 int32_t *result, void *workspace, size_t ws_bytes, void *stream) {
+  const char *fn = "kvprm_compact_pages";
+  if (!h) return fail(KVPRM_E_INVALID, "%s: null handle", fn);
+  kvprm_status st = check_pool(h, cache, fn);
+  if (st != KVPRM_OK) return st;
+  if ((st = check_page_rows(rows, false, "rows", fn)) != KVPRM_OK) return st;
+  if ((rows->rows > 0 && !new_table) || !refs || !new_refs || !moved || !result)
+    return fail(KVPRM_E_INVALID, "%s: null new_table, refs, new_refs, moved or result", fn);
+  const int64_t n = rows->rows, pages = cache->num_pages;
+  const Words w[] = {{n ? rows->page_table : nullptr, n * rows->max_pages, false}, {n ? rows->held : nullptr, n, false},
+                     {n ? new_table : nullptr, n * rows->max_pages, true}, {refs, pages, false}, {new_refs, pages, true},
+                     {moved, pages, true}, {result, 4, true}, {workspace, (int64_t)(pages_ws_bytes(pages) / 4), true}};
+  if ((st = check_words(w, sizeof w / sizeof *w, fn)) != KVPRM_OK) return st;
+  if ((st = check_pages_ws(pages, workspace, ws_bytes, fn)) != KVPRM_OK) return st;
+  HIP_TRY(launch_compact_pages(h->dm, *cache, *rows, new_table, refs, new_refs, moved, result, workspace,
+                               (hipStream_t)stream),
+          "compact pages");
   return ok();
 }
 

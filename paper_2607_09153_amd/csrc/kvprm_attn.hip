@@ -28,7 +28,7 @@ template <int KVT, int D>
 __device__ __forceinline__ void load_query(const float *qr, int cq, QueryRaw<D> &r) {
 #pragma unroll
   for (int kk = 0; kk < D / 32; ++kk) {
-    const int dim = (KVT == 1) ? kk * 32 + 8 * cq : 16 * (4 * (kk >> 1) + cq) + 8 * (kk & 1);
+    const int dim = key_dim<KVT, D>(kk, cq);
     r.v[kk][0] = *(const f32x4u *)(qr + dim);
     r.v[kk][1] = *(const f32x4u *)(qr + dim + 4);
   }
@@ -178,7 +178,7 @@ __device__ __forceinline__ void walk_pages(const AttnArgs &a, int b, int j, int 
                                            float &l_run, floatx4 (&acc)[D / 16]) {
   constexpr int NKB = D / 32;  // 32-dim blocks of q.k
   constexpr int NDB = D / 16;  // 16-dim blocks of the output
-  constexpr size_t TILE = (size_t)kPage * D * (KVT == 1 ? 2 : 1);
+  constexpr size_t TILE = tile_bytes(KVT, D);
   const int nkv = a.nkv;
   const int lane = threadIdx.x & 63, cq = lane >> 4;
   // each wave reads the chunk's page ids itself into lane registers (lane i holds page i, lanes
@@ -191,27 +191,25 @@ __device__ __forceinline__ void walk_pages(const AttnArgs &a, int b, int j, int 
     vsc_l = a.vsc[(size_t)ph_l * nkv + j];
   }
   const int npairs = (np + 1) >> 1;
-  auto load_pair = [&](int pp, PairRaw<D> &r) {
+  auto load_pair = [&](int pp, PairOf<KVT, D> &r) {
     // indices past the chunk are clamped to its last page: those tokens are masked anyway
     const int pa = lane_value(ph_l, min(2 * pp, np - 1));
     const int pb = lane_value(ph_l, min(2 * pp + 1, np - 1));
-    load_pair_raw<KVT, D, true>((const uint4 *)(a.kp + ((size_t)pa * nkv + j) * TILE),
-                          (const uint4 *)(a.kp + ((size_t)pb * nkv + j) * TILE),
-                          (const uint4 *)(a.vp + ((size_t)pa * nkv + j) * TILE),
-                          (const uint4 *)(a.vp + ((size_t)pb * nkv + j) * TILE), lane, r);
+    load_pair_of<KVT, D, true>(a.kp + ((size_t)pa * nkv + j) * TILE, a.kp + ((size_t)pb * nkv + j) * TILE,
+                               a.vp + ((size_t)pa * nkv + j) * TILE, a.vp + ((size_t)pb * nkv + j) * TILE, lane, r);
   };
-  PairRaw<D> r0, r1;
+  PairOf<KVT, D> r0, r1;
   load_pair(0, r0);
   __builtin_amdgcn_sched_barrier(0);
   uint4 q0[NKB], q1[NKB], q2[NKB];
   query_ops<D>(qraw, colv, q0, q1, q2);
   const float rs = kLog2e / sqrtf((float)D);  // scores in log2 units
-  auto compute_pair = [&](int pp, const PairRaw<D> &r, auto maskv) {
+  auto compute_pair = [&](int pp, const PairOf<KVT, D> &r, auto maskv) {
     const int la = min(2 * pp, np - 1), lb = 2 * pp + 1;
     const bool hasA = 2 * pp < np, hasB = lb < np;
     uint4 KA[NKB], KB[NKB];
     uint2 VA[NDB], VB[NDB];
-    unpack_pair<KVT, D>(r, KA, KB, VA, VB);
+    unpack_pair_of<KVT, D>(r, KA, KB, VA, VB);
     const int ta = (p0 + la) * kPage + 4 * cq, tb = (p0 + lb) * kPage + 4 * cq;
     bool ok[8];
 #pragma unroll
@@ -249,7 +247,7 @@ __device__ __forceinline__ void walk_pages(const AttnArgs &a, int b, int j, int 
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  if (KVT == 2 && p0 + np < npages)
+  if (KVT >= 2 && p0 + np < npages)
     chunk_loop(std::integral_constant<bool, false>{});
   else
     chunk_loop(std::integral_constant<bool, true>{});
@@ -465,8 +463,7 @@ __global__ __launch_bounds__(64 * kShortWaves) void k_attn_short(AttnArgs a) {
 template <int KVT, int D>
 __global__ __launch_bounds__(64 * kPrefixWaves) void k_prefix_mx(AttnArgs a) {
   constexpr int NKB = D / 32, NDB = D / 16;
-  constexpr int EB = KVT == 1 ? 2 : 1;
-  constexpr int TILE16 = kPage * D * EB / 16;  // uint4 entries per tile
+  constexpr int TILE16 = (int)(tile_bytes(KVT, D) / 16);  // uint4 entries per tile
   __shared__ uint4 stage_s[2][4][TILE16];      // [buffer][K A, K B, V A, V B]
   const int c = blockIdx.x, j = blockIdx.y;
   // group and column block of this block
@@ -500,7 +497,7 @@ __global__ __launch_bounds__(64 * kPrefixWaves) void k_prefix_mx(AttnArgs a) {
   // the pair being computed sits in one of two LDS buffers. Fetches past the last pair repeat
   // it (an L2 hit), so that no load is conditional.
   constexpr int PER = (4 * TILE16 + nthr - 1) / nthr;
-  constexpr int NPF = KVT == 2 ? 2 : 4;  // pairs in flight (fp8 unpacking needs the registers)
+  constexpr int NPF = KVT >= 2 ? 2 : 4;  // pairs in flight (fp8 unpacking needs the registers)
   struct Stage {
     uint4 v[PER];
   };
@@ -550,12 +547,12 @@ __global__ __launch_bounds__(64 * kPrefixWaves) void k_prefix_mx(AttnArgs a) {
   auto step = [&](int pp, Stage &mine, const Stage &next) __attribute__((always_inline)) {
     mine = fetch(pp + NPF);
     const int buf = pp & 1;
-    PairRaw<D> r;
-    load_pair_raw<KVT, D, false>(stage_s[buf][0], stage_s[buf][1], stage_s[buf][2], stage_s[buf][3],
-                                 lane, r);
+    PairOf<KVT, D> r;
+    load_pair_of<KVT, D, false>((const char *)stage_s[buf][0], (const char *)stage_s[buf][1],
+                                (const char *)stage_s[buf][2], (const char *)stage_s[buf][3], lane, r);
     uint4 KA[NKB], KB[NKB];
     uint2 VA[NDB], VB[NDB];
-    unpack_pair<KVT, D>(r, KA, KB, VA, VB);
+    unpack_pair_of<KVT, D>(r, KA, KB, VA, VB);
     const int la = 2 * pp, lb = 2 * pp + 1;
     const bool hasB = lb < np;
     bool ok[8];
@@ -773,6 +770,9 @@ hipError_t launch_attn_mx(const Dims &dm, const Plan &p, const Workspace &w, con
     if (dm.kvdt == 1) {
       if (dm.d == 64) KVPRM_P(1, 64);
       else KVPRM_P(1, 128);
+    } else if (dm.kvdt == 3) {
+      if (dm.d == 64) KVPRM_P(3, 64);
+      else KVPRM_P(3, 128);
     } else {
       if (dm.d == 64) KVPRM_P(2, 64);
       else KVPRM_P(2, 128);
@@ -797,6 +797,12 @@ hipError_t launch_attn_mx(const Dims &dm, const Plan &p, const Workspace &w, con
       KVPRM_A(1, 64);
     } else {
       KVPRM_A(1, 128);
+    }
+  } else if (dm.kvdt == 3) {
+    if (dm.d == 64) {
+      KVPRM_A(3, 64);
+    } else {
+      KVPRM_A(3, 128);
     }
   } else {
     if (dm.d == 64) {
@@ -997,6 +1003,9 @@ hipError_t launch_attn_short(const Dims &dm, const Plan &p, const Workspace &w, 
   } else if (dm.kvdt == 1) {
     if (dm.d == 64) hipLaunchKernelGGL((k_attn_short<1, 64>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((k_attn_short<1, 128>), grid, block, 0, s, a);
+  } else if (dm.kvdt == 3) {
+    if (dm.d == 64) hipLaunchKernelGGL((k_attn_short<3, 64>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_attn_short<3, 128>), grid, block, 0, s, a);
   } else {
     if (dm.d == 64) hipLaunchKernelGGL((k_attn_short<2, 64>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((k_attn_short<2, 128>), grid, block, 0, s, a);

@@ -1,8 +1,10 @@
 // The cache's traffic outside scoring for gfx950: rotary positions of queries and keys (k_rotary),
-// rows of keys and values written into the paged cache (k_write_kv) and read back (k_read_kv).
+// rows of keys and values written into the paged cache (k_write_kv, 4 bits: k_write_kv4) and read back
+// (k_read_kv, k_read_kv4).
 #include <hip/hip_runtime.h>
 #include <math.h>
 
+#include "kvprm_attn_common.h"
 #include "kvprm_internal.h"
 #include "kvprm_mx_common.h"
 
@@ -583,6 +585,233 @@ __global__ __launch_bounds__(256) void k_read_kv(RowArgs a) {
   }
 }
 
+// ------------------------------------------------------------------------------- rows in 4 bits
+
+// Scale byte of 32 values of which the largest magnitude has the bits `amax` (as an integer, so that infinities and
+// NaN are the largest): the exponent, biased by 127, of the smallest s = 2^k with 7 s >= amax (7 = 1.75 * 2^2), from
+// 2^kMinScaleExp to 2^125. Values up to 7 s are off by at most s, as those between codes 4 s and 6 s are. 255 (NaN)
+// where the 32 hold something not finite.
+__device__ __forceinline__ uint32_t scale_byte4(uint32_t amax) {
+  if (amax >= 0x7F800000u) return 255u;
+  const int e = (int)(amax >> 23) - 2 + ((amax & 0x7FFFFFu) > 0x600000u);
+  return (uint32_t)min(max(e, 127 + kMinScaleExp), 252);
+}
+
+// N values (4 or 8), divided by the scale, to N codes, the first in the low bits (nearest even).
+template <int N>
+__device__ __forceinline__ uint32_t codes4(const float *x, float scale) {
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
+  if constexpr (N == 8) {
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
+  }
+  return w;
+}
+
+// k_write_kv for 4-bit tiles: a token's codes and scales depend on that token alone, so nothing that the page holds
+// is read or changed, and the bytes of a value belong to one slot each. The rows of a tile are in registers (16
+// bytes of a row per lane and load); the lanes that share a group of 32 dims find its largest magnitude, and the
+// codes meet in LDS in the stored order.
+template <int D, typename S>
+__global__ __launch_bounds__(256) void k_write_kv4(RowArgs a) {
+  typedef RowMap<D, S> Map;
+  constexpr int VS = Map::VS, RL = Map::RL, NP = Map::NP, TILE = (int)tile_bytes(3, D), CELL = D / 8;
+  __shared__ __align__(16) unsigned char lds[4][TILE];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int b = blockIdx.y;
+  const int item = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + wave);
+  const int per = 2 * a.nkv, slotpage = item / per, pj = item - slotpage * per;
+  const bool part = pj >= a.nkv;
+  const int j = part ? pj - a.nkv : pj;
+  const int L = a.lengths[b], r0 = a.start[b];
+  if (L < 0 || r0 < 0) return;
+  const int n = (int)min((int64_t)min(a.start[b + 1] - r0, a.max_rows), (int64_t)a.max_pages * kPage - L);
+  const int page = L / kPage + slotpage;
+  if (n <= 0 || page * kPage >= L + n) return;
+  const int id = a.page_table[(size_t)b * a.max_pages + page];
+  if (id < 0 || id >= a.num_pages) return;
+  const S *rows = (const S *)(part ? a.v : a.k);
+  const int64_t stride = part ? a.vs : a.ks;
+
+  const Map at(lane);
+  uint4 raw[NP][RL];
+  uint32_t news = 0;  // slots this lane loads that are new
+#pragma unroll
+  for (int p = 0; p < NP; ++p)
+#pragma unroll
+    for (int i = 0; i < RL; ++i) {
+      const int slot = at.slot(p, i), t = page * kPage + slot - L;
+      bool ok = t >= 0 && t < n;
+      int64_t row = 0;
+      if (ok) {
+        row = a.index ? a.index[r0 + t] : r0 + t;
+        ok = row >= 0 && row < a.num_rows;
+      }
+      raw[p][i] = make_uint4(0, 0, 0, 0);
+      if (ok) {
+        raw[p][i] = *(const uint4 *)(rows + row * stride + (int64_t)j * D + at.e0);
+        news |= 1u << slot;
+      }
+    }
+  unsigned char *tb = lds[wave];
+  const int g = at.e0 / kFp4Group, in = at.e0 % kFp4Group;
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    uint32_t code[RL], other[RL];
+#pragma unroll
+    for (int i = 0; i < RL; ++i) {
+      float x[VS];
+      Vec<S, VS>::load((const S *)&raw[p][i], x);
+      uint32_t m = 0;
+#pragma unroll
+      for (int k = 0; k < VS; ++k) m = max(m, __float_as_uint(x[k]) & 0x7FFFFFFFu);
+#pragma unroll
+      for (int off = 1; off < kFp4Group / VS; off <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, off, 64));
+      const uint32_t sc = scale_byte4(m);
+      code[i] = sc == 255u ? 0u : codes4<VS>(x, __uint_as_float(sc << 23));
+      const int slot = at.slot(p, i);
+      if (in == 0) tb[8 * D + (part ? (slot >> 2) * CELL + g * 4 + (slot & 3) : g * 16 + slot)] = (unsigned char)sc;
+    }
+    if (!part) {
+#pragma unroll
+      for (int i = 0; i < RL; ++i) {
+        unsigned char *c = tb + (g * 16 + at.slot(p, i)) * 16 + in / 2;
+        if (VS == 8) *(uint32_t *)c = code[i];
+        else *(uint16_t *)c = (uint16_t)code[i];
+      }
+    } else {
+      // The lanes of dims m .. and m + 16 .. pair up (a byte of values holds the codes of both): the first forms the
+      // bytes of the even dims, the second those of the odd ones.
+      const bool odd = in >= 16;
+#pragma unroll
+      for (int i = 0; i < RL; ++i) {
+        other[i] = (uint32_t)__shfl_xor((int)code[i], 16 / VS, 64);
+        const uint32_t lo = odd ? other[i] >> 4 : code[i], hi = odd ? code[i] >> 4 : other[i];
+        code[i] = (lo & 0x0F0F0F0Fu) | (hi & 0x0F0F0F0Fu) << 4;  // byte k: dim 2 k (+ 1) of this lane pair's VS
+      }
+#pragma unroll
+      for (int k = 0; k < VS / 2; ++k) {
+        const int dim = in % 16 + 2 * k + odd, slot = at.slot(p, 0);
+        unsigned char *c = tb + ((slot >> 2) * 16 + dim) * CELL + g * 4 + (slot & 3);
+        uint32_t w = 0;
+#pragma unroll
+        for (int i = 0; i < RL; ++i) w |= (code[i] >> 8 * k & 255u) << 8 * i;
+        if (RL == 4) *(uint32_t *)c = w;
+        else *(uint16_t *)c = (uint16_t)w;
+      }
+    }
+  }
+#pragma unroll
+  for (int off = Map::LPR; off < 64; off <<= 1) news |= __shfl_xor(news, off, 64);
+  if (!news) return;
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  char *out = (part ? a.vp : a.kp) + ((size_t)id * a.nkv + j) * TILE;
+  if (!part) {
+    if (lane < D / 2 && (news >> (lane & 15) & 1)) *(uint4 *)(out + 16 * lane) = *(const uint4 *)(tb + 16 * lane);
+  } else {
+    const uint32_t bits = news >> 4 * (lane >> 4) & 15u;
+    const uint32_t *from = (const uint32_t *)(tb + lane * CELL);
+    uint32_t *to = (uint32_t *)(out + lane * CELL);
+    if (bits == 15u) {
+      if (CELL == 16) *(uint4 *)to = *(const uint4 *)from;
+      else *(uint2 *)to = *(const uint2 *)from;
+    } else {
+#pragma unroll
+      for (int x = 0; x < CELL; ++x)
+        if (bits >> (x & 3) & 1) ((char *)to)[x] = ((const char *)from)[x];
+    }
+  }
+  const int slot = part ? lane / CELL * 4 + (lane & 3) : lane & 15;
+  if (lane < D / 2 && (news >> slot & 1)) out[8 * D + lane] = (char)tb[8 * D + lane];
+}
+
+// k_read_kv for 4-bit tiles.
+template <int D, typename S>
+__global__ __launch_bounds__(256) void k_read_kv4(RowArgs a) {
+  typedef RowMap<D, S> Map;
+  constexpr int VS = Map::VS, RL = Map::RL, NP = Map::NP, TILE = (int)tile_bytes(3, D), CELL = D / 8;
+  __shared__ uint4 lds[4][TILE / 16];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int b = blockIdx.y;
+  const int item = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + wave);
+  const int parts = (a.k ? 1 : 0) + (a.v ? 1 : 0);
+  const int per = parts * a.nkv, slotpage = item / per, pj = item - slotpage * per;
+  const bool part = !a.k || pj >= a.nkv;
+  const int j = pj >= a.nkv ? pj - a.nkv : pj;
+  const int L = (int)min((int64_t)a.lengths[b], (int64_t)a.max_pages * kPage);
+  const int r0 = a.start[b], n = min(a.start[b + 1] - r0, a.max_rows);
+  const int p0 = a.first ? a.first[b] : 0;  // position of the first row
+  const int from = max(p0, 0), to = (int)min((int64_t)L, (int64_t)p0 + n);
+  const int page = from / kPage + slotpage;
+  if (n <= 0 || from >= to || page * kPage >= to) return;
+  const int id = a.page_table[(size_t)b * a.max_pages + page];
+  if (id < 0 || id >= a.num_pages) return;
+  const uint4 *in = (const uint4 *)((part ? a.vp : a.kp) + ((size_t)id * a.nkv + j) * TILE);
+#pragma unroll
+  for (int it = 0; it < (TILE / 16 + 63) / 64; ++it)
+    if (it * 64 + lane < TILE / 16) lds[wave][it * 64 + lane] = load_group(in + it * 64 + lane, a.once);
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  const unsigned char *tb = (const unsigned char *)lds[wave];
+  S *rows = (S *)(part ? a.v : a.k);
+  const int64_t stride = part ? a.vs : a.ks;
+  const Map at(lane);
+  const int g = at.e0 / kFp4Group, first = at.e0 % kFp4Group;
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    uint32_t y[RL][VS / 2];  // bf16 pairs (every value is one)
+    if (!part) {
+#pragma unroll
+      for (int i = 0; i < RL; ++i) {
+        const int cell = g * 16 + at.slot(p, i);
+        const float sc = scale_of<0>(tb[8 * D + cell]);
+        const unsigned char *c = tb + cell * 16 + first / 2;
+        const uint32_t w = VS == 8 ? *(const uint32_t *)c : *(const uint16_t *)c;
+        y[i][0] = fp4x2_to_bf16x2<0>(w, sc);
+        y[i][1] = fp4x2_to_bf16x2<1>(w, sc);
+        if constexpr (VS == 8) y[i][2] = fp4x2_to_bf16x2<2>(w, sc), y[i][3] = fp4x2_to_bf16x2<3>(w, sc);
+      }
+    } else {
+      // a byte holds dims m and m + 16 of a slot: both are converted, this lane's kept
+      const uint32_t keep = first >= 16 ? 0x07060302u : 0x05040100u;
+      const int slot = at.slot(p, 0), cell = (slot >> 2) * 16 + first % 16;
+      auto bytes = [&](const unsigned char *c) -> uint32_t {
+        return RL == 4 ? *(const uint32_t *)c : *(const uint16_t *)c;
+      };
+      const uint32_t sw = bytes(tb + 8 * D + (slot >> 2) * CELL + g * 4 + (slot & 3));
+      const float sc[4] = {scale_of<0>(sw), scale_of<1>(sw), scale_of<2>(sw), scale_of<3>(sw)};
+#pragma unroll
+      for (int k = 0; k < VS / 2; ++k) {
+        const uint32_t w0 = bytes(tb + (cell + 2 * k) * CELL + g * 4 + (slot & 3));
+        const uint32_t w1 = bytes(tb + (cell + 2 * k + 1) * CELL + g * 4 + (slot & 3));
+        auto pair = [&](uint32_t x1, uint32_t x0) { return __builtin_amdgcn_perm(x1, x0, keep); };
+        y[0][k] = pair(fp4x2_to_bf16x2<0>(w1, sc[0]), fp4x2_to_bf16x2<0>(w0, sc[0]));
+        y[1][k] = pair(fp4x2_to_bf16x2<1>(w1, sc[1]), fp4x2_to_bf16x2<1>(w0, sc[1]));
+        if constexpr (RL == 4) {
+          y[2][k] = pair(fp4x2_to_bf16x2<2>(w1, sc[2]), fp4x2_to_bf16x2<2>(w0, sc[2]));
+          y[3][k] = pair(fp4x2_to_bf16x2<3>(w1, sc[3]), fp4x2_to_bf16x2<3>(w0, sc[3]));
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < RL; ++i) {
+      const int pos = page * kPage + at.slot(p, i);
+      const int64_t row = (int64_t)r0 + pos - p0;
+      if (pos < from || pos >= to || row < 0 || row >= a.num_rows) continue;
+      S *dst = rows + row * stride + (int64_t)j * D + at.e0;
+      if constexpr (VS == 8) {
+        *(u32x4v *)dst = u32x4v{y[i][0], y[i][1], y[i][2], y[i][3]};
+      } else {
+        *(float4 *)dst = make_float4(__uint_as_float(y[i][0] << 16), __uint_as_float(y[i][0] & 0xFFFF0000u),
+                                     __uint_as_float(y[i][1] << 16), __uint_as_float(y[i][1] & 0xFFFF0000u));
+      }
+    }
+  }
+}
+
 // The tiles are read past the caches where the rows take this much: 128 MB of fp32 rows from fp32 tiles 51.1 us so and
 // 55.6 through the caches, bf16 from bf16 51.0 and 54.9, bf16 from fp8 39.9 and 42.0, 512 MB 192, 192 and 148 instead of
 // 207, 206 and 157. A smaller call leaves the tiles there for whoever reads them next (8 MB take 7.9 and 8.0 us).
@@ -591,7 +820,7 @@ constexpr int64_t kOnceBytes = (int64_t)128 << 20;
 static RowArgs row_args(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batch &b, int layer,
                         const kvprm_kv_rows &r) {
   const size_t tiles = (size_t)c.num_pages * dm.nkv;
-  const size_t bytes = tiles * kPage * dm.d * (dm.kvdt == 0 ? 4 : dm.kvdt == 1 ? 2 : 1);
+  const size_t bytes = tiles * tile_bytes(dm.kvdt, dm.d);
   RowArgs a;
   a.kp = (char *)c.k_pages + layer * bytes;
   a.vp = (char *)c.v_pages + layer * bytes;
@@ -628,6 +857,12 @@ static int pages_of(int n) { return (n + 2 * kPage - 2) / kPage; }
   if (dm.kvdt == 0) { KVPRM_ROWS_D(K_, 0) }                                                       \
   else if (dm.kvdt == 1) { KVPRM_ROWS_D(K_, 1) }                                                  \
   else { KVPRM_ROWS_D(K_, 2) }
+#define KVPRM_ROWS4_S(K_, D_)                                                                     \
+  if (bf16) hipLaunchKernelGGL((K_<D_, uint16_t>), grid, dim3(256), 0, s, a);                     \
+  else hipLaunchKernelGGL((K_<D_, float>), grid, dim3(256), 0, s, a)
+#define KVPRM_ROWS4(K_)                                                                           \
+  if (dm.d == 64) { KVPRM_ROWS4_S(K_, 64); }                                                      \
+  else { KVPRM_ROWS4_S(K_, 128); }
 
 hipError_t launch_write_kv(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batch &b, int layer,
                            const kvprm_kv_rows &r, hipStream_t s) {
@@ -635,7 +870,8 @@ hipError_t launch_write_kv(const Dims &dm, const kvprm_kv_cache &c, const kvprm_
   const bool bf16 = r.dtype == KVPRM_BF16;
   const int pages = min(pages_of(a.max_rows), b.max_pages);
   const dim3 grid((unsigned)(((int64_t)pages * 2 * dm.nkv + 3) / 4), b.batch);
-  KVPRM_ROWS(k_write_kv)
+  if (dm.kvdt == 3) { KVPRM_ROWS4(k_write_kv4) }
+  else KVPRM_ROWS(k_write_kv)
   return hipGetLastError();
 }
 
@@ -651,7 +887,8 @@ hipError_t launch_read_kv(const Dims &dm, const kvprm_kv_cache &c, const kvprm_b
   a.once = rows * dm.nkv * dm.d * parts * (bf16 ? 2 : 4) >= kOnceBytes;
   const int pages = min(pages_of(most), b.max_pages);
   const dim3 grid((unsigned)(((int64_t)pages * parts * dm.nkv + 3) / 4), b.batch);
-  KVPRM_ROWS(k_read_kv)
+  if (dm.kvdt == 3) { KVPRM_ROWS4(k_read_kv4) }
+  else KVPRM_ROWS(k_read_kv)
   return hipGetLastError();
 }
 

@@ -13,7 +13,7 @@ struct Dims {
   int layers, H, nq, nkv, d, F, g;
   float theta, eps;
   int wdt;   // 0 fp32, 1 bf16
-  int kvdt;  // 0 fp32, 1 bf16, 2 fp8 e4m3
+  int kvdt;  // 0 fp32, 1 bf16, 2 fp8 e4m3, 3 fp4 e2m1
 };
 
 // Prefix-sharing groups, passed by value to the attention kernels (no host->device copy).
@@ -45,6 +45,13 @@ constexpr int kShortPages = 32;   // longest cache of the one-launch attention
 constexpr int kShortWaves = 8;    // its waves per block
 constexpr int kMaxBatch = 256;    // candidates of a call
 constexpr int kPage = 16;
+constexpr int kFp4Group = 32;  // dims of a token that share a scale of a 4-bit tile
+
+// Bytes of a stored tile (keys or values of one page and kv-head) by cache type. A 4-bit tile is 8 d bytes of
+// codes and d / 2 of scales.
+__host__ __device__ constexpr size_t tile_bytes(int kvdt, int d) {
+  return kvdt == 3 ? 17 * (size_t)d / 2 : (size_t)kPage * d * (kvdt == 0 ? 4 : kvdt == 1 ? 2 : 1);
+}
 
 // Workspace carve-up (all offsets 256-byte aligned).
 struct Workspace {
@@ -244,6 +251,16 @@ hipError_t launch_write_kv(const Dims &dm, const kvprm_kv_cache &c, const kvprm_
                            const kvprm_kv_rows &r, hipStream_t s);
 hipError_t launch_read_kv(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batch &b, int layer,
                           const kvprm_kv_rows &r, const int32_t *first, hipStream_t s);
+// pages of the cache (kvprm_pages.hip)
+constexpr int kMaxTablePages = 1 << 20;  // entries of a row
+int64_t max_pool_pages();
+size_t pages_ws_bytes(int64_t num_pages);
+hipError_t launch_fork_pages(const Dims &dm, const kvprm_kv_cache &c, const kvprm_page_rows &from,
+                             const kvprm_page_rows &to, const int32_t *parent, const int32_t *room, const int32_t *refs,
+                             int32_t *new_refs, int32_t *result, void *ws, hipStream_t s);
+hipError_t launch_compact_pages(const Dims &dm, const kvprm_kv_cache &c, const kvprm_page_rows &rows,
+                                int32_t *new_table, const int32_t *refs, int32_t *new_refs, int32_t *moved,
+                                int32_t *result, void *ws, hipStream_t s);
 // attention of drafted tokens (kvprm_tree.hip)
 constexpr int kMaxTreeRows = 256;
 size_t tree_ws_need(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t);   // of this call

@@ -57,7 +57,7 @@ static size_t partial_elems(const GemvPlan &g) {
 
 // Bytes of keys and values of one page and head.
 static int page_bytes(const Dims &dm) {
-  return 2 * kPage * dm.d * (dm.kvdt == 0 ? 4 : dm.kvdt == 1 ? 2 : 1);
+  return 2 * (int)tile_bytes(dm.kvdt, dm.d);
 }
 
 // Waves (kv-head x chunk) up to which shorter attention chunks pay: a wave takes about 4 us to
@@ -348,10 +348,9 @@ hipError_t launch_attention(const Dims &dm, const Plan &p, const Workspace &w, i
                             const int32_t *lengths, const GroupTable &gt, const float *q,
                             const float *kself, const float *vself, float *o, uint16_t *op,
                             hipStream_t s, float *lse, bool partials_only) {
-  const int EB = dm.kvdt == 0 ? 4 : (dm.kvdt == 1 ? 2 : 1);
-  const size_t layer_elems = (size_t)num_pages * dm.nkv * kPage * dm.d;
-  const char *kp = (const char *)kpool + layer_elems * EB * layer;
-  const char *vp = (const char *)vpool + layer_elems * EB * layer;
+  const size_t layer_bytes = (size_t)num_pages * dm.nkv * tile_bytes(dm.kvdt, dm.d);
+  const char *kp = (const char *)kpool + layer_bytes * layer;
+  const char *vp = (const char *)vpool + layer_bytes * layer;
   const float *ksc = kscale ? kscale + (size_t)layer * num_pages * dm.nkv : nullptr;
   const float *vsc = vscale ? vscale + (size_t)layer * num_pages * dm.nkv : nullptr;
   if (gt.one_launch && !partials_only)

@@ -1,0 +1,449 @@
+// Pages of the cache for gfx950: rows of a page table forked into others with copy-on-write (kvprm_fork_pages), and the
+// live pages of a pool moved into its lowest ids (kvprm_compact_pages). Both plan on the device from holders' counts
+// and tables, in a few short launches, and end with one launch that copies the pages of all layers.
+#include <hip/hip_runtime.h>
+
+#include "kvprm_attn_common.h"
+#include "kvprm_internal.h"
+
+namespace kvprm {
+
+// Pages of a scan block: each of its waves takes 64 pages at a time and keeps their flags as one word.
+constexpr int kScanPages = 4096, kScanWords = kScanPages / 64;
+constexpr int kMaxScanBlocks = 1024;  // blocks of a pool (4 M pages)
+
+// Workspace of both calls. Nothing in it needs to be set on entry.
+struct PageScan {
+  uint64_t *mask;    // [words] a bit per page: free for fresh pages, or (compact) live
+  int32_t *before;   // [words] such pages of the block before the word
+  int32_t *total;    // [blocks], then their exclusive sums
+  int32_t *count;    // [num_pages] holders besides the old rows; (compact) the pages that move
+  int32_t *shared;   // [num_pages] new rows that share the page
+  uint64_t *source;  // [words] a bit per page: the source of a copy
+  int32_t *row;      // [rows][4] of a fork, see RowPlan
+  int32_t *state;    // [8] see State
+  size_t bytes;
+};
+enum State { kBad = 0, kArrived = 1, kTotal = 2, kNeed = 3, kEmpty = 4, kDone = 5 };
+
+// A new row: its tokens, the pages it shares with its parent, the pages it holds, and the source of its copy or -1.
+struct RowPlan {
+  int len, shared, held, copy;
+};
+
+static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+static PageScan carve_pages(int64_t num_pages, void *base) {
+  PageScan w;
+  char *p = (char *)base;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    char *r = p + at;
+    at += align256(bytes);
+    return r;
+  };
+  const size_t blocks = (size_t)((num_pages + kScanPages - 1) / kScanPages), words = blocks * kScanWords;
+  w.mask = (uint64_t *)take(words * 8);
+  w.source = (uint64_t *)take(words * 8);
+  w.before = (int32_t *)take(words * 4);
+  w.total = (int32_t *)take((blocks + 1) * 4);
+  w.count = (int32_t *)take((size_t)num_pages * 4);
+  w.shared = (int32_t *)take((size_t)num_pages * 4);
+  w.row = (int32_t *)take((size_t)kMaxBatch * 16);
+  w.state = (int32_t *)take(64);
+  w.bytes = at;
+  return w;
+}
+
+int64_t max_pool_pages() { return (int64_t)kMaxScanBlocks * kScanPages; }
+size_t pages_ws_bytes(int64_t num_pages) { return carve_pages(num_pages, nullptr).bytes; }
+
+struct PageArgs {
+  int num_pages, rows, max_pages;
+  const int32_t *table, *lengths, *held;
+  const int32_t *refs;
+  int32_t *new_refs, *result;
+  // fork
+  int children, to_pages;
+  const int32_t *parent, *room;
+  int32_t *to_table, *to_lengths, *to_held;
+  // compact
+  int32_t *moved;
+  PageScan w;
+  // the pools
+  char *pool[2];
+  float *scale[2];
+  int layers, nkv;
+  size_t page_bytes;  // of one page and layer, keys or values
+};
+
+// The k-th page (from 0) whose bit is set: a search among the blocks' sums, one among the block's words, then the
+// word's bits.
+__device__ __forceinline__ int select_page(const PageScan &w, int blocks, int k) {
+  int lo = 0, hi = blocks - 1;  // the last block whose sum is at most k
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (w.total[mid] <= k) lo = mid;
+    else hi = mid - 1;
+  }
+  k -= w.total[lo];
+  const int32_t *before = w.before + lo * kScanWords;
+  int a = 0, b = kScanWords - 1;
+  while (a < b) {
+    const int mid = (a + b + 1) / 2;
+    if (before[mid] <= k) a = mid;
+    else b = mid - 1;
+  }
+  k -= before[a];
+  uint64_t m = w.mask[lo * kScanWords + a];
+  int at = 0;
+#pragma unroll
+  for (int width = 32; width > 0; width >>= 1) {  // the half that holds bit k
+    const int low = __popcll(m & ((1ull << width) - 1));
+    if (k >= low) k -= low, m >>= width, at += width;
+  }
+  return (lo * kScanWords + a) * 64 + at;
+}
+// Set bits among the pages below `page`.
+__device__ __forceinline__ int rank_page(const PageScan &w, int page) {
+  const int word = page >> 6;
+  return w.total[word / kScanWords] + w.before[word] + __popcll(w.mask[word] & ((1ull << (page & 63)) - 1));
+}
+
+// A block's flags, counted: words and the block's sum; the last block to arrive turns the sums into exclusive ones.
+// 256 threads of blocks 0 .. blocks - 1; flag(page) is called for pages of the pool alone.
+template <typename F>
+__device__ __forceinline__ void scan_flags(const PageArgs &a, int blocks, F flag) {
+  __shared__ int word_s[kScanWords];
+  __shared__ int last_s;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int blk = blockIdx.x;
+#pragma unroll
+  for (int i = 0; i < kScanWords / 4; ++i) {
+    const int word = i * 4 + wave, page = blk * kScanPages + word * 64 + lane;
+    const uint64_t m = __ballot(page < a.num_pages && flag(page));
+    if (lane == 0) {
+      word_s[word] = __popcll(m);
+      a.w.mask[blk * kScanWords + word] = m;
+    }
+  }
+  __syncthreads();
+  if (wave == 0) {
+    const int n = word_s[lane], cum = lane_scan(n);
+    a.w.before[blk * kScanWords + lane] = cum - n;
+    if (lane == 63) {
+      __hip_atomic_store(&a.w.total[blk], cum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __threadfence();
+      last_s = __hip_atomic_fetch_add(&a.w.state[kArrived], 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == blocks - 1;
+    }
+  }
+  __syncthreads();
+  if (!last_s) return;
+  __threadfence();
+  if (wave == 0) {
+    int sum = 0;
+    for (int i0 = 0; i0 < blocks; i0 += 64) {
+      const int i = i0 + lane;
+      const int n = i < blocks ? __hip_atomic_load(&a.w.total[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+      const int cum = lane_scan(n);
+      if (i < blocks) a.w.total[i] = sum + cum - n;
+      sum += __builtin_amdgcn_readlane(cum, 63);
+    }
+    if (lane == 0) a.w.state[kTotal] = sum;
+  }
+}
+
+// ------------------------------------------------------------------------------- fork
+
+// Holders before the call, a thread per page; the state.
+__global__ __launch_bounds__(256) void k_fork_init(PageArgs a) {
+  const int page = blockIdx.x * 256 + threadIdx.x;
+  if (page < a.num_pages) a.w.count[page] = a.refs[page], a.w.shared[page] = 0;
+  if (page < (a.num_pages + 63) / 64) a.w.source[page] = 0;
+  if (blockIdx.x == 0 && threadIdx.x < 8) a.w.state[threadIdx.x] = 0;
+}
+
+// What child i takes from its parent (the same in every thread of a block of at least kMaxBatch). False where the
+// rows are inconsistent.
+__device__ __forceinline__ bool plan_row(const PageArgs &a, int i, RowPlan &r) {
+  r = {0, 0, 0, -1};
+  const int p = a.parent[i];
+  const bool first = !__syncthreads_or((int)threadIdx.x < i && a.parent[threadIdx.x] == p);
+  const int64_t room = a.room ? a.room[i] : 0;
+  if (p >= a.rows || room < 0) return false;
+  if (p >= 0) {
+    r.len = a.lengths[p];
+    const int held = a.held[p];
+    if (r.len < 0 || held < 0 || held > a.max_pages || r.len > (int64_t)held * kPage) return false;
+  }
+  const int64_t want = (r.len + room + kPage - 1) / kPage;
+  if (want > a.to_pages) return false;
+  r.held = (int)want;
+  r.shared = r.len / kPage;
+  if (r.len % kPage == 0) return true;
+  const int last = a.table[(size_t)p * a.max_pages + r.shared];
+  if (last < 0 || last >= a.num_pages) return false;
+  if (first && a.refs[last] == 1) ++r.shared;
+  else r.copy = last;
+  return true;
+}
+
+static_assert(kMaxBatch <= 256, "a block compares a child's parent with every earlier one's");
+
+// Block (row, slice): the entries of one row, old rows first (their holds end), then new ones (those of the pages they
+// share begin).
+__global__ __launch_bounds__(256) void k_fork_count(PageArgs a) {
+  const int row = blockIdx.x;
+  const int from = blockIdx.y * 1024, tid = threadIdx.x;
+  bool bad = false;
+  if (row < a.rows) {
+    const int held = a.held[row];
+    if (held < 0 || held > a.max_pages) {
+      bad = true;
+    } else {
+      for (int c = from + tid; c < min(held, from + 1024); c += 256) {
+        const int id = a.table[(size_t)row * a.max_pages + c];
+        if (id < 0 || id >= a.num_pages) bad = true;
+        else atomicSub(&a.w.count[id], 1);
+      }
+    }
+  } else {
+    const int i = row - a.rows;
+    RowPlan r;
+    bad = !plan_row(a, i, r);
+    if (!bad) {
+      const int p = a.parent[i];
+      for (int c = from + tid; c < min(r.shared, from + 1024); c += 256) {
+        const int id = a.table[(size_t)p * a.max_pages + c];
+        if (id < 0 || id >= a.num_pages) bad = true;
+        else atomicAdd(&a.w.shared[id], 1);
+      }
+      if (blockIdx.y == 0 && tid == 0) {
+        *(int4 *)(a.w.row + 4 * i) = make_int4(r.len, r.shared, r.held, r.copy);
+        if (r.copy >= 0) atomicOr((unsigned long long *)&a.w.source[r.copy >> 6], 1ull << (r.copy & 63));
+        atomicAdd(&a.w.state[kNeed], r.held - r.shared);
+      }
+    }
+  }
+  if (bad) atomicOr(&a.w.state[kBad], 1);
+}
+
+// Pages free for fresh entries, counted: those that nobody holds any more and no copy reads.
+__global__ __launch_bounds__(256) void k_fork_scan(PageArgs a) {
+  bool bad = false;
+  int empty = 0;
+  scan_flags(a, gridDim.x, [&](int page) {
+    const int others = a.w.count[page], n = others + a.w.shared[page];
+    bad = bad || others < 0 || n < 0;
+    empty += n == 0;
+    return n == 0 && !(a.w.source[page >> 6] >> (page & 63) & 1);
+  });
+  const int all = lane_scan(empty);
+  if ((threadIdx.x & 63) == 63 && all) atomicAdd(&a.w.state[kEmpty], all);
+  if (bad) atomicOr(&a.w.state[kBad], 1);
+}
+
+// The new rows' tables and the holders of every page.
+__global__ __launch_bounds__(256) void k_fork_write(PageArgs a, int scan_blocks) {
+  const int need = a.w.state[kNeed], have = a.w.state[kTotal];
+  const int status = a.w.state[kBad] ? 2 : need > have ? 1 : 0;
+  const int tid = threadIdx.x;
+  if (blockIdx.x == 0 && tid == 0) {
+    a.result[0] = status;
+    a.result[1] = status == 2 ? 0 : need;
+    a.result[2] = status == 2 ? 0 : have;
+    a.result[3] = status ? 0 : a.w.state[kEmpty] - need;
+  }
+  if (status) return;
+  __shared__ int first_s[kMaxBatch + 1];  // fresh pages of the rows before
+  if (tid < 64) {
+    int sum = 0;
+    for (int i0 = 0; i0 < a.children; i0 += 64) {
+      const int i = i0 + tid;
+      const int n = i < a.children ? a.w.row[4 * i + 2] - a.w.row[4 * i + 1] : 0;
+      const int cum = lane_scan(n);
+      if (i < a.children) first_s[i] = sum + cum - n;
+      sum += __builtin_amdgcn_readlane(cum, 63);
+    }
+    if (tid == 0) first_s[a.children] = sum;
+  }
+  __syncthreads();
+  const int64_t threads = (int64_t)gridDim.x * 256, me = (int64_t)blockIdx.x * 256 + tid;
+  for (int64_t e = me; e < (int64_t)a.children * a.to_pages; e += threads) {
+    const int i = (int)(e / a.to_pages), c = (int)(e - (int64_t)i * a.to_pages);
+    const int4 r = *(const int4 *)(a.w.row + 4 * i);
+    int id = -1;
+    if (c < r.y) id = a.table[(size_t)a.parent[i] * a.max_pages + c];
+    else if (c < r.z) id = select_page(a.w, scan_blocks, first_s[i] + c - r.y);
+    a.to_table[e] = id;
+    if (c == 0) a.to_lengths[i] = r.x, a.to_held[i] = r.z;
+  }
+  for (int64_t page = me; page < a.num_pages; page += threads) {
+    const bool free = a.w.mask[page >> 6] >> (page & 63) & 1;
+    a.new_refs[page] = free && rank_page(a.w, (int)page) < need ? 1 : a.w.count[page] + a.w.shared[page];
+  }
+}
+
+// Pages of every layer, keys and values: blocks take (copy, layer, part) in turn, 16 bytes a thread and load, four in
+// flight.
+__device__ __forceinline__ void copy_page(const PageArgs &a, int src, int dst, int layer, int part) {
+  const size_t base = (size_t)layer * a.num_pages;
+  const uint4 *from = (const uint4 *)(a.pool[part] + (base + src) * a.page_bytes);
+  uint4 *to = (uint4 *)(a.pool[part] + (base + dst) * a.page_bytes);
+  const int n = (int)(a.page_bytes / 16);
+  for (int i0 = threadIdx.x; i0 < n; i0 += 1024) {
+    uint4 v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = from[min(i0 + 256 * u, n - 1)];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i0 + 256 * u < n) to[i0 + 256 * u] = v[u];
+  }
+  if (a.scale[part])
+    for (int i = threadIdx.x; i < a.nkv; i += 256)
+      a.scale[part][(base + dst) * a.nkv + i] = a.scale[part][(base + src) * a.nkv + i];
+}
+
+__global__ __launch_bounds__(256) void k_fork_copy(PageArgs a) {
+  const int i = blockIdx.x;
+  const int4 r = *(const int4 *)(a.w.row + 4 * i);
+  if (a.result[0] != 0 || r.w < 0) return;
+  const int dst = a.to_table[(size_t)i * a.to_pages + r.y];
+  for (int k = blockIdx.y; k < 2 * a.layers; k += gridDim.y) copy_page(a, r.w, dst, k >> 1, k & 1);
+}
+
+// ------------------------------------------------------------------------------- compact
+
+__global__ __launch_bounds__(64) void k_compact_init(PageArgs a) {
+  if (threadIdx.x < 8) a.w.state[threadIdx.x] = 0;
+}
+
+// Live pages, counted by the first blocks; the others look whether every entry of the rows names one, 1024 entries
+// each.
+__global__ __launch_bounds__(256) void k_compact_scan(PageArgs a, int blocks) {
+  bool bad = false;
+  if ((int)blockIdx.x < blocks) {
+    scan_flags(a, blocks, [&](int page) {
+      const int n = a.refs[page];
+      bad = bad || n < 0;
+      return n > 0;
+    });
+  } else {
+    const int per = (a.max_pages + 1023) / 1024, k = blockIdx.x - blocks, row = k / per, from = k % per * 1024;
+    const int held = a.held[row];
+    bad = held < 0 || held > a.max_pages;
+    for (int c = from + threadIdx.x; !bad && c < min(held, from + 1024); c += 256) {
+      const int id = a.table[(size_t)row * a.max_pages + c];
+      bad = id < 0 || id >= a.num_pages || a.refs[id] <= 0;
+    }
+  }
+  if (bad) atomicOr(&a.w.state[kBad], 1);
+}
+
+// The k-th page (from 0) whose bit is not set: a search for it by rank.
+__device__ __forceinline__ int select_hole(const PageScan &w, int num_pages, int k) {
+  int lo = 0, hi = num_pages - 1;  // the first page with k + 1 holes up to and including it
+  while (lo < hi) {
+    const int mid = (int)(((int64_t)lo + hi) / 2);
+    if (mid + 1 - rank_page(w, mid + 1) >= k + 1) hi = mid;
+    else lo = mid + 1;
+  }
+  return lo;
+}
+
+// Where every page goes: the i-th live one past the live pages' number into the i-th hole below it.
+__global__ __launch_bounds__(256) void k_compact_plan(PageArgs a) {
+  const int live = a.w.state[kTotal];
+  const int status = a.w.state[kBad] ? 2 : 0;
+  const int page = blockIdx.x * 256 + threadIdx.x;
+  const int stay = live < a.num_pages ? rank_page(a.w, live) : live;  // live pages that keep their places
+  if (page == 0) {
+    a.result[0] = status;
+    a.result[1] = status ? 0 : live;
+    a.result[2] = status ? 0 : live - stay;
+    a.result[3] = status ? 0 : a.num_pages - live;
+  }
+  if (status || page >= a.num_pages) return;
+  const bool alive = a.w.mask[page >> 6] >> (page & 63) & 1;
+  int to = -1;
+  if (alive) to = page < live ? page : select_hole(a.w, live, rank_page(a.w, page) - stay);
+  a.moved[page] = to;
+  if (alive) {
+    a.new_refs[to] = a.refs[page];
+    if (page >= live) {
+      a.new_refs[page] = 0;
+      a.w.count[rank_page(a.w, page) - stay] = page;  // the list of moves, by rank
+    }
+  } else if (page >= live) {
+    a.new_refs[page] = 0;
+  }
+}
+
+// The rows' new entries, and the moves: blocks take (move, layer, part) in turn.
+__global__ __launch_bounds__(256) void k_compact_move(PageArgs a) {
+  if (a.result[0] != 0) return;
+  const int moves = a.result[2];
+  const int64_t threads = (int64_t)gridDim.x * 256;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < (int64_t)a.rows * a.max_pages; e += threads) {
+    const int row = (int)(e / a.max_pages), c = (int)(e - (int64_t)row * a.max_pages);
+    a.to_table[e] = c < a.held[row] ? a.moved[a.table[e]] : -1;
+  }
+  const int per = 2 * a.layers;
+  for (int64_t k = blockIdx.x; k < (int64_t)moves * per; k += gridDim.x) {
+    const int src = a.w.count[k / per], lp = (int)(k % per);
+    copy_page(a, src, a.moved[src], lp >> 1, lp & 1);
+  }
+}
+
+// ------------------------------------------------------------------------------- launch
+
+static PageArgs page_args(const Dims &dm, const kvprm_kv_cache &c, const kvprm_page_rows &from, const int32_t *refs,
+                          int32_t *new_refs, int32_t *result, void *ws) {
+  PageArgs a{};
+  a.num_pages = c.num_pages;
+  a.rows = from.rows, a.max_pages = from.max_pages;
+  a.table = from.page_table, a.lengths = from.lengths, a.held = from.held;
+  a.refs = refs, a.new_refs = new_refs, a.result = result;
+  a.w = carve_pages(c.num_pages, ws);
+  a.pool[0] = (char *)c.k_pages, a.pool[1] = (char *)c.v_pages;
+  if (dm.kvdt == 2) a.scale[0] = (float *)c.k_scale, a.scale[1] = (float *)c.v_scale;
+  a.layers = dm.layers, a.nkv = dm.nkv;
+  a.page_bytes = dm.nkv * tile_bytes(dm.kvdt, dm.d);
+  return a;
+}
+
+hipError_t launch_fork_pages(const Dims &dm, const kvprm_kv_cache &c, const kvprm_page_rows &from,
+                             const kvprm_page_rows &to, const int32_t *parent, const int32_t *room, const int32_t *refs,
+                             int32_t *new_refs, int32_t *result, void *ws, hipStream_t s) {
+  PageArgs a = page_args(dm, c, from, refs, new_refs, result, ws);
+  a.children = to.rows, a.to_pages = to.max_pages;
+  a.parent = parent, a.room = room;
+  a.to_table = to.page_table, a.to_lengths = to.lengths, a.to_held = to.held;
+  const int blocks = (a.num_pages + kScanPages - 1) / kScanPages;
+  hipLaunchKernelGGL(k_fork_init, dim3((a.num_pages + 255) / 256), dim3(256), 0, s, a);
+  if (a.rows + a.children > 0) {
+    const int wide = max(a.rows > 0 ? a.max_pages : 1, 1);
+    hipLaunchKernelGGL(k_fork_count, dim3(a.rows + a.children, (wide + 1023) / 1024), dim3(256), 0, s, a);
+  }
+  hipLaunchKernelGGL(k_fork_scan, dim3(blocks), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(k_fork_write, dim3(256), dim3(256), 0, s, a, blocks);
+  if (a.children > 0)
+    hipLaunchKernelGGL(k_fork_copy, dim3(a.children, min(2 * a.layers, 64)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_compact_pages(const Dims &dm, const kvprm_kv_cache &c, const kvprm_page_rows &rows,
+                                int32_t *new_table, const int32_t *refs, int32_t *new_refs, int32_t *moved,
+                                int32_t *result, void *ws, hipStream_t s) {
+  PageArgs a = page_args(dm, c, rows, refs, new_refs, result, ws);
+  a.to_table = new_table;
+  a.moved = moved;
+  const int blocks = (a.num_pages + kScanPages - 1) / kScanPages;
+  hipLaunchKernelGGL(k_compact_init, dim3(1), dim3(64), 0, s, a);
+  hipLaunchKernelGGL(k_compact_scan, dim3(blocks + a.rows * ((a.max_pages + 1023) / 1024)), dim3(256), 0, s, a, blocks);
+  hipLaunchKernelGGL(k_compact_plan, dim3((a.num_pages + 255) / 256), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(k_compact_move, dim3(1024), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace kvprm

@@ -298,7 +298,7 @@ template <int KVT, int D, int NC, typename T>
 __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
   constexpr int NKB = D / 32, NDB = D / 16, W = kTreeWaves;
   constexpr int QT = Terms<T>::Q, PT = Terms<T>::P;
-  constexpr size_t TILE = (size_t)kPage * D * (KVT == 0 ? 4 : KVT == 1 ? 2 : 1);
+  constexpr size_t TILE = tile_bytes(KVT, D);
   __shared__ floatx4 sacc[W][NC][NDB][64];
   __shared__ float2 sml[W][NC * 16];
   TreeItem it;
@@ -374,14 +374,13 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
         ksc_l = a.ksc[(size_t)id_l * a.nkv + j];
         vsc_l = a.vsc[(size_t)id_l * a.nkv + j];
       }
-      auto load_pair = [&](int i, PairRaw<D> &r) {
+      auto load_pair = [&](int i, PairOf<KVT, D> &r) {
         const int ia = 2 * min(i, mine - 1);
         const size_t ta = ((size_t)lane_value(id_l, ia) * a.nkv + j) * TILE;
         const size_t tb = ((size_t)lane_value(id_l, ia + 1) * a.nkv + j) * TILE;
-        load_pair_raw<KVT, D, false>((const uint4 *)(a.kp + ta), (const uint4 *)(a.kp + tb),
-                                     (const uint4 *)(a.vp + ta), (const uint4 *)(a.vp + tb), lane, r);
+        load_pair_of<KVT, D, false>(a.kp + ta, a.kp + tb, a.vp + ta, a.vp + tb, lane, r);
       };
-      PairRaw<D> r0, r1;
+      PairOf<KVT, D> r0, r1;
       load_pair(0, r0);
       uint4 qo[NC][QT][NKB];
 #pragma unroll
@@ -389,7 +388,7 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
         const T *qr = qrow(ct);
 #pragma unroll
         for (int kk = 0; kk < NKB; ++kk) {
-          const int dim = KVT == 1 ? kk * 32 + 8 * cq : 16 * (4 * (kk >> 1) + cq) + 8 * (kk & 1);
+          const int dim = key_dim<KVT, D>(kk, cq);
           if constexpr (QT == 1) {
             const uint4 v = *(const uint4 *)(qr + dim);
             qo[ct][0][kk] = present[ct] ? v : make_uint4(0, 0, 0, 0);
@@ -406,10 +405,10 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
           }
         }
       }
-      auto compute = [&](int i, const PairRaw<D> &r) {
+      auto compute = [&](int i, const PairOf<KVT, D> &r) {
         uint4 KA[NKB], KB[NKB];
         uint2 VA[NDB], VB[NDB];
-        unpack_pair<KVT, D>(r, KA, KB, VA, VB);
+        unpack_pair_of<KVT, D>(r, KA, KB, VA, VB);
         const int la = 2 * i;
         const float sca = KVT == 2 ? lane_value(ksc_l, la) * rs : rs;
         const float scb = KVT == 2 ? lane_value(ksc_l, la + 1) * rs : rs;
@@ -675,12 +674,14 @@ template <int KVT, int D, int W>
 __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs a) {
   typedef uint16_t T;
   constexpr int KS = D / 16, NT = D / 32, TC = 2 * D;  // k steps, output tiles, 16-byte groups of a bf16 tile
-  constexpr int SC = KVT == 1 ? 2 * TC : TC;           // 16-byte groups of a pair in memory
-  constexpr int NLC = (SC + 64 * W - 1) / (64 * W);    // of these per thread, K or V
+  constexpr int SC = KVT == 1 ? 2 * TC : KVT == 2 ? TC : TC / 2;  // 16-byte groups of a pair in memory (codes)
+  // of these per thread, K or V (4-bit: a lane's codes and scales, of the page that its wave has)
+  constexpr int NLC = KVT == 3 ? 2 : (SC + 64 * W - 1) / (64 * W);
   constexpr int SEG = kTreeSegStages;
   constexpr bool HALF = KVT == 2;  // values and weights in fp16
   // Pairs that half of the waves can move: the first half of them moves keys, the others values.
   constexpr bool ROLES = 2 * SC <= 64 * W;
+  static_assert(KVT != 3 || (ROLES && W == 4), "4-bit stages: two waves for keys, two for values");
   __shared__ uint4 kb[2][2 * TC], vb[2][2 * TC];
   __shared__ int id_s[2 * SEG + 12];                    // page ids of a segment
   __shared__ float ksc_s[KVT == 2 ? 2 * SEG + 12 : 1];  // key scales / sqrt(d), log2 units
@@ -744,7 +745,15 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
   auto load_half = [&](const char *pool, int s, int &id_l, Half &r) {
     const int i = 2 * (s - s0);
     if ((i & 63) == 0) id_l = id_s[min(i + lane, 2 * SEG + 11)];
-    constexpr size_t TILE = (size_t)kPage * D * (KVT == 1 ? 2 : 1);
+    constexpr size_t TILE = tile_bytes(KVT, D);
+    if constexpr (KVT == 3) {
+      const char *t = pool + ((size_t)lane_value(id_l, (i & 63) + (w & 1)) * a.nkv + j) * TILE;
+      const bool val = w >= W / 2;
+      r.g[0] = load_bytes<D / 8, false>(t + (val ? value_code4<D>(lane) : key_code4<D>(lane)));
+      if (val) r.g[1] = load_bytes<D / 8, false>(t + value_scale4<D>(lane));
+      else r.g[1].x = *(const uint8_t *)(t + key_scale4<D>(lane));
+      return;
+    }
     const int ia = lane_value(id_l, i & 63), ib = lane_value(id_l, (i & 63) + 1);
 #pragma unroll
     for (int k = 0; k < NLC; ++k) {
@@ -760,6 +769,13 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
   // 64 ks + lane.
   auto store_keys = [&](int s, const Half &r) {
     uint4 *kt = kb[s & 1];
+    if constexpr (KVT == 3) {
+      const float sc = scale_of<0>(r.g[1].x);
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x)
+        kt[((lane >> 4) * (D / 32) + x) * 32 + (w & 1) * 16 + (lane & 15)] = keys4(word(r.g[0], x), sc);
+      return;
+    }
 #pragma unroll
     for (int k = 0; k < NLC; ++k) {
       const int i0 = (k * 64 * W + w * 64) % SC, i = i0 % (SC / 2) + lane;
@@ -779,6 +795,22 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
   // product of page and tile t reads groups 64 t + lane of the page.
   auto value_at = [&](int t, int mm, int q) { return ((t * 2 + (q & 1)) * 32 + mm) * 2 + (q >> 1); };
   auto store_values = [&](int s, const Half &r) {
+    if constexpr (KVT == 3) {
+      uint2 *vt = (uint2 *)(vb[s & 1] + ((w & 1) ? TC : 0));
+      const int q = lane >> 4, mm = lane & 15;
+      // slots at or past L may hold anything: they become zeros
+      const int have = s >= nfull ? L - (p0 + 2 * s + (w & 1)) * kPage - 4 * q : kPage;
+      const uint32_t m0 = (have > 0 ? 0xFFFFu : 0u) | (have > 1 ? 0xFFFF0000u : 0u);
+      const uint32_t m1 = (have > 2 ? 0xFFFFu : 0u) | (have > 3 ? 0xFFFF0000u : 0u);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {  // dims mm and mm + 16 of tile t
+        uint2 lo, hi;
+        values4(word(r.g[0], t), word(r.g[1], t), lo, hi);
+        vt[value_at(t, mm, q)] = make_uint2(lo.x & m0, lo.y & m1);
+        vt[value_at(t, mm + 16, q)] = make_uint2(hi.x & m0, hi.y & m1);
+      }
+      return;
+    }
 #pragma unroll
     for (int k = 0; k < NLC; ++k) {
       const int i0 = (k * 64 * W + w * 64) % SC, i = i0 % (SC / 2) + lane;
@@ -1101,7 +1133,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
       if (busy) {
         const Scales sc = scales(s);
         new_max(Cached(), largest(sv, sc.ka, sc.kc));
-        const float ms = KVT == 1 && m == -INFINITY ? 0.f : m;  // (all scores -inf so far; fp8 keys are finite)
+        const float ms = KVT != 2 && m == -INFINITY ? 0.f : m;  // (all scores -inf so far; fp8 keys are finite)
         float p[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -1415,7 +1447,7 @@ hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batc
     p.blocks = (t.max_rows * dm.g + 15) / 16;
   }
   const size_t tiles = (size_t)c.num_pages * dm.nkv;
-  const size_t bytes = tiles * kPage * dm.d * (dm.kvdt == 0 ? 4 : dm.kvdt == 1 ? 2 : 1);
+  const size_t bytes = tiles * tile_bytes(dm.kvdt, dm.d);
   TreeArgs a;
   a.kp = (const char *)c.k_pages + layer * bytes;
   a.vp = (const char *)c.v_pages + layer * bytes;
@@ -1470,10 +1502,13 @@ hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batc
   if (p.wide) {
     if (dm.kvdt == 1 && dm.d == 64) { KVPRM_WIDE(1, 64); }
     else if (dm.kvdt == 1) { KVPRM_WIDE(1, 128); }
+    else if (dm.kvdt == 3 && dm.d == 64) { KVPRM_WIDE(3, 64); }
+    else if (dm.kvdt == 3) { KVPRM_WIDE(3, 128); }
     else if (dm.d == 64) { KVPRM_WIDE(2, 64); }
     else { KVPRM_WIDE(2, 128); }
   } else if (dm.kvdt == 0) { KVPRM_TREE_D(0) }
   else if (dm.kvdt == 1) { KVPRM_TREE_D(1) }
+  else if (dm.kvdt == 3) { KVPRM_TREE_D(3) }
   else { KVPRM_TREE_D(2) }
 #undef KVPRM_WIDE
 #undef KVPRM_TREE_D
