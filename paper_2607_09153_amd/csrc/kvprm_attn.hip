@@ -57,12 +57,12 @@ __device__ __forceinline__ void query_ops(const QueryRaw<D> &r, bool present, ui
 // One online-softmax step over a page pair for the 16 columns (queries) of a wave:
 // S = K Q^T (lane holds tokens 4c + i of pages A and B for column lane % 16; q0, q1, q2 = the
 // query's hi, mid, lo bf16 terms, three MFMAs per 32-dim block), running max and sum, then
-// O^T += V^T P^T with P split hi + lo (two MFMAs per 16-dim block). Scores arrive scaled by
+// O^T += V^T P^T with P split in PT bf16 terms, hi + lo or three (an MFMA each per 16-dim block). Scores arrive scaled by
 // log2(e) (sca, scb include it), so the running max m_run is in log2 units and p = 2^(s - m).
 // ok[] marks valid tokens: masked tokens get p = 0 and, with MASKV, their V entries are zeroed,
 // since slots past a candidate's length may hold NaN (a caller that knows every masked slot holds
 // finite data passes MASKV = false). vsa / vsb scale P for fp8 V.
-template <int D, bool MASKV = true>
+template <int D, bool MASKV = true, int PT = 2>
 __device__ __forceinline__ void online_step(const uint4 *KA, const uint4 *KB, const uint2 *VA,
                                             const uint2 *VB, const uint4 *q0, const uint4 *q1,
                                             const uint4 *q2, const bool *ok, float sca, float scb,
@@ -111,11 +111,15 @@ __device__ __forceinline__ void online_step(const uint4 *KA, const uint4 *KB, co
     pv[i] *= vsa;
     pv[4 + i] *= vsb;
   }
-  uint32_t ph[4], pl[4];
+  uint32_t ph[4], pl[4], pt[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) split2(pv[2 * i], pv[2 * i + 1], ph[i], pl[i]);
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (PT == 2) split2(pv[2 * i], pv[2 * i + 1], ph[i], pl[i]);
+    else split3(pv[2 * i], pv[2 * i + 1], ph[i], pl[i], pt[i]);
+  }
   const uint4 Phi = make_uint4(ph[0], ph[1], ph[2], ph[3]);
   const uint4 Plo = make_uint4(pl[0], pl[1], pl[2], pl[3]);
+  const uint4 Pt = PT == 2 ? Plo : make_uint4(pt[0], pt[1], pt[2], pt[3]);
   const uint32_t ma0 = (ok[0] ? 0xFFFFu : 0u) | (ok[1] ? 0xFFFF0000u : 0u);
   const uint32_t ma1 = (ok[2] ? 0xFFFFu : 0u) | (ok[3] ? 0xFFFF0000u : 0u);
   const uint32_t mb0 = (ok[4] ? 0xFFFFu : 0u) | (ok[5] ? 0xFFFF0000u : 0u);
@@ -126,6 +130,7 @@ __device__ __forceinline__ void online_step(const uint4 *KA, const uint4 *KB, co
                             : make_uint4(VA[nb].x, VA[nb].y, VB[nb].x, VB[nb].y);
     acc[nb] = mfma16(vop, Phi, acc[nb]);
     acc[nb] = mfma16(vop, Plo, acc[nb]);
+    if constexpr (PT == 3) acc[nb] = mfma16(vop, Pt, acc[nb]);
   }
 }
 
@@ -222,7 +227,7 @@ __device__ __forceinline__ void walk_pages(const AttnArgs &a, int b, int j, int 
     const float scb = (KVT == 2) ? lane_value(ksc_l, lbc) * rs : rs;
     const float vsa = (KVT == 2) ? lane_value(vsc_l, la) : 1.f;
     const float vsb = (KVT == 2) ? lane_value(vsc_l, lbc) : 1.f;
-    online_step<D, decltype(maskv)::value>(KA, KB, VA, VB, q0, q1, q2, ok, sca, scb, vsa, vsb,
+    online_step<D, decltype(maskv)::value, KVT == 3 ? 3 : 2>(KA, KB, VA, VB, q0, q1, q2, ok, sca, scb, vsa, vsb,
                                            m_run, l_run, acc);
   };
   // a branch-free loop over an even number of pairs: the pair past the end (if any) is fully
@@ -566,7 +571,7 @@ __global__ __launch_bounds__(64 * kPrefixWaves) void k_prefix_mx(AttnArgs a) {
     const float scb = (KVT == 2) ? lane_value(ksc_l, lbc) * rs : rs;
     const float vsa = (KVT == 2) ? lane_value(vsc_l, la) : 1.f;
     const float vsb = (KVT == 2) ? lane_value(vsc_l, lbc) : 1.f;
-    online_step<D>(KA, KB, VA, VB, qhi, qmd, qlo, ok, sca, scb, vsa, vsb, m_run, l_run, acc);
+    online_step<D, true, KVT == 3 ? 3 : 2>(KA, KB, VA, VB, qhi, qmd, qlo, ok, sca, scb, vsa, vsb, m_run, l_run, acc);
     if (pp + 1 < npairs) stash(buf ^ 1, next);
     __syncthreads();
   };
