@@ -7,6 +7,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <algorithm>
 #include <exception>
 #include <mutex>
 #include <new>
@@ -227,7 +228,15 @@ static kvprm_status plan_for(const kvprm_handle h, const kvprm_batch *b, int ran
 // H = 256, 8 candidates: 300 tokens fp8 29.5 / 34.3 us, bf16 29.4 / 32.6, 512 tokens 31.0 / 32.8,
 // fp32 100 tokens 27.0 / 28.8 but 512 32.7 / 30.1; H = 1024 with 8 kv-heads, 100 tokens, 256 blocks
 // 46.9 / 49.0 but 512 blocks 61.3 / 58.6; 7B shape, 64 candidates of 300 148.8 / 154.8.
+// A 4-bit page takes a wave half the time of a bf16 one to load but the same to compute, and more blocks leave the
+// chunk kernel less to gain: up to 36 pages and 3 more for 8 blocks. One launch / chunks and merge, us: 1 candidate, 8
+// kv-heads of 128: 32 pages 8.4 / 10.1, 48 9.9 / 9.9, 80 12.3 / 9.8; 64 blocks: 48 10.0 / 10.6, 64 11.0 / 11.1, 80 12.6 /
+// 12.0; 256 blocks: 48 11.4 / 15.5, 128 18.0 / 23.3; d_h = 64, 256 blocks: 128 14.4 / 20.2, 64 blocks: 96 11.8 / 11.4.
 constexpr int kShortBlocks = 256;
+static int short_pages(const Dims &dm, int blocks) {
+  if (dm.kvdt == 3) return std::min(kShortPages4, 36 + blocks * 3 / 8);
+  return dm.kvdt == 0 ? kShortWaves : kShortPages;
+}
 
 // Launch table of the attention kernels. The prefix-sharing hint is used by the matrix-core
 // attention only (the fp32 attention reads every page per candidate), only for up to kMaxGroups
@@ -287,7 +296,7 @@ static GroupTable group_table(const kvprm_handle h, const kvprm_batch *b, const 
     if (priv[i] > longest) longest = priv[i];
   }
   // (a prefix group's shared pages are read by the chunk kernels)
-  gt.one_launch = gt.n == 0 && longest <= (h->dm.kvdt == 0 ? kShortWaves : kShortPages) &&
+  gt.one_launch = gt.n == 0 && longest <= short_pages(h->dm, b->batch * h->dm.nkv) &&
                   b->batch * h->dm.nkv <= kShortBlocks;
   return gt;
 }

@@ -196,25 +196,27 @@ __device__ __forceinline__ void walk_pages(const AttnArgs &a, int b, int j, int 
     vsc_l = a.vsc[(size_t)ph_l * nkv + j];
   }
   const int npairs = (np + 1) >> 1;
-  auto load_pair = [&](int pp, PairOf<KVT, D> &r) {
+  auto load_pair = [&](int pp, PairRaw<D> &r) {
     // indices past the chunk are clamped to its last page: those tokens are masked anyway
     const int pa = lane_value(ph_l, min(2 * pp, np - 1));
     const int pb = lane_value(ph_l, min(2 * pp + 1, np - 1));
-    load_pair_of<KVT, D, true>(a.kp + ((size_t)pa * nkv + j) * TILE, a.kp + ((size_t)pb * nkv + j) * TILE,
-                               a.vp + ((size_t)pa * nkv + j) * TILE, a.vp + ((size_t)pb * nkv + j) * TILE, lane, r);
+    load_pair_raw<KVT, D, true>((const uint4 *)(a.kp + ((size_t)pa * nkv + j) * TILE),
+                          (const uint4 *)(a.kp + ((size_t)pb * nkv + j) * TILE),
+                          (const uint4 *)(a.vp + ((size_t)pa * nkv + j) * TILE),
+                          (const uint4 *)(a.vp + ((size_t)pb * nkv + j) * TILE), lane, r);
   };
-  PairOf<KVT, D> r0, r1;
+  PairRaw<D> r0, r1;
   load_pair(0, r0);
   __builtin_amdgcn_sched_barrier(0);
   uint4 q0[NKB], q1[NKB], q2[NKB];
   query_ops<D>(qraw, colv, q0, q1, q2);
   const float rs = kLog2e / sqrtf((float)D);  // scores in log2 units
-  auto compute_pair = [&](int pp, const PairOf<KVT, D> &r, auto maskv) {
+  auto compute_pair = [&](int pp, const PairRaw<D> &r, auto maskv) {
     const int la = min(2 * pp, np - 1), lb = 2 * pp + 1;
     const bool hasA = 2 * pp < np, hasB = lb < np;
     uint4 KA[NKB], KB[NKB];
     uint2 VA[NDB], VB[NDB];
-    unpack_pair_of<KVT, D>(r, KA, KB, VA, VB);
+    unpack_pair<KVT, D>(r, KA, KB, VA, VB);
     const int ta = (p0 + la) * kPage + 4 * cq, tb = (p0 + lb) * kPage + 4 * cq;
     bool ok[8];
 #pragma unroll
@@ -227,7 +229,7 @@ __device__ __forceinline__ void walk_pages(const AttnArgs &a, int b, int j, int 
     const float scb = (KVT == 2) ? lane_value(ksc_l, lbc) * rs : rs;
     const float vsa = (KVT == 2) ? lane_value(vsc_l, la) : 1.f;
     const float vsb = (KVT == 2) ? lane_value(vsc_l, lbc) : 1.f;
-    online_step<D, decltype(maskv)::value, KVT == 3 ? 3 : 2>(KA, KB, VA, VB, q0, q1, q2, ok, sca, scb, vsa, vsb,
+    online_step<D, decltype(maskv)::value>(KA, KB, VA, VB, q0, q1, q2, ok, sca, scb, vsa, vsb,
                                            m_run, l_run, acc);
   };
   // a branch-free loop over an even number of pairs: the pair past the end (if any) is fully
@@ -252,10 +254,272 @@ __device__ __forceinline__ void walk_pages(const AttnArgs &a, int b, int j, int 
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  if (KVT >= 2 && p0 + np < npages)
+  if (KVT == 2 && p0 + np < npages)
     chunk_loop(std::integral_constant<bool, false>{});
   else
     chunk_loop(std::integral_constant<bool, true>{});
+}
+
+// ---- 4-bit caches
+
+// walk_pages over a 4-bit cache. Scores come from the matrix cores' scaled products of 4-bit keys as they lie in memory (16
+// tokens x 128 dims, a scale byte per lane: its 32 dims of its token) and the query in terms of 6 bits (e2m3), each with
+// a power of two for the lane's 32 dims: kTerms4 terms, each 2^-4 of the one before, keep 2^-20 of the 32 dims' largest.
+// (Such a product takes the time of a bf16 one of 32 dims, so that five terms cost 5/12 of three bf16 terms', and no
+// conversion of keys. 8-bit terms keep no more bits and take twice the time.) At d_h = 64 a product holds two terms, one in
+// lanes 0 to 31 and one in the others, which read the same keys. Values become bf16 (exactly) for bf16 products with
+// weights in three terms. A step without a new maximum does not touch acc; slots at or past L are masked in the
+// chunk's last pair alone.
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+constexpr int kTerms4 = 5;
+
+template <int D>
+struct Query4 {
+  static constexpr int NQ = D == 128 ? kTerms4 : (kTerms4 + 1) / 2;  // products
+  uint32_t t[NQ][6];
+  uint32_t scale[2];  // bytes: of products 0 to 3, and of the fourth
+};
+
+// The terms of a column's query (`present`: it exists) times `factor`, for this lane's 32 dims. A query that is not finite
+// gets scales that make its scores NaN.
+template <int D>
+__device__ __forceinline__ void query_terms4(const float *qr, bool present, float factor, int lane, Query4<D> &q) {
+  typedef float f32x16 __attribute__((ext_vector_type(16)));
+  typedef float f32x32 __attribute__((ext_vector_type(32)));
+  typedef uint32_t u32x6 __attribute__((ext_vector_type(6)));
+  constexpr int TERMS = D == 128 ? Query4<D>::NQ : 2 * Query4<D>::NQ;
+  const float *p = qr + 32 * (D == 128 ? lane >> 4 : lane >> 4 & 1);
+  f32x16 even, odd;
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const f32x4u v = *(const f32x4u *)(p + 4 * i);
+    even[2 * i] = present ? v[0] * factor : 0.f;
+    odd[2 * i] = present ? v[1] * factor : 0.f;
+    even[2 * i + 1] = present ? v[2] * factor : 0.f;
+    odd[2 * i + 1] = present ? v[3] * factor : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    top = max(top, max(__float_as_uint(even[i]) & 0x7FFFFFFFu, __float_as_uint(odd[i]) & 0x7FFFFFFFu));
+  // the smallest power of two s with 7.5 s >= the largest (7.5 = 1.875 * 2^2), kept where every term's scale is one
+  int e = max((int)(top >> 23) - 2 + ((top & 0x7FFFFFu) > 0x700000u), 4 * TERMS);
+  uint32_t bytes[TERMS];
+  u32x6 term[TERMS];
+#pragma unroll
+  for (int k = 0; k < TERMS; ++k) {
+    const float s = __uint_as_float((uint32_t)(e - 4 * k) << 23);
+    bytes[k] = top >= 0x7F800000u ? 255u : (uint32_t)(e - 4 * k);
+    term[k] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, s);  // even and odd dims side by side
+    if (k + 1 == TERMS) break;
+    const f32x32 back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(term[k], s);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) even[i] -= back[2 * i], odd[i] -= back[2 * i + 1];
+  }
+  const bool second = D == 64 && (lane >> 5);
+  q.scale[0] = q.scale[1] = 0;
+#pragma unroll
+  for (int k = 0; k < Query4<D>::NQ; ++k) {
+    const uint32_t b = D == 128 ? bytes[k] : second ? bytes[2 * k + 1] : bytes[2 * k];
+    q.scale[k >> 2] |= b << 8 * (k & 3);
+#pragma unroll
+    for (int i = 0; i < 6; ++i) q.t[k][i] = D == 128 ? term[k][i] : second ? term[2 * k + 1][i] : term[2 * k][i];
+  }
+}
+
+template <int D, int K>
+__device__ __forceinline__ floatx4 score_term4(const uint4 &key, uint32_t scale, const Query4<D> &q, const floatx4 &c) {
+  const i32x8 a = {(int)key.x, (int)key.y, (int)key.z, (int)key.w, 0, 0, 0, 0};
+  const i32x8 b = {(int)q.t[K][0], (int)q.t[K][1], (int)q.t[K][2], (int)q.t[K][3], (int)q.t[K][4], (int)q.t[K][5], 0, 0};
+  // (formats 4: e2m1, 2: e2m3)
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, 2, 0, (int)scale, K & 3, (int)q.scale[K >> 2]);
+}
+template <int D>
+__device__ __forceinline__ floatx4 scores4(const uint4 &key, uint32_t scale, const Query4<D> &q) {
+  floatx4 c = {0.f, 0.f, 0.f, 0.f};
+  c = score_term4<D, 0>(key, scale, q, c);
+  c = score_term4<D, 1>(key, scale, q, c);
+  c = score_term4<D, 2>(key, scale, q, c);
+  if constexpr (D == 128) {
+    c = score_term4<D, 3>(key, scale, q, c);
+    c = score_term4<D, 4>(key, scale, q, c);
+  }
+  return c;
+}
+static_assert(kTerms4 == 5, "products of scores4");
+
+// A page pair in registers: key codes of a slot's 32 dims and their scale, value codes and scales as in PairRaw4.
+template <int D>
+struct Pair4 {
+  uint4 k[2], v[2], vs[2];
+  uint32_t ks[2];
+};
+
+template <int D>
+__device__ __forceinline__ void walk_pages4(const AttnArgs &a, int b, int j, int L, int p0, int np, const float *qr,
+                                            bool colv, float &m_run, float &l_run, floatx4 (&acc)[D / 16]) {
+  constexpr int NDB = D / 16;
+  constexpr size_t TILE = tile_bytes(3, D);
+  const int nkv = a.nkv;
+  const int lane = threadIdx.x & 63, cq = lane >> 4;
+  const int ph_l = a.page_table[(size_t)b * a.max_pages + p0 + min(lane, np - 1)];
+  const int cell = D == 128 ? lane : lane & 31;  // (32 dims, slot)
+  // (indices past the chunk are clamped to its last page: those tokens are masked anyway)
+  auto tile = [&](int p) { return ((size_t)lane_value(ph_l, min(p, np - 1)) * nkv + j) * TILE; };
+  auto load_pair = [&](int pp, Pair4<D> &r) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const size_t t = tile(2 * pp + x);
+      r.k[x] = ld_stream((const uint4 *)(a.kp + t) + cell);
+      r.ks[x] = *(const uint8_t *)(a.kp + t + 8 * D + cell);
+      r.v[x] = load_bytes<D / 8, true>(a.vp + t + value_code4<D>(lane));
+      r.vs[x] = load_bytes<D / 8, false>(a.vp + t + value_scale4<D>(lane));
+    }
+  };
+  Pair4<D> r0, r1;
+  load_pair(0, r0);
+  load_pair(1, r1);
+  __builtin_amdgcn_sched_barrier(0);
+  Query4<D> q;
+  query_terms4<D>(qr, colv, kLog2e / sqrtf((float)D), lane, q);  // scores in log2 units
+  auto compute = [&](int pp, const Pair4<D> &r, auto tail) {
+    constexpr bool TAIL = decltype(tail)::value;
+    const floatx4 sa = scores4<D>(r.k[0], r.ks[0], q), sb = scores4<D>(r.k[1], r.ks[1], q);
+    float s[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = sa[i], s[4 + i] = sb[i];
+    uint32_t mk[4];
+    if (TAIL) {
+      // this lane's tokens, 0 .. 3 of page A and 16 .. 19 of page B, before the chunk's and the cache's end
+      const int left = min(L, (p0 + np) * kPage) - (p0 + 2 * pp) * kPage - 4 * cq;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[i] = left > i ? s[i] : -INFINITY;
+        s[4 + i] = left > 16 + i ? s[4 + i] : -INFINITY;
+        const int t = (i >> 1) * 16 + 2 * (i & 1);
+        mk[i] = (left > t ? 0xFFFFu : 0u) | (left > t + 1 ? 0xFFFF0000u : 0u);
+      }
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[i]);
+    mx = column_max(mx);
+    if (__any(mx > m_run)) {
+      const float mn = fmaxf(m_run, mx), alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - mn);
+      m_run = mn;
+      l_run *= alpha;
+#pragma unroll
+      for (int nb = 0; nb < NDB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[nb][i] *= alpha;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      s[i] = __builtin_amdgcn_exp2f(s[i] - m_run);
+      l_run += s[i];
+    }
+    uint32_t p0_[4], p1_[4], p2_[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split3(s[2 * i], s[2 * i + 1], p0_[i], p1_[i], p2_[i]);
+    const uint4 P0 = make_uint4(p0_[0], p0_[1], p0_[2], p0_[3]), P1 = make_uint4(p1_[0], p1_[1], p1_[2], p1_[3]);
+    const uint4 P2 = make_uint4(p2_[0], p2_[1], p2_[2], p2_[3]);
+#pragma unroll
+    for (int g = 0; g < D / 32; ++g) {
+      uint2 A[2], B[2];
+      values4(word(r.v[0], g), word(r.vs[0], g), A[0], A[1]);
+      values4(word(r.v[1], g), word(r.vs[1], g), B[0], B[1]);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint4 v = make_uint4(A[h].x, A[h].y, B[h].x, B[h].y);
+        if (TAIL) v = make_uint4(v.x & mk[0], v.y & mk[1], v.z & mk[2], v.w & mk[3]);
+        floatx4 &o = acc[2 * g + h];
+        o = mfma16(v, P0, o);
+        o = mfma16(v, P1, o);
+        o = mfma16(v, P2, o);
+      }
+    }
+  };
+  // pairs without a slot at or past the end; the last one may have some
+  const int last = ((np + 1) >> 1) - 1;
+  auto step = [&](int pp, Pair4<D> &r) {
+    compute(pp, r, std::integral_constant<bool, false>{});
+    __builtin_amdgcn_sched_barrier(0);
+    load_pair(pp + 2, r);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  int pp = 0;
+  for (; pp + 2 <= last; pp += 2) {
+    step(pp, r0);
+    step(pp + 1, r1);
+  }
+  if (pp < last) {
+    compute(pp, r0, std::integral_constant<bool, false>{});
+    r0 = r1;
+  }
+  compute(last, r0, std::integral_constant<bool, true>{});
+}
+
+// Which candidate and chunk block `id` of the private pages' grid has (see k_attn_mx), its length and shared pages.
+struct ChunkItem {
+  int b, c, L, first;
+};
+template <bool ONE>
+__device__ __forceinline__ bool chunk_item(const AttnArgs &a, int id, ChunkItem &it) {
+  const int lane = threadIdx.x & 63;
+  it = {0, id, 0, 0};
+  if constexpr (ONE) {
+    it.L = a.lengths[0];
+    if (a.gt.n > 0) it.first = a.gt.prefix_pages[0];
+    return true;
+  }
+  // lane i: candidate i's length, shared pages and full private chunks
+  const int bl = min(lane, a.B - 1);
+  const int L_l = a.lengths[bl];
+  int first_l = 0;
+  for (int gi = 0; gi < a.gt.n; ++gi)
+    if (bl * a.kq >= a.gt.start[gi] && bl * a.kq < a.gt.start[gi + 1]) first_l = a.gt.prefix_pages[gi];
+  const int full_l =
+      lane < a.B ? max(0, (L_l + kPage - 1) / kPage - first_l) >> a.gt.cshift_private : 0;
+  const int cum_l = lane_scan(full_l);
+  const int total = __builtin_amdgcn_readlane(cum_l, 63);
+  if (id < total) {
+    it.b = __builtin_popcountll(__ballot(id >= cum_l));
+    it.c = id - (__builtin_amdgcn_readlane(cum_l, it.b) - __builtin_amdgcn_readlane(full_l, it.b));
+  } else {
+    it.b = id - total;
+    if (it.b >= a.B) return false;
+    it.c = __builtin_amdgcn_readlane(full_l, it.b);
+  }
+  it.L = __builtin_amdgcn_readlane(L_l, it.b);
+  it.first = __builtin_amdgcn_readlane(first_l, it.b);
+  return true;
+}
+
+// k_attn_mx over a 4-bit cache.
+template <int D, bool ONE>
+__global__ __launch_bounds__(64 * kMaxKvHeadsMx, 2) void k_attn4(AttnArgs a) {
+  constexpr int NDB = D / 16;
+  const int j =
+      __builtin_amdgcn_readfirstlane((int)(blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6)));
+  const int lane = threadIdx.x & 63, n = lane & 15, cq = lane >> 4;
+  ChunkItem it;
+  if (!chunk_item<ONE>(a, blockIdx.y, it)) return;
+  const bool colv = n < a.kq * a.g;
+  const int ti = colv ? (n * a.ginv) >> 16 : 0, hh = colv ? n - ti * a.g : 0;
+  const size_t head = ((size_t)it.b * a.kq + ti) * a.nq + (size_t)j * a.g + hh;
+  const int npages = (it.L + kPage - 1) / kPage;
+  const int ncp = (it.first + (1 << a.gt.cshift_prefix) - 1) >> a.gt.cshift_prefix;  // prefix chunks
+  const int p0 = it.first + (it.c << a.gt.cshift_private);
+  // (a device length above its host mirror must not reach past the candidate's slots)
+  if (p0 >= npages || ncp + it.c >= a.nch) return;
+  const int np = min(npages - p0, 1 << a.gt.cshift_private);
+  float m_run = -INFINITY, l_run = 0.f;
+  floatx4 acc[NDB];
+#pragma unroll
+  for (int nb = 0; nb < NDB; ++nb) acc[nb] = floatx4{0.f, 0.f, 0.f, 0.f};
+  walk_pages4<D>(a, it.b, j, it.L, p0, np, a.q + head * D, colv, m_run, l_run, acc);
+  l_run = column_sum(l_run);
+  if (colv) store_partial<D>(a.apart + (head * a.nch + ncp + it.c) * (D + 2), cq, acc, m_run, l_run);
 }
 
 // One wave per kv-head j and chunk of a candidate's private pages, over the whole batch; it writes its
@@ -445,7 +709,7 @@ __global__ __launch_bounds__(64 * kShortWaves) void k_attn_short(AttnArgs a) {
     s = column_sum(s) * rs;
     if (cq == 0) st.sself[i][n] = s;
   }
-  const int npages = min((L + kPage - 1) / kPage, kShortPages);
+  const int npages = min((L + kPage - 1) / kPage, KVT == 3 ? kShortPages4 : kShortPages);
   const int per = (npages + kShortWaves - 1) / kShortWaves;
   const int p0 = w * per, np = min(npages - p0, per);
   float m_run = -INFINITY, l_run = 0.f;
@@ -453,7 +717,11 @@ __global__ __launch_bounds__(64 * kShortWaves) void k_attn_short(AttnArgs a) {
 #pragma unroll
   for (int nb = 0; nb < NDB; ++nb) acc[nb] = floatx4{0.f, 0.f, 0.f, 0.f};
   if (np > 0) {  // wave-uniform
-    walk_pages<KVT, D>(a, b, j, L, npages, p0, np, qraw, colv, m_run, l_run, acc);
+    if constexpr (KVT == 3)
+      walk_pages4<D>(a, b, j, L, p0, np, a.q + (((size_t)b * kq + ti) * nq + (size_t)j * g + hh) * D, colv, m_run, l_run,
+                     acc);
+    else
+      walk_pages<KVT, D>(a, b, j, L, npages, p0, np, qraw, colv, m_run, l_run, acc);
     l_run = column_sum(l_run);
   }
   finish_short<D>(a, b, j, st, np > 0, m_run * kLn2, l_run, acc);
@@ -804,10 +1072,12 @@ hipError_t launch_attn_mx(const Dims &dm, const Plan &p, const Workspace &w, con
       KVPRM_A(1, 128);
     }
   } else if (dm.kvdt == 3) {
-    if (dm.d == 64) {
-      KVPRM_A(3, 64);
+    if (p.Breal == 1) {
+      if (dm.d == 64) hipLaunchKernelGGL((k_attn4<64, true>), grid, dim3(64 * hpb), 0, s, a);
+      else hipLaunchKernelGGL((k_attn4<128, true>), grid, dim3(64 * hpb), 0, s, a);
     } else {
-      KVPRM_A(3, 128);
+      if (dm.d == 64) hipLaunchKernelGGL((k_attn4<64, false>), grid, dim3(64 * hpb), 0, s, a);
+      else hipLaunchKernelGGL((k_attn4<128, false>), grid, dim3(64 * hpb), 0, s, a);
     }
   } else {
     if (dm.d == 64) {

@@ -146,18 +146,19 @@ __device__ __forceinline__ void load_pair_raw4(const char *kA, const char *kB, c
   r.vs[1] = load_bytes<N, false>(vB + value_scale4<D>(lane));
 }
 
-// Two e2m1 codes (byte B of w) -> two bf16, times the power of two `scale` (its exponent is used): exact up to
-// scales of 2^125; an exponent of all ones (scale byte 255) gives NaN.
+// Two e2m1 codes (byte B of w) -> two bf16, times a power of two. The instruction takes the exponent of `scale` alone,
+// whatever its sign and significand; the product is exact up to 2^125, and an exponent of all ones (scale byte 255)
+// gives NaN.
 template <int B>
 __device__ __forceinline__ uint32_t fp4x2_to_bf16x2(uint32_t w, float scale) {
   typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
   const bf16x2v v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, B);
   return __builtin_bit_cast(uint32_t, v);
 }
-// Byte B of w, a scale's biased exponent, as the power of two it stands for.
+// A float whose exponent is byte B of w (a scale's biased exponent), for the conversions: other bits are w's.
 template <int B>
 __device__ __forceinline__ float scale_of(uint32_t w) {
-  return __uint_as_float(B == 3 ? w >> 1 & 0x7F800000u : B == 0 ? w << 23 : w << (23 - 8 * B) & 0x7F800000u);
+  return __uint_as_float(B == 3 ? w >> 1 : w << (23 - 8 * B));
 }
 // The codes of 8 dims of a slot -> bf16.
 __device__ __forceinline__ uint4 keys4(uint32_t w, float scale) {

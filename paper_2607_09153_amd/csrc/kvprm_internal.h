@@ -42,6 +42,7 @@ constexpr int kMaxChunks = 1024;  // chunk partials one merge handles
 constexpr int kMaxKvHeadsMx = 8;  // kv-heads with bf16 and fp8 caches
 constexpr int kFineChunks = 128;  // chunks of one candidate at most, in chunks under 16 pages
 constexpr int kShortPages = 32;   // longest cache of the one-launch attention
+constexpr int kShortPages4 = 128;  // ... in 4 bits (fewer by short_pages)
 constexpr int kShortWaves = 8;    // its waves per block
 constexpr int kMaxBatch = 256;    // candidates of a call
 constexpr int kPage = 16;

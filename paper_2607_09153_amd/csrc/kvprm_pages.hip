@@ -395,7 +395,334 @@ __global__ __launch_bounds__(256) void k_compact_move(PageArgs a) {
   }
 }
 
+// ------------------------------------------------------------------------------- one launch
+
+// Pools of up to kOnePages pages: one launch, whose blocks, one to a compute unit, each form the whole plan in LDS from the
+// counts and tables (read from the caches, each for itself), then write their share of the results and copy their
+// share of the pages. Nothing that a block reads is written by another, so that no block waits for one. Against the
+// launches above, whose plan is spread over the blocks: a beam of 64 rows of 300 pages in a pool of 2048, 31 copies of
+// 917 KB: XX us instead of 40; 4 rows of 10 pages: XX instead of 20.
+constexpr int kOnePages = 16384, kOneThreads = 1024;
+constexpr int64_t kOneEntries = 1 << 17;  // entries of the rows
+
+// Flags of the pool's pages as words in LDS, with the flags before each word, for selecting by rank.
+struct WordScan {
+  uint64_t *mask;   // [words]
+  int32_t *before;  // [words]
+  int words;
+};
+// Exclusive sums of the words' bits; returns their number. Every thread of the block calls it.
+__device__ __forceinline__ int scan_words(const WordScan &s) {
+  __shared__ int all_s;
+  const int tid = threadIdx.x;
+  __syncthreads();
+  if (tid < 64) {
+    int sum = 0;
+    for (int i0 = 0; i0 < s.words; i0 += 64) {
+      const int i = i0 + tid, n = i < s.words ? __popcll(s.mask[i]) : 0, cum = lane_scan(n);
+      if (i < s.words) s.before[i] = sum + cum - n;
+      sum += __builtin_amdgcn_readlane(cum, 63);
+    }
+    if (tid == 0) all_s = sum;
+  }
+  __syncthreads();
+  return all_s;
+}
+// Bit k of m's set ones.
+__device__ __forceinline__ int select_bit(uint64_t m, int k) {
+  int at = 0;
+#pragma unroll
+  for (int width = 32; width > 0; width >>= 1) {  // the half that holds it
+    const int low = __popcll(m & ((1ull << width) - 1));
+    if (k >= low) k -= low, m >>= width, at += width;
+  }
+  return at;
+}
+// The k-th page whose flag is set (NOT: is not set; every word's pages count).
+template <bool NOT = false>
+__device__ __forceinline__ int select_word(const WordScan &s, int k) {
+  int a = 0, b = s.words - 1;  // the last word with at most k before it
+  while (a < b) {
+    const int mid = (a + b + 1) / 2;
+    if ((NOT ? 64 * mid - s.before[mid] : s.before[mid]) <= k) a = mid;
+    else b = mid - 1;
+  }
+  const uint64_t m = NOT ? ~s.mask[a] : s.mask[a];
+  return 64 * a + select_bit(m, k - (NOT ? 64 * a - s.before[a] : s.before[a]));
+}
+__device__ __forceinline__ int rank_word(const WordScan &s, int page) {
+  return s.before[page >> 6] + __popcll(s.mask[page >> 6] & ((1ull << (page & 63)) - 1));
+}
+
+// f(row, entry, id) for every entry that a row holds; held: the rows' counts, in range. Eight loads in flight a thread.
+template <typename F>
+__device__ __forceinline__ void each_entry(const PageArgs &a, const int32_t *held, F f) {
+  constexpr int U = 8;
+  const uint32_t total = (uint32_t)(a.rows * a.max_pages);  // (at most kOneEntries)
+  for (uint32_t e0 = threadIdx.x; e0 < total; e0 += U * kOneThreads) {
+    int id[U], row[U], c[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t e = min(e0 + u * kOneThreads, total - 1);
+      row[u] = (int)(e / (uint32_t)a.max_pages);
+      c[u] = (int)(e - (uint32_t)row[u] * a.max_pages);
+      if (e0 + u * kOneThreads >= total || c[u] >= held[row[u]]) c[u] = -1;
+      id[u] = a.table[e];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (c[u] >= 0) f(row[u], c[u], id[u]);
+  }
+}
+
+// Pages src[i] -> dst[i] of every layer, keys and values, spread over all threads of the grid in pieces of 16 bytes,
+// two of them in flight a thread (I: a type that counts them). Past the caches both ways: 485 pages of 917 KB (890 MB
+// moved) 269 us through them, 185 past them; four or eight in flight 189 and 196, each block a range of its own 192.
+template <typename I>
+__device__ __forceinline__ void copy_pieces(const PageArgs &a, const int32_t *src, const int32_t *dst, I total) {
+  constexpr int U = 2;
+  const uint32_t per = (uint32_t)(a.page_bytes / 16);
+  const I threads = (I)gridDim.x * kOneThreads;
+  for (I e0 = (I)blockIdx.x * kOneThreads + threadIdx.x; e0 < total; e0 += U * threads) {
+    uint4 v[U];
+    uint4 *to[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const I e = min(e0 + u * threads, total - 1);
+      const uint32_t unit = (uint32_t)(e / per), at = (uint32_t)(e - (I)unit * per);
+      const uint32_t i = unit / (2 * a.layers), lp = unit - i * 2 * a.layers;
+      char *pool = a.pool[lp & 1];
+      const size_t base = (size_t)(lp >> 1) * a.num_pages;
+      v[u] = ld_stream((const uint4 *)(pool + (base + src[i]) * a.page_bytes) + at);
+      to[u] = (uint4 *)(pool + (base + dst[i]) * a.page_bytes) + at;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (e0 + u * threads < total)
+        __builtin_nontemporal_store(u32x4{v[u].x, v[u].y, v[u].z, v[u].w}, (u32x4 *)to[u]);
+  }
+}
+__device__ __forceinline__ void copy_pages(const PageArgs &a, const int32_t *src, const int32_t *dst, int n) {
+  const uint64_t total = (uint64_t)n * 2 * a.layers * (a.page_bytes / 16);
+  const int64_t threads = (int64_t)gridDim.x * kOneThreads;
+  if (total < 1u << 31) copy_pieces<uint32_t>(a, src, dst, (uint32_t)total);
+  else copy_pieces<uint64_t>(a, src, dst, total);
+  if (!a.scale[0]) return;
+  const int64_t scales = (int64_t)n * 2 * a.layers * a.nkv;
+  for (int64_t e = (int64_t)blockIdx.x * kOneThreads + threadIdx.x; e < scales; e += threads) {
+    const int unit = (int)(e / a.nkv), h = (int)(e - (int64_t)unit * a.nkv), i = unit / (2 * a.layers), lp = unit - i * 2 * a.layers;
+    float *pool = a.scale[lp & 1];
+    const size_t base = (size_t)(lp >> 1) * a.num_pages;
+    pool[(base + dst[i]) * a.nkv + h] = pool[(base + src[i]) * a.nkv + h];
+  }
+}
+
+__global__ __launch_bounds__(kOneThreads) void k_fork_one(PageArgs a) {
+  extern __shared__ uint64_t lds[];
+  const int P = a.num_pages, words = (P + 63) / 64, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  // per page: the rows of `from` that hold it (low half) and those of `to` that share it
+  uint64_t *count = lds, *mask = count + P;
+  int32_t *before = (int32_t *)(mask + words);
+  uint64_t *source = (uint64_t *)(before + ((words + 1) & ~1));
+  __shared__ RowPlan row_s[kMaxBatch];
+  __shared__ int first_s[kMaxBatch + 1];                    // fresh pages of the rows before
+  __shared__ int child_s[kMaxBatch], eldest_s[kMaxBatch];   // of a row of `from`: its children, the first of them
+  __shared__ int full_s[kMaxBatch], kept_s[kMaxBatch];      // its full pages; whether a child takes the next one
+  __shared__ int src_s[kMaxBatch], dst_s[kMaxBatch];
+  __shared__ int held_s[kMaxBatch];
+  __shared__ int bad_s, empty_s, copies_s;
+  bool bad = false;
+  if (tid < a.rows) {
+    const int held = a.held[tid];
+    bad = held < 0 || held > a.max_pages;
+    held_s[tid] = bad ? 0 : held;
+  }
+  for (int i = tid; i < P; i += kOneThreads) count[i] = 0;
+  for (int i = tid; i < words; i += kOneThreads) source[i] = 0;
+  if (tid < kMaxBatch) child_s[tid] = kept_s[tid] = full_s[tid] = 0, eldest_s[tid] = kMaxBatch;
+  if (tid == 0) bad_s = empty_s = copies_s = 0;
+  __syncthreads();
+  const int i = tid;
+  const int p = i < a.children ? a.parent[i] : -1;
+  bad = bad || p >= a.rows;
+  if (p >= 0 && p < a.rows) {
+    atomicAdd(&child_s[p], 1);
+    atomicMin(&eldest_s[p], i);
+  }
+  __syncthreads();
+  if (i < a.children) {
+    RowPlan r = {0, 0, 0, -1};
+    const int64_t room = a.room ? a.room[i] : 0;
+    bad = bad || room < 0;
+    if (p >= 0 && !bad) {
+      r.len = a.lengths[p];
+      bad = r.len < 0 || r.len > (int64_t)held_s[p] * kPage;
+    }
+    const int64_t want = (r.len + room + kPage - 1) / kPage;
+    bad = bad || want > a.to_pages;
+    if (!bad) {
+      r.held = (int)want;
+      r.shared = r.len / kPage;
+      if (p >= 0) full_s[p] = r.shared;  // (the same for all its children)
+      if (r.len % kPage) {
+        const int last = a.table[(size_t)p * a.max_pages + r.shared];
+        if (last < 0 || last >= P) {
+          bad = true;
+        } else if (eldest_s[p] == i && a.refs[last] == 1) {
+          ++r.shared;
+          kept_s[p] = 1;
+        } else {
+          r.copy = last;
+          atomicOr((unsigned long long *)&source[last >> 6], 1ull << (last & 63));
+        }
+      }
+    }
+    row_s[i] = r;
+  }
+  if (bad) bad_s = 1;
+  __syncthreads();
+  if (bad_s) {
+    if (blockIdx.x == 0 && tid < 4) a.result[tid] = tid == 0 ? 2 : 0;
+    return;
+  }
+  each_entry(a, held_s, [&](int row, int c, int id) {
+    const uint64_t share = c < full_s[row] ? child_s[row] : c == full_s[row] ? kept_s[row] : 0;
+    if (id < 0 || id >= P) bad = true;
+    else atomicAdd((unsigned long long *)&count[id], (unsigned long long)(share << 32 | 1));
+  });
+  __syncthreads();
+  int empty = 0;
+  for (int word = wave; word < words; word += kOneThreads / 64) {
+    const int page = word * 64 + lane;
+    bool free = false;
+    if (page < P) {
+      const int64_t others = (int64_t)a.refs[page] - (uint32_t)count[page], n = others + (int64_t)(count[page] >> 32);
+      bad = bad || others < 0 || n > INT32_MAX;
+      empty += n == 0;
+      free = n == 0 && !(source[word] >> lane & 1);
+      count[page] = (uint64_t)n;
+    }
+    const uint64_t m = __ballot(free);
+    if (lane == 0) mask[word] = m;
+  }
+  empty = lane_scan(empty);
+  if (lane == 63 && empty) atomicAdd(&empty_s, empty);
+  if (bad) bad_s = 1;
+  const WordScan ws = {mask, before, words};
+  const int have = scan_words(ws);
+  if (tid < 64) {
+    int sum = 0;
+    for (int i0 = 0; i0 < a.children; i0 += 64) {
+      const int c = i0 + tid, n = c < a.children ? row_s[c].held - row_s[c].shared : 0, cum = lane_scan(n);
+      if (c < a.children) first_s[c] = sum + cum - n;
+      sum += __builtin_amdgcn_readlane(cum, 63);
+    }
+    if (tid == 0) first_s[a.children] = sum;
+  }
+  __syncthreads();
+  const int need = first_s[a.children], status = bad_s ? 2 : need > have ? 1 : 0;
+  if (blockIdx.x == 0 && tid == 0) {
+    a.result[0] = status;
+    a.result[1] = status == 2 ? 0 : need;
+    a.result[2] = status == 2 ? 0 : have;
+    a.result[3] = status ? 0 : empty_s - need;
+  }
+  if (status) return;
+  if (i < a.children && row_s[i].copy >= 0) {
+    const int k = atomicAdd(&copies_s, 1);  // (the order of the copies is of no effect)
+    src_s[k] = row_s[i].copy;
+    dst_s[k] = select_word(ws, first_s[i]);  // (the first fresh page of the row)
+  }
+  __syncthreads();
+  const int64_t threads = (int64_t)gridDim.x * kOneThreads, me = (int64_t)blockIdx.x * kOneThreads + tid;
+  for (int64_t e = me; e < (int64_t)a.children * a.to_pages; e += threads) {
+    const int row = (int)(e / a.to_pages), c = (int)(e - (int64_t)row * a.to_pages);
+    const RowPlan r = row_s[row];
+    int id = -1;
+    if (c < r.shared) id = a.table[(size_t)a.parent[row] * a.max_pages + c];
+    else if (c < r.held) id = select_word(ws, first_s[row] + c - r.shared);
+    a.to_table[e] = id;
+    if (c == 0) a.to_lengths[row] = r.len, a.to_held[row] = r.held;
+  }
+  for (int64_t page = me; page < P; page += threads) {
+    const bool free = mask[page >> 6] >> (page & 63) & 1;
+    a.new_refs[page] = free && rank_word(ws, (int)page) < need ? 1 : (int)count[page];
+  }
+  copy_pages(a, src_s, dst_s, copies_s);
+}
+
+__global__ __launch_bounds__(kOneThreads) void k_compact_one(PageArgs a) {
+  extern __shared__ uint64_t lds[];
+  const int P = a.num_pages, words = (P + 63) / 64, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  uint64_t *mask = lds;
+  int32_t *before = (int32_t *)(mask + words), *src = before + words, *dst = src + P / 2;
+  __shared__ int held_s[kMaxBatch];
+  __shared__ int bad_s;
+  if (tid == 0) bad_s = 0;
+  bool bad = false;
+  if (tid < a.rows) {
+    const int held = a.held[tid];
+    bad = held < 0 || held > a.max_pages;
+    held_s[tid] = bad ? 0 : held;
+  }
+  for (int word = wave; word < words; word += kOneThreads / 64) {
+    const int page = word * 64 + lane, n = page < P ? a.refs[page] : 0;
+    bad = bad || n < 0;
+    const uint64_t m = __ballot(n > 0);
+    if (lane == 0) mask[word] = m;
+  }
+  const WordScan ws = {mask, before, words};
+  const int live = scan_words(ws);
+  each_entry(a, held_s, [&](int, int, int id) {
+    bad = bad || id < 0 || id >= P || !(mask[id >> 6] >> (id & 63) & 1);
+  });
+  if (bad) bad_s = 1;
+  __syncthreads();
+  const int stay = live < P ? rank_word(ws, live) : live;  // live pages that keep their places
+  const int moves = live - stay, status = bad_s ? 2 : 0;
+  if (blockIdx.x == 0 && tid == 0) {
+    a.result[0] = status;
+    a.result[1] = status ? 0 : live;
+    a.result[2] = status ? 0 : moves;
+    a.result[3] = status ? 0 : P - live;
+  }
+  if (status) return;
+  for (int k = tid; k < moves; k += kOneThreads) {  // the i-th live page past the live ones' number, the i-th hole
+    src[k] = select_word(ws, stay + k);
+    dst[k] = select_word<true>(ws, k);
+  }
+  __syncthreads();
+  // (alive pages only)
+  auto goes = [&](int page) { return page < live ? page : dst[rank_word(ws, page) - stay]; };
+  const int64_t threads = (int64_t)gridDim.x * kOneThreads, me = (int64_t)blockIdx.x * kOneThreads + tid;
+  for (int64_t page = me; page < P; page += threads) {
+    const bool alive = mask[page >> 6] >> (page & 63) & 1;
+    const int to = alive ? goes((int)page) : -1;
+    a.moved[page] = to;
+    if (alive) a.new_refs[to] = a.refs[page];
+    if (page >= live) a.new_refs[page] = 0;
+  }
+  for (int64_t e = me; e < (int64_t)a.rows * a.max_pages; e += threads) {
+    const int row = (int)(e / a.max_pages), c = (int)(e - (int64_t)row * a.max_pages);
+    a.to_table[e] = c < held_s[row] ? goes(a.table[e]) : -1;
+  }
+  copy_pages(a, src, dst, moves);
+}
+
 // ------------------------------------------------------------------------------- launch
+
+// Blocks of a one-launch call, or 0: the pool or its tables are too large for one.
+static int one_launch(const PageArgs &a) {
+  return a.num_pages <= kOnePages && (int64_t)a.rows * a.max_pages <= kOneEntries ? 256 : 0;
+}
+static int fork_lds(int pages) {
+  const int words = (pages + 63) / 64;
+  return pages * 8 + words * 8 + ((words + 1) & ~1) * 4 + words * 8;
+}
+static int compact_lds(int pages) {
+  const int words = (pages + 63) / 64;
+  return words * 12 + pages / 2 * 8;
+}
 
 static PageArgs page_args(const Dims &dm, const kvprm_kv_cache &c, const kvprm_page_rows &from, const int32_t *refs,
                           int32_t *new_refs, int32_t *result, void *ws) {
@@ -419,6 +746,10 @@ hipError_t launch_fork_pages(const Dims &dm, const kvprm_kv_cache &c, const kvpr
   a.children = to.rows, a.to_pages = to.max_pages;
   a.parent = parent, a.room = room;
   a.to_table = to.page_table, a.to_lengths = to.lengths, a.to_held = to.held;
+  if (const int n = one_launch(a)) {
+    hipLaunchKernelGGL(k_fork_one, dim3(n), dim3(kOneThreads), fork_lds(a.num_pages), s, a);
+    return hipGetLastError();
+  }
   const int blocks = (a.num_pages + kScanPages - 1) / kScanPages;
   hipLaunchKernelGGL(k_fork_init, dim3((a.num_pages + 255) / 256), dim3(256), 0, s, a);
   if (a.rows + a.children > 0) {
@@ -438,6 +769,10 @@ hipError_t launch_compact_pages(const Dims &dm, const kvprm_kv_cache &c, const k
   PageArgs a = page_args(dm, c, rows, refs, new_refs, result, ws);
   a.to_table = new_table;
   a.moved = moved;
+  if (const int n = one_launch(a)) {
+    hipLaunchKernelGGL(k_compact_one, dim3(n), dim3(kOneThreads), compact_lds(a.num_pages), s, a);
+    return hipGetLastError();
+  }
   const int blocks = (a.num_pages + kScanPages - 1) / kScanPages;
   hipLaunchKernelGGL(k_compact_init, dim3(1), dim3(64), 0, s, a);
   hipLaunchKernelGGL(k_compact_scan, dim3(blocks + a.rows * ((a.max_pages + 1023) / 1024)), dim3(256), 0, s, a, blocks);

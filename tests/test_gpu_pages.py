@@ -163,7 +163,8 @@ def test_fork_that_cannot_be():
     pool.same()
 
 
-@pytest.mark.parametrize("pages,n,most", [(4096, 30, 60), (4097, 40, 100), (20000, 64, 200), (70000, 256, 150)])
+@pytest.mark.parametrize("pages,n,most", [(4096, 30, 60), (4097, 40, 100), (16384, 64, 200), (16385, 64, 200),
+                                          (20000, 64, 200), (70000, 256, 150)])
 def test_large_pools(pages, n, most):
     """Pools of several scan blocks, up to 256 rows; a long prefix."""
     _say("large", pages)
