@@ -610,14 +610,33 @@ __device__ __forceinline__ uint32_t codes4(const float *x, float scale) {
   return w;
 }
 
+// The largest of m over the lanes that share 32 dims (LANES neighbours), and the value of the lane that is LANES / 2 on or
+// back: row operations, where an LDS permute would cost a round trip.
+template <int LANES>
+__device__ __forceinline__ uint32_t group_max(uint32_t m) {
+  m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0xB1, 0xF, 0xF, false));  // lanes 1 0 3 2
+  m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x4E, 0xF, 0xF, false));  // lanes 2 3 0 1
+  if (LANES == 8) m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x141, 0xF, 0xF, false));  // lane 7 - i of 8
+  return m;
+}
+template <int LANES>
+__device__ __forceinline__ uint32_t half_on(uint32_t v) {
+  if (LANES == 4) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, false);
+  return (uint32_t)__builtin_amdgcn_ds_swizzle((int)v, 4 << 10 | 0x1F);  // lane i ^ 4
+}
+
 // k_write_kv for 4-bit tiles: a token's codes and scales depend on that token alone, so nothing that the page holds
 // is read or changed, and the bytes of a value belong to one slot each. The rows of a tile are in registers (16
-// bytes of a row per lane and load); the lanes that share a group of 32 dims find its largest magnitude, and the
-// codes meet in LDS in the stored order.
+// bytes of a row per lane and load; slots that get no row repeat one that does); the lanes that share a group of 32
+// dims find its largest magnitude, and the codes meet in LDS in the stored order.
+// Bound by memory on long prompts: 8 of 16384 to 32768 rows, 4 kv-heads of 128 dims, bf16 (520 MB moved): 103 us, 5.0
+// TB/s (99 with loads and stores past the caches, which the next reader of the pages would pay for). Single tokens of 16
+// sequences: 3.7 us, the launch.
 template <int D, typename S>
 __global__ __launch_bounds__(256) void k_write_kv4(RowArgs a) {
   typedef RowMap<D, S> Map;
   constexpr int VS = Map::VS, RL = Map::RL, NP = Map::NP, TILE = (int)tile_bytes(3, D), CELL = D / 8;
+  constexpr int LANES = kFp4Group / VS;  // lanes of 32 dims
   __shared__ __align__(16) unsigned char lds[4][TILE];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int b = blockIdx.y;
@@ -632,34 +651,46 @@ __global__ __launch_bounds__(256) void k_write_kv4(RowArgs a) {
   if (n <= 0 || page * kPage >= L + n) return;
   const int id = a.page_table[(size_t)b * a.max_pages + page];
   if (id < 0 || id >= a.num_pages) return;
-  const S *rows = (const S *)(part ? a.v : a.k);
+  const S *rows = (const S *)(part ? a.v : a.k) + (int64_t)j * D;
   const int64_t stride = part ? a.vs : a.ks;
 
+  // slots [lo, hi) are new: rows t0 + slot of the candidate
+  const int t0 = page * kPage - L, lo = max(0, -t0);
+  int hi = min(kPage, n - t0);
   const Map at(lane);
   uint4 raw[NP][RL];
-  uint32_t news = 0;  // slots this lane loads that are new
+  uint32_t news;
+  if (!a.index) {
+    hi = (int)min((int64_t)hi, a.num_rows - r0 - t0);
+    if (hi <= lo) return;
+    news = (1u << hi) - (1u << lo);
+    const S *row = rows + (int64_t)(r0 + t0) * stride + at.e0;
 #pragma unroll
-  for (int p = 0; p < NP; ++p)
+    for (int p = 0; p < NP; ++p)
 #pragma unroll
-    for (int i = 0; i < RL; ++i) {
-      const int slot = at.slot(p, i), t = page * kPage + slot - L;
-      bool ok = t >= 0 && t < n;
-      int64_t row = 0;
-      if (ok) {
-        row = a.index ? a.index[r0 + t] : r0 + t;
-        ok = row >= 0 && row < a.num_rows;
+      for (int i = 0; i < RL; ++i)
+        raw[p][i] = *(const uint4 *)(row + min(max(at.slot(p, i), lo), hi - 1) * stride);
+  } else {
+    news = 0;
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int i = 0; i < RL; ++i) {
+        const int slot = at.slot(p, i);
+        const int64_t row = a.index[r0 + t0 + min(max(slot, lo), hi - 1)];
+        if (slot >= lo && slot < hi && row >= 0 && row < a.num_rows) news |= 1u << slot;
+        raw[p][i] = *(const uint4 *)(rows + min(max(row, (int64_t)0), a.num_rows - 1) * stride + at.e0);
       }
-      raw[p][i] = make_uint4(0, 0, 0, 0);
-      if (ok) {
-        raw[p][i] = *(const uint4 *)(rows + row * stride + (int64_t)j * D + at.e0);
-        news |= 1u << slot;
-      }
-    }
+#pragma unroll
+    for (int off = Map::LPR; off < 64; off <<= 1) news |= __shfl_xor(news, off, 64);
+    if (!news) return;
+  }
   unsigned char *tb = lds[wave];
   const int g = at.e0 / kFp4Group, in = at.e0 % kFp4Group;
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
-    uint32_t code[RL], other[RL];
+    uint32_t code[RL], scales = 0;
+    const int slot = at.slot(p, 0);  // RL slots from here on
 #pragma unroll
     for (int i = 0; i < RL; ++i) {
       float x[VS];
@@ -667,17 +698,19 @@ __global__ __launch_bounds__(256) void k_write_kv4(RowArgs a) {
       uint32_t m = 0;
 #pragma unroll
       for (int k = 0; k < VS; ++k) m = max(m, __float_as_uint(x[k]) & 0x7FFFFFFFu);
-#pragma unroll
-      for (int off = 1; off < kFp4Group / VS; off <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, off, 64));
-      const uint32_t sc = scale_byte4(m);
+      const uint32_t sc = scale_byte4(group_max<LANES>(m));
       code[i] = sc == 255u ? 0u : codes4<VS>(x, __uint_as_float(sc << 23));
-      const int slot = at.slot(p, i);
-      if (in == 0) tb[8 * D + (part ? (slot >> 2) * CELL + g * 4 + (slot & 3) : g * 16 + slot)] = (unsigned char)sc;
+      scales |= sc << 8 * i;
+    }
+    if (in == 0) {
+      unsigned char *s = tb + 8 * D + (part ? (slot >> 2) * CELL + g * 4 + (slot & 3) : g * 16 + slot);
+      if (RL == 4) *(uint32_t *)s = scales;
+      else *(uint16_t *)s = (uint16_t)scales;
     }
     if (!part) {
 #pragma unroll
       for (int i = 0; i < RL; ++i) {
-        unsigned char *c = tb + (g * 16 + at.slot(p, i)) * 16 + in / 2;
+        unsigned char *c = tb + (g * 16 + slot + i) * 16 + in / 2;
         if (VS == 8) *(uint32_t *)c = code[i];
         else *(uint16_t *)c = (uint16_t)code[i];
       }
@@ -685,50 +718,56 @@ __global__ __launch_bounds__(256) void k_write_kv4(RowArgs a) {
       // The lanes of dims m .. and m + 16 .. pair up (a byte of values holds the codes of both): the first forms the
       // bytes of the even dims, the second those of the odd ones.
       const bool odd = in >= 16;
+      uint32_t w[4] = {0, 0, 0, 0};  // byte k: dim 2 k (+ 1) of this lane pair's VS, of slot i
 #pragma unroll
       for (int i = 0; i < RL; ++i) {
-        other[i] = (uint32_t)__shfl_xor((int)code[i], 16 / VS, 64);
-        const uint32_t lo = odd ? other[i] >> 4 : code[i], hi = odd ? code[i] >> 4 : other[i];
-        code[i] = (lo & 0x0F0F0F0Fu) | (hi & 0x0F0F0F0Fu) << 4;  // byte k: dim 2 k (+ 1) of this lane pair's VS
+        const uint32_t other = half_on<LANES>(code[i]);
+        const uint32_t low = odd ? other >> 4 : code[i], high = odd ? code[i] >> 4 : other;
+        w[i] = (low & 0x0F0F0F0Fu) | (high & 0x0F0F0F0Fu) << 4;
       }
-#pragma unroll
-      for (int k = 0; k < VS / 2; ++k) {
-        const int dim = in % 16 + 2 * k + odd, slot = at.slot(p, 0);
-        unsigned char *c = tb + ((slot >> 2) * 16 + dim) * CELL + g * 4 + (slot & 3);
-        uint32_t w = 0;
-#pragma unroll
-        for (int i = 0; i < RL; ++i) w |= (code[i] >> 8 * k & 255u) << 8 * i;
-        if (RL == 4) *(uint32_t *)c = w;
-        else *(uint16_t *)c = (uint16_t)w;
+      // transposed: word k holds the slots' bytes of dim 2 k (+ 1)
+      const uint32_t a0 = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), a1 = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);
+      unsigned char *c = tb + ((slot >> 2) * 16 + in % 16 + odd) * CELL + g * 4 + (slot & 3);
+      if constexpr (RL == 4) {
+        const uint32_t b0 = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), b1 = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+        *(uint32_t *)c = __builtin_amdgcn_perm(b0, a0, 0x05040100u);
+        *(uint32_t *)(c + 2 * CELL) = __builtin_amdgcn_perm(b0, a0, 0x07060302u);
+        if (VS == 8) {
+          *(uint32_t *)(c + 4 * CELL) = __builtin_amdgcn_perm(b1, a1, 0x05040100u);
+          *(uint32_t *)(c + 6 * CELL) = __builtin_amdgcn_perm(b1, a1, 0x07060302u);
+        }
+      } else {
+        *(uint16_t *)c = (uint16_t)a0;
+        *(uint16_t *)(c + 2 * CELL) = (uint16_t)(a0 >> 16);
+        if (VS == 8) {
+          *(uint16_t *)(c + 4 * CELL) = (uint16_t)a1;
+          *(uint16_t *)(c + 6 * CELL) = (uint16_t)(a1 >> 16);
+        }
       }
     }
   }
-#pragma unroll
-  for (int off = Map::LPR; off < 64; off <<= 1) news |= __shfl_xor(news, off, 64);
-  if (!news) return;
   __builtin_amdgcn_wave_barrier();
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   char *out = (part ? a.vp : a.kp) + ((size_t)id * a.nkv + j) * TILE;
+  if (news == 0xFFFFu) {  // (the same in every lane)
+#pragma unroll
+    for (int it = 0; it < (TILE / 16 + 63) / 64; ++it)
+      if (it * 64 + lane < TILE / 16) ((uint4 *)out)[it * 64 + lane] = ((const uint4 *)tb)[it * 64 + lane];
+    return;
+  }
   if (!part) {
     if (lane < D / 2 && (news >> (lane & 15) & 1)) *(uint4 *)(out + 16 * lane) = *(const uint4 *)(tb + 16 * lane);
   } else {
     const uint32_t bits = news >> 4 * (lane >> 4) & 15u;
-    const uint32_t *from = (const uint32_t *)(tb + lane * CELL);
-    uint32_t *to = (uint32_t *)(out + lane * CELL);
-    if (bits == 15u) {
-      if (CELL == 16) *(uint4 *)to = *(const uint4 *)from;
-      else *(uint2 *)to = *(const uint2 *)from;
-    } else {
 #pragma unroll
-      for (int x = 0; x < CELL; ++x)
-        if (bits >> (x & 3) & 1) ((char *)to)[x] = ((const char *)from)[x];
-    }
+    for (int x = 0; x < CELL; ++x)
+      if (bits >> (x & 3) & 1) out[lane * CELL + x] = (char)tb[lane * CELL + x];
   }
   const int slot = part ? lane / CELL * 4 + (lane & 3) : lane & 15;
   if (lane < D / 2 && (news >> slot & 1)) out[8 * D + lane] = (char)tb[8 * D + lane];
 }
 
-// k_read_kv for 4-bit tiles.
+// k_read_kv for 4-bit tiles. Bound by memory: the same prompts back as rows, 101 us, 5.1 TB/s.
 template <int D, typename S>
 __global__ __launch_bounds__(256) void k_read_kv4(RowArgs a) {
   typedef RowMap<D, S> Map;
