@@ -282,9 +282,16 @@ static GroupTable group_table(const kvprm_handle h, const kvprm_batch *b, const 
     priv[i] = b->lengths_host ? (b->lengths_host[i] + kPage - 1) / kPage - first : b->max_pages;
     slots[i] = p.nch - ((first + (1 << gt.cshift_prefix) - 1) >> gt.cshift_prefix);
   }
-  const PrivateChunks pc = private_chunk_rule(h->dm, b->batch, priv, slots, b->lengths_host != nullptr);
-  const int CP = 1 << pc.shift;
+  PrivateChunks pc = {0, 1};
+  if (h->dm.kvdt == 3) {
+    gt.chunk_private = chunk_pages4(h->dm, b->batch, priv, slots, b->lengths_host != nullptr);
+  } else {
+    pc = private_chunk_rule(h->dm, b->batch, priv, slots, b->lengths_host != nullptr);
+    gt.chunk_private = 1 << pc.shift;
+  }
+  const int CP = gt.chunk_private;
   gt.cshift_private = pc.shift;
+  gt.cinv_private = (uint32_t)(((1ull << 32) + CP - 1) / CP);
   gt.heads_per_block = pc.heads_per_block;
   gt.private_chunks = 1;
   gt.private_items = b->batch;
@@ -292,7 +299,7 @@ static GroupTable group_table(const kvprm_handle h, const kvprm_batch *b, const 
   for (int i = 0; i < b->batch; ++i) {
     const int ch = (priv[i] + CP - 1) / CP;
     if (ch > gt.private_chunks) gt.private_chunks = ch;
-    gt.private_items += priv[i] >> pc.shift;
+    gt.private_items += priv[i] / CP;
     if (priv[i] > longest) longest = priv[i];
   }
   // (a prefix group's shared pages are read by the chunk kernels)

@@ -334,17 +334,23 @@ __device__ __forceinline__ floatx4 score_term4(const uint4 &key, uint32_t scale,
   // (formats 4: e2m1, 2: e2m3)
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, 2, 0, (int)scale, K & 3, (int)q.scale[K >> 2]);
 }
+// Two pages' scores, their chains of products side by side.
 template <int D>
-__device__ __forceinline__ floatx4 scores4(const uint4 &key, uint32_t scale, const Query4<D> &q) {
-  floatx4 c = {0.f, 0.f, 0.f, 0.f};
-  c = score_term4<D, 0>(key, scale, q, c);
-  c = score_term4<D, 1>(key, scale, q, c);
-  c = score_term4<D, 2>(key, scale, q, c);
+__device__ __forceinline__ void scores4(const uint4 (&key)[2], const uint32_t (&scale)[2], const Query4<D> &q, floatx4 &sa,
+                                        floatx4 &sb) {
+  sa = sb = floatx4{0.f, 0.f, 0.f, 0.f};
+  sa = score_term4<D, 0>(key[0], scale[0], q, sa);
+  sb = score_term4<D, 0>(key[1], scale[1], q, sb);
+  sa = score_term4<D, 1>(key[0], scale[0], q, sa);
+  sb = score_term4<D, 1>(key[1], scale[1], q, sb);
+  sa = score_term4<D, 2>(key[0], scale[0], q, sa);
+  sb = score_term4<D, 2>(key[1], scale[1], q, sb);
   if constexpr (D == 128) {
-    c = score_term4<D, 3>(key, scale, q, c);
-    c = score_term4<D, 4>(key, scale, q, c);
+    sa = score_term4<D, 3>(key[0], scale[0], q, sa);
+    sb = score_term4<D, 3>(key[1], scale[1], q, sb);
+    sa = score_term4<D, 4>(key[0], scale[0], q, sa);
+    sb = score_term4<D, 4>(key[1], scale[1], q, sb);
   }
-  return c;
 }
 static_assert(kTerms4 == 5, "products of scores4");
 
@@ -393,7 +399,8 @@ __device__ __forceinline__ void walk_pages4(const AttnArgs &a, int b, int j, int
   const uint32_t on0 = second ? 0u : ~0u, on1 = TWO && !second ? 0u : ~0u;  // the page halves of a lane's weights
   auto compute = [&](int pp, const Pair4<D> &r, auto tail) {
     constexpr bool TAIL = decltype(tail)::value;
-    const floatx4 sa = scores4<D>(r.k[0], r.ks[0], q), sb = scores4<D>(r.k[1], r.ks[1], q);
+    floatx4 sa, sb;
+    scores4<D>(r.k, r.ks, q, sa, sb);
     float s[N];
     // this lane's tokens, 0 .. 3 of page A and 16 .. 19 of page B, before the chunk's and the cache's end
     const int left = min(L, (p0 + np) * kPage) - (p0 + 2 * pp) * kPage - 4 * cq, mine = left - (second ? 16 : 0);
@@ -443,14 +450,16 @@ __device__ __forceinline__ void walk_pages4(const AttnArgs &a, int b, int j, int
       uint2 A[2], B[2];
       values4(word(r.v[0], g), word(r.vs[0], g), A[0], A[1]);
       values4(word(r.v[1], g), word(r.vs[1], g), B[0], B[1]);
+      uint4 v[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        uint4 v = make_uint4(A[h].x, A[h].y, B[h].x, B[h].y);
-        if (TAIL) v = make_uint4(v.x & mk[0], v.y & mk[1], v.z & mk[2], v.w & mk[3]);
-        floatx4 &o = acc[2 * g + h];
-#pragma unroll
-        for (int x = 0; x < 3; ++x) o = mfma16(v, P[x], o);
+        v[h] = make_uint4(A[h].x, A[h].y, B[h].x, B[h].y);
+        if (TAIL) v[h] = make_uint4(v[h].x & mk[0], v[h].y & mk[1], v[h].z & mk[2], v[h].w & mk[3]);
       }
+#pragma unroll
+      for (int x = 0; x < 3; ++x)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) acc[2 * g + h] = mfma16(v[h], P[x], acc[2 * g + h]);
     }
   };
   // pairs without a slot at or past the end; the last one may have some
@@ -509,7 +518,7 @@ __device__ __forceinline__ bool chunk_item(const AttnArgs &a, int id, ChunkItem 
   for (int gi = 0; gi < a.gt.n; ++gi)
     if (bl * a.kq >= a.gt.start[gi] && bl * a.kq < a.gt.start[gi + 1]) first_l = a.gt.prefix_pages[gi];
   const int full_l =
-      lane < a.B ? max(0, (L_l + kPage - 1) / kPage - first_l) >> a.gt.cshift_private : 0;
+      lane < a.B ? (int)__umulhi(max(0, (L_l + kPage - 1) / kPage - first_l), a.gt.cinv_private) : 0;
   const int cum_l = lane_scan(full_l);
   const int total = __builtin_amdgcn_readlane(cum_l, 63);
   if (id < total) {
@@ -540,10 +549,10 @@ __global__ __launch_bounds__(64 * kMaxKvHeadsMx, 2) void k_attn4(AttnArgs a) {
   const size_t head = ((size_t)it.b * a.kq + ti) * a.nq + (size_t)j * a.g + hh;
   const int npages = (it.L + kPage - 1) / kPage;
   const int ncp = (it.first + (1 << a.gt.cshift_prefix) - 1) >> a.gt.cshift_prefix;  // prefix chunks
-  const int p0 = it.first + (it.c << a.gt.cshift_private);
+  const int p0 = it.first + it.c * a.gt.chunk_private;
   // (a device length above its host mirror must not reach past the candidate's slots)
   if (p0 >= npages || ncp + it.c >= a.nch) return;
-  const int np = min(npages - p0, 1 << a.gt.cshift_private);
+  const int np = min(npages - p0, a.gt.chunk_private);
   float m_run = -INFINITY, l_run = 0.f;
   floatx4 acc[NDB];
 #pragma unroll
@@ -922,9 +931,9 @@ __global__ __launch_bounds__(NTHR) void k_merge_mx(AttnArgs a) {
   for (int gi = 0; gi < a.gt.n; ++gi)
     if (b >= a.gt.start[gi] && b < a.gt.start[gi + 1]) first = a.gt.prefix_pages[gi];
   // shared-prefix chunks, then private chunks
-  const int sp = a.gt.cshift_prefix, sv = a.gt.cshift_private;
-  const int nc =
-      min(a.nch, ((first + (1 << sp) - 1) >> sp) + ((npages - first + (1 << sv) - 1) >> sv));
+  const int sp = a.gt.cshift_prefix;
+  const int nc = min(a.nch, ((first + (1 << sp) - 1) >> sp) +
+                                (int)__umulhi(max(0, npages - first) + a.gt.chunk_private - 1, a.gt.cinv_private));
   const float *base = a.apart + ((size_t)b * a.nq + h) * a.nch * (D + 2);
   // (chunks past the last read the last one again, so that no load is conditional; they are not
   // added. A row without chunks reads slot 0, which exists)

@@ -32,6 +32,8 @@ struct GroupTable {
   int private_items;                   // chunks of all candidates: full ones and a slot for each last one
   int one_launch;                      // short caches: k_attn_short in place of chunks and merge
   int cshift_prefix, cshift_private;   // chunk lengths (1 << shift pages) of the two kernels
+  int chunk_private;                   // the latter in pages (4-bit caches: any even number up to 64)
+  uint32_t cinv_private;               // ceil(2^32 / chunk_private): x / chunk_private = x * cinv >> 32 for x < 2^20
 };
 
 // Attention split: each work item covers one chunk of pages of one candidate (and kv-head).
@@ -172,6 +174,8 @@ struct PrivateChunks {
 };
 PrivateChunks private_chunk_rule(const Dims &dm, int n, const int *pages, const int *slots,
                                  bool known);
+// Chunk length of 4-bit caches in pages, a wave and a block per kv-head.
+int chunk_pages4(const Dims &dm, int n, const int *pages, const int *slots, bool known);
 // Long chunks: the longest of 16, 32, 64 pages that leaves at least 160 work items for `pages` pages.
 int long_chunk_shift(long long pages);
 // Chunk length of the backward attention, in pages.

@@ -95,41 +95,8 @@ int long_chunk_shift(long long pages) {
 // against one: 13-18% slower at any chunk length, 1.4% faster on the 63 that this rule picks; eight of
 // 200616 tokens in all, 4 heads 70.0 against 78.4 us a call (as waves of their own some units get four,
 // others two or three), but 24 of 4096, 8 heads 96.5 against 65.1.
-// 4-bit caches, whose waves are bound by vector instructions and products rather than by memory: the chunk with the
-// smallest time by a model of the chip's 1024 SIMD units. In units of a page pair on a unit of its own (0.8 us at d_h =
-// 128): a pair takes 1, 1.6 and 1.8 on a unit of one, two and three waves (the resident ones; more follow in turn), a
-// wave's start and end 4, the merge 1 for every 1024 waves; at d_h = 64 1, 1.5, 1.8, 2 and 2. 88 batches (eight head
-// layouts, 1 to 64 candidates of up to 32k tokens, equal and ragged): 0.3% above each one's fastest chunk length in the
-// mean, 8% at most; by the limit on waves that the other types have, 2.1% and 18%.
-// All heads in a block were slower wherever the limit's rule would take them.
-static PrivateChunks chunk_rule4(const Dims &dm, int n, const int *pages, const int *slots, bool known) {
-  PrivateChunks r{6, 1};
-  double best = 0;
-  long long total = 0;
-  for (int i = 0; i < n; ++i) total += pages[i];
-  for (int sh = 6; sh >= 2; --sh) {
-    bool fits = true;
-    long long waves = 0;
-    for (int i = 0; i < n; ++i) {
-      const int ch = (pages[i] + (1 << sh) - 1) >> sh;
-      waves += (long long)ch * dm.nkv;
-      if (ch > slots[i] || (sh < 4 && ch > kFineChunks)) fits = false;
-    }
-    if (!fits && sh < 6) break;  // (nor do shorter ones)
-    const bool half = dm.d == 64;
-    const double shared[4] = {0, 1, half ? 1.5 : 1.6, 1.8};
-    const long long each = (waves + 1023) / 1024;  // waves of a unit
-    const double t = ((1 << sh) / 2 + (half ? 2 : 4)) * (each / 3 * shared[3] + shared[each % 3]) +
-                     (half ? 2 : 1) * waves / 1024.;
-    if (sh == 6 || t < best) best = t, r.shift = sh;
-  }
-  if (!known) r.shift = std::min(r.shift, long_chunk_shift(total));
-  return r;
-}
-
 PrivateChunks private_chunk_rule(const Dims &dm, int n, const int *pages, const int *slots,
                                  bool known) {
-  if (dm.kvdt == 3) return chunk_rule4(dm, n, pages, slots, known);
   const bool f32 = dm.kvdt == 0;
   const int lo = f32 ? 1 : 2, hi = f32 ? 5 : 6;
   PrivateChunks r{hi, 1};
@@ -156,6 +123,38 @@ PrivateChunks private_chunk_rule(const Dims &dm, int n, const int *pages, const 
     if (items <= 512 && items * 10 >= round * 7) r.heads_per_block = dm.nkv;
   }
   return r;
+}
+
+// 4-bit caches, whose waves are bound by vector instructions and products as much as by memory: the chunk with the
+// smallest time by a model of the chip's 1024 SIMD units. In units of a page pair on a unit of its own (0.8 us at d_h =
+// 128): a pair takes 1, 1.5 and 2 on a unit of one, two and three waves (the resident ones; more follow in turn), a
+// wave's start and end 5, the merge 3 for every 1024 waves; at d_h = 64 1, 1.4, 1.8, 5 and 2. 52 batches (eight head
+// layouts, 1 to 64 candidates of up to 32k tokens, equal and ragged): 1.2% above each one's fastest of these lengths in
+// the mean, 8% at most; the fastest power of two is 2.6% above. (The limit on waves that the other types have: 2.1% above
+// the fastest power of two, 18% at most.) All heads in a block were slower wherever the rule of the other types
+// would take them.
+int chunk_pages4(const Dims &dm, int n, const int *pages, const int *slots, bool known) {
+  static const int lengths[] = {64, 56, 48, 40, 32, 28, 24, 20, 16, 14, 12, 10, 8, 6, 4};
+  const bool half = dm.d == 64;
+  const double shared[4] = {0, 1, half ? 1.4 : 1.5, half ? 1.8 : 2};
+  long long total = 0;
+  for (int i = 0; i < n; ++i) total += pages[i];
+  int pick = lengths[0];
+  double best = 0;
+  for (int len : lengths) {
+    bool fits = true;
+    long long waves = 0;
+    for (int i = 0; i < n; ++i) {
+      const int ch = (pages[i] + len - 1) / len;
+      waves += (long long)ch * dm.nkv;
+      if (ch > slots[i] || (len < 16 && ch > kFineChunks)) fits = false;
+    }
+    if (!fits && len < lengths[0]) break;  // (nor do shorter ones)
+    const long long each = (waves + 1023) / 1024;  // waves of a unit
+    const double t = (len / 2 + 5) * (each / 3 * shared[3] + shared[each % 3]) + (half ? 2 : 3) * waves / 1024.;
+    if (len == lengths[0] || t < best) best = t, pick = len;
+  }
+  return known ? pick : std::min(pick, 1 << long_chunk_shift(total));
 }
 
 // The backward attention runs eight waves (chunks) to a block and one block per compute unit
