@@ -354,20 +354,10 @@ __device__ __forceinline__ void scores4(const uint4 (&key)[2], const uint32_t (&
 }
 static_assert(kTerms4 == 5, "products of scores4");
 
-// A page pair in registers: key codes of a slot's 32 dims and their scale, value codes and scales as in PairRaw4.
-template <int D>
-struct Pair4 {
-  uint4 k[2], v[2], vs[2];
-  uint32_t ks[2];
-};
-
 // The larger of two, NaN if one is (one instruction; fmaxf takes another for each operand that may be a signalling NaN).
 __device__ __forceinline__ float larger(float x, float y) { return __builtin_elementwise_maximum(x, y); }
 
-// TWO: at most 8 columns, whose queries lanes 8 to 15 of 16 repeat; there a column goes over the second page of each
-// pair, in the others over the first, so that no lane's softmax is idle (8 chunks of 64 pages, 7 columns: XX us instead of
-// XX). The two are joined at the end.
-template <int D, bool TWO>
+template <int D>
 __device__ __forceinline__ void walk_pages4(const AttnArgs &a, int b, int j, int L, int p0, int np, const float *qr,
                                             bool colv, float &m_run, float &l_run, floatx4 (&acc)[D / 16]) {
   constexpr int NDB = D / 16;
@@ -378,7 +368,7 @@ __device__ __forceinline__ void walk_pages4(const AttnArgs &a, int b, int j, int
   const int cell = D == 128 ? lane : lane & 31;  // (32 dims, slot)
   // (indices past the chunk are clamped to its last page: those tokens are masked anyway)
   auto tile = [&](int p) { return ((size_t)lane_value(ph_l, min(p, np - 1)) * nkv + j) * TILE; };
-  auto load_pair = [&](int pp, Pair4<D> &r) {
+  auto load_pair = [&](int pp, PairRaw4<D> &r) {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const size_t t = tile(2 * pp + x);
@@ -388,31 +378,27 @@ __device__ __forceinline__ void walk_pages4(const AttnArgs &a, int b, int j, int
       r.vs[x] = load_bytes<D / 8, false>(a.vp + t + value_scale4<D>(lane));
     }
   };
-  Pair4<D> r0, r1;
+  PairRaw4<D> r0, r1;
   load_pair(0, r0);
   load_pair(1, r1);
   __builtin_amdgcn_sched_barrier(0);
   Query4<D> q;
   query_terms4<D>(qr, colv, kLog2e / sqrtf((float)D), lane, q);  // scores in log2 units
-  constexpr int N = TWO ? 4 : 8;  // a lane's tokens of a pair
-  const bool second = TWO && (lane & 8);
-  const uint32_t on0 = second ? 0u : ~0u, on1 = TWO && !second ? 0u : ~0u;  // the page halves of a lane's weights
-  auto compute = [&](int pp, const Pair4<D> &r, auto tail) {
+  auto compute = [&](int pp, const PairRaw4<D> &r, auto tail) {
     constexpr bool TAIL = decltype(tail)::value;
     floatx4 sa, sb;
     scores4<D>(r.k, r.ks, q, sa, sb);
-    float s[N];
+    float s[8];
     // this lane's tokens, 0 .. 3 of page A and 16 .. 19 of page B, before the chunk's and the cache's end
-    const int left = min(L, (p0 + np) * kPage) - (p0 + 2 * pp) * kPage - 4 * cq, mine = left - (second ? 16 : 0);
-    auto valid = [&](int i) { return i < 4 ? mine > i : left > 12 + i; };
+    const int left = min(L, (p0 + np) * kPage) - (p0 + 2 * pp) * kPage - 4 * cq;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      s[i] = i >= 4 ? sb[i & 3] : second ? sb[i] : sa[i];
-      if (TAIL) s[i] = valid(i) ? s[i] : -INFINITY;
+    for (int i = 0; i < 4; ++i) {
+      s[i] = !TAIL || left > i ? sa[i] : -INFINITY;
+      s[4 + i] = !TAIL || left > 16 + i ? sb[i] : -INFINITY;
     }
     float mx = s[0];
 #pragma unroll
-    for (int i = 1; i < N; ++i) mx = larger(mx, s[i]);
+    for (int i = 1; i < 8; ++i) mx = larger(mx, s[i]);
     mx = column_reduce(mx, larger);
     if (__any(!(mx <= m_run))) {  // (a NaN among a column's scores becomes its maximum and stays)
       const float mn = larger(m_run, mx), alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - mn);
@@ -424,20 +410,16 @@ __device__ __forceinline__ void walk_pages4(const AttnArgs &a, int b, int j, int
         for (int i = 0; i < 4; ++i) acc[nb][i] *= alpha;
     }
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      s[i] = __builtin_amdgcn_exp2f(s[i] - m_run);
-      if (TAIL) s[i] = valid(i) ? s[i] : 0.f;  // (of no token so far: -inf less -inf)
+    for (int i = 0; i < 8; ++i) {
+      s[i] = __builtin_amdgcn_exp2f(s[i] - m_run);  // (the pair's first token counts: m_run is not -inf)
       l_run += s[i];
     }
     uint32_t p[3][4];
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i) split3(s[2 * i], s[2 * i + 1], p[0][i], p[1][i], p[2][i]);
+    for (int i = 0; i < 4; ++i) split3(s[2 * i], s[2 * i + 1], p[0][i], p[1][i], p[2][i]);
     uint4 P[3];
 #pragma unroll
-    for (int x = 0; x < 3; ++x) {
-      if (TWO) P[x] = make_uint4(p[x][0] & on0, p[x][1] & on0, p[x][0] & on1, p[x][1] & on1);
-      else P[x] = make_uint4(p[x][0], p[x][1], p[x][2], p[x][3]);
-    }
+    for (int x = 0; x < 3; ++x) P[x] = make_uint4(p[x][0], p[x][1], p[x][2], p[x][3]);
     uint32_t mk[4];  // slots before the end
     if (TAIL)
 #pragma unroll
@@ -464,7 +446,7 @@ __device__ __forceinline__ void walk_pages4(const AttnArgs &a, int b, int j, int
   };
   // pairs without a slot at or past the end; the last one may have some
   const int last = ((np + 1) >> 1) - 1;
-  auto step = [&](int pp, Pair4<D> &r) {
+  auto step = [&](int pp, PairRaw4<D> &r) {
     compute(pp, r, std::integral_constant<bool, false>{});
     __builtin_amdgcn_sched_barrier(0);
     load_pair(pp + 2, r);
@@ -480,22 +462,6 @@ __device__ __forceinline__ void walk_pages4(const AttnArgs &a, int b, int j, int
     r0 = r1;
   }
   compute(last, r0, std::integral_constant<bool, true>{});
-  if (TWO) {  // (lanes i and i + 8 of 16: a rotation by 8)
-    auto other = [](float v) {
-      return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x128, 0xF, 0xF, false));
-    };
-    const float m = larger(m_run, other(m_run)), f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m);
-    m_run = m;
-    l_run *= f;
-    l_run += other(l_run);
-#pragma unroll
-    for (int nb = 0; nb < NDB; ++nb)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        acc[nb][i] *= f;
-        acc[nb][i] += other(acc[nb][i]);
-      }
-  }
 }
 
 // Which candidate and chunk block `id` of the private pages' grid has (see k_attn_mx), its length and shared pages.
@@ -535,7 +501,7 @@ __device__ __forceinline__ bool chunk_item(const AttnArgs &a, int id, ChunkItem 
 }
 
 // k_attn_mx over a 4-bit cache.
-template <int D, bool ONE, bool TWO>
+template <int D, bool ONE>
 __global__ __launch_bounds__(64 * kMaxKvHeadsMx, 2) void k_attn4(AttnArgs a) {
   constexpr int NDB = D / 16;
   const int j =
@@ -543,9 +509,8 @@ __global__ __launch_bounds__(64 * kMaxKvHeadsMx, 2) void k_attn4(AttnArgs a) {
   const int lane = threadIdx.x & 63, n = lane & 15, cq = lane >> 4;
   ChunkItem it;
   if (!chunk_item<ONE>(a, blockIdx.y, it)) return;
-  const int col = TWO ? n & 7 : n;
-  const bool colv = col < a.kq * a.g;
-  const int ti = colv ? (col * a.ginv) >> 16 : 0, hh = colv ? col - ti * a.g : 0;
+  const bool colv = n < a.kq * a.g;
+  const int ti = colv ? (n * a.ginv) >> 16 : 0, hh = colv ? n - ti * a.g : 0;
   const size_t head = ((size_t)it.b * a.kq + ti) * a.nq + (size_t)j * a.g + hh;
   const int npages = (it.L + kPage - 1) / kPage;
   const int ncp = (it.first + (1 << a.gt.cshift_prefix) - 1) >> a.gt.cshift_prefix;  // prefix chunks
@@ -557,9 +522,9 @@ __global__ __launch_bounds__(64 * kMaxKvHeadsMx, 2) void k_attn4(AttnArgs a) {
   floatx4 acc[NDB];
 #pragma unroll
   for (int nb = 0; nb < NDB; ++nb) acc[nb] = floatx4{0.f, 0.f, 0.f, 0.f};
-  walk_pages4<D, TWO>(a, it.b, j, it.L, p0, np, a.q + head * D, colv, m_run, l_run, acc);
+  walk_pages4<D>(a, it.b, j, it.L, p0, np, a.q + head * D, colv, m_run, l_run, acc);
   l_run = column_sum(l_run);
-  if (colv && col == n) store_partial<D>(a.apart + (head * a.nch + ncp + it.c) * (D + 2), cq, acc, m_run, l_run);
+  if (colv) store_partial<D>(a.apart + (head * a.nch + ncp + it.c) * (D + 2), cq, acc, m_run, l_run);
 }
 
 // One wave per kv-head j and chunk of a candidate's private pages, over the whole batch; it writes its
@@ -758,7 +723,7 @@ __global__ __launch_bounds__(64 * kShortWaves) void k_attn_short(AttnArgs a) {
   for (int nb = 0; nb < NDB; ++nb) acc[nb] = floatx4{0.f, 0.f, 0.f, 0.f};
   if (np > 0) {  // wave-uniform
     if constexpr (KVT == 3)
-      walk_pages4<D, false>(a, b, j, L, p0, np, a.q + (((size_t)b * kq + ti) * nq + (size_t)j * g + hh) * D, colv, m_run,
+      walk_pages4<D>(a, b, j, L, p0, np, a.q + (((size_t)b * kq + ti) * nq + (size_t)j * g + hh) * D, colv, m_run,
                             l_run, acc);
     else
       walk_pages<KVT, D>(a, b, j, L, npages, p0, np, qraw, colv, m_run, l_run, acc);
@@ -1112,17 +1077,13 @@ hipError_t launch_attn_mx(const Dims &dm, const Plan &p, const Workspace &w, con
       KVPRM_A(1, 128);
     }
   } else if (dm.kvdt == 3) {
-#define KVPRM_A4(D, ONE)                                                                               \
-  if (p.kq * dm.g <= 8) hipLaunchKernelGGL((k_attn4<D, ONE, true>), grid, dim3(64 * hpb), 0, s, a);    \
-  else hipLaunchKernelGGL((k_attn4<D, ONE, false>), grid, dim3(64 * hpb), 0, s, a)
     if (p.Breal == 1) {
-      if (dm.d == 64) { KVPRM_A4(64, true); }
-      else { KVPRM_A4(128, true); }
+      if (dm.d == 64) hipLaunchKernelGGL((k_attn4<64, true>), grid, dim3(64 * hpb), 0, s, a);
+      else hipLaunchKernelGGL((k_attn4<128, true>), grid, dim3(64 * hpb), 0, s, a);
     } else {
-      if (dm.d == 64) { KVPRM_A4(64, false); }
-      else { KVPRM_A4(128, false); }
+      if (dm.d == 64) hipLaunchKernelGGL((k_attn4<64, false>), grid, dim3(64 * hpb), 0, s, a);
+      else hipLaunchKernelGGL((k_attn4<128, false>), grid, dim3(64 * hpb), 0, s, a);
     }
-#undef KVPRM_A4
   } else {
     if (dm.d == 64) {
       KVPRM_A(2, 64);

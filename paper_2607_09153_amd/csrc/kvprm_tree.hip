@@ -295,7 +295,7 @@ struct Special {
 // columns (410 MB): 90 us, 4.5 TB/s. On short ones by the chain of loads, products and join: 1103 tokens,
 // 16 drafted, 8 kv-heads, 32 columns in two blocks of 16: 8 us, and 4 for k_tree_merge.
 template <int KVT, int D, int NC, typename T>
-__global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
+__global__ __launch_bounds__(64 * kTreeWaves, KVT == 3 && (NC == 1 || D == 64 || sizeof(T) == 2) ? 2 : 1) void k_tree(TreeArgs a) {
   constexpr int NKB = D / 32, NDB = D / 16, W = kTreeWaves;
   constexpr int QT = Terms<T>::Q, PT = Terms<T>::P;
   constexpr size_t TILE = tile_bytes(KVT, D);
@@ -405,7 +405,79 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_tree(TreeArgs a) {
           }
         }
       }
+      // 4-bit pairs: keys and values become operands 32 dims at a time (all at once they would not fit beside two tiles'
+      // sums in the registers of two waves a unit), and only the candidate's last pair masks slots (8 caches of 16384 to
+      // 32768 tokens, 4 drafted, 28 columns: 59 us a call in the other types' order, 53 so; 16 of 4000, 32 columns, 44 and 38).
+      auto compute4 = [&](int i, const PairOf<KVT, D> &r, auto masked) {
+        constexpr bool TAIL = decltype(masked)::value;
+        if constexpr (KVT == 3) {
+          const int left = L - (first + 2 * (w + W * i)) * kPage - 4 * cq;  // (as below)
+          floatx4 sa[NC], sb[NC];
+#pragma unroll
+          for (int ct = 0; ct < NC; ++ct) sa[ct] = sb[ct] = floatx4{0.f, 0.f, 0.f, 0.f};
+          const float ka = scale_of<0>(r.ks[0]), kb = scale_of<0>(r.ks[1]);
+#pragma unroll
+          for (int kk = 0; kk < NKB; ++kk) {
+            const uint4 a4 = keys4(word(r.k[0], kk), ka), b4 = keys4(word(r.k[1], kk), kb);
+#pragma unroll
+            for (int x = 0; x < QT; ++x)
+#pragma unroll
+              for (int ct = 0; ct < NC; ++ct) {
+                sa[ct] = mfma16(a4, qo[ct][x][kk], sa[ct]);
+                sb[ct] = mfma16(b4, qo[ct][x][kk], sb[ct]);
+              }
+          }
+          uint4 P[NC][PT];
+#pragma unroll
+          for (int ct = 0; ct < NC; ++ct) {
+            float p[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              p[e] = sa[ct][e] * rs;
+              p[4 + e] = sb[ct][e] * rs;
+              if (TAIL) {
+                p[e] = left > e ? p[e] : -INFINITY;
+                p[4 + e] = left > 16 + e ? p[4 + e] : -INFINITY;
+              }
+            }
+            st[ct].template weights<8>(p);
+            uint32_t t[3][4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              if constexpr (PT == 2) split2(p[2 * e], p[2 * e + 1], t[0][e], t[1][e]);
+              else split3(p[2 * e], p[2 * e + 1], t[0][e], t[1][e], t[2][e]);
+            }
+#pragma unroll
+            for (int x = 0; x < PT; ++x) P[ct][x] = make_uint4(t[x][0], t[x][1], t[x][2], t[x][3]);
+          }
+          const uint32_t a0 = (left > 0 ? 0xFFFFu : 0u) | (left > 1 ? 0xFFFF0000u : 0u);
+          const uint32_t a1 = (left > 2 ? 0xFFFFu : 0u) | (left > 3 ? 0xFFFF0000u : 0u);
+          const uint32_t b0 = (left > 16 ? 0xFFFFu : 0u) | (left > 17 ? 0xFFFF0000u : 0u);
+          const uint32_t b1 = (left > 18 ? 0xFFFFu : 0u) | (left > 19 ? 0xFFFF0000u : 0u);
+#pragma unroll
+          for (int g4 = 0; g4 < NKB; ++g4) {
+            uint2 A[2], B[2];
+            values4(word(r.v[0], g4), word(r.vs[0], g4), A[0], A[1]);
+            values4(word(r.v[1], g4), word(r.vs[1], g4), B[0], B[1]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              uint4 v = make_uint4(A[h].x, A[h].y, B[h].x, B[h].y);
+              if (TAIL) v = make_uint4(v.x & a0, v.y & a1, v.z & b0, v.w & b1);
+#pragma unroll
+              for (int x = 0; x < PT; ++x)
+#pragma unroll
+                for (int ct = 0; ct < NC; ++ct)
+                  st[ct].acc[2 * g4 + h] = mfma16(v, P[ct][x], st[ct].acc[2 * g4 + h]);
+            }
+          }
+        }
+      };
       auto compute = [&](int i, const PairOf<KVT, D> &r) {
+        if constexpr (KVT == 3) {
+          if ((first + 2 * (w + W * i) + 2) * kPage > L) compute4(i, r, std::integral_constant<bool, true>{});
+          else compute4(i, r, std::integral_constant<bool, false>{});
+          return;
+        }
         uint4 KA[NKB], KB[NKB];
         uint2 VA[NDB], VB[NDB];
         unpack_pair_of<KVT, D>(r, KA, KB, VA, VB);
