@@ -747,13 +747,17 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
   typedef uint16_t T;
   constexpr int KS = D / 16, NT = D / 32, TC = 2 * D;  // k steps, output tiles, 16-byte groups of a bf16 tile
   constexpr int SC = KVT == 1 ? 2 * TC : KVT == 2 ? TC : TC / 2;  // 16-byte groups of a pair in memory (codes)
-  // of these per thread, K or V (4-bit: a lane's codes and scales, of the page that its wave has)
+  // of these per thread, K or V (4-bit: a lane's codes and scales)
   constexpr int NLC = KVT == 3 ? 2 : (SC + 64 * W - 1) / (64 * W);
   constexpr int SEG = kTreeSegStages;
   constexpr bool HALF = KVT == 2;  // values and weights in fp16
   // Pairs that half of the waves can move: the first half of them moves keys, the others values.
-  constexpr bool ROLES = 2 * SC <= 64 * W;
-  static_assert(KVT != 3 || (ROLES && W == 4), "4-bit stages: two waves for keys, two for values");
+  constexpr bool ROLES = KVT != 3 && 2 * SC <= 64 * W;
+  // 4-bit pairs: a wave widens words of 8 codes of one page, W4 of the keys and W4 of the values for each lane. (With
+  // whole pages to a wave, two waves for keys and two for values, all waited at each stage's barrier for those with
+  // the values, which take more instructions: 8 caches of 16384 to 32768 tokens as below 309 us instead of 282.)
+  constexpr int W4 = D / 64;
+  static_assert(KVT != 3 || W == 4, "4-bit stages: two waves a page");
   __shared__ uint4 kb[2][2 * TC], vb[2][2 * TC];
   __shared__ int id_s[2 * SEG + 12];                    // page ids of a segment
   __shared__ float ksc_s[KVT == 2 ? 2 * SEG + 12 : 1];  // key scales / sqrt(d), log2 units
@@ -814,16 +818,24 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
   };
   int s0 = 0, se = 0;         // the segment's stages
   int kid_l = 0, vid_l = 0;   // lane i: page id i of the 64 that the key (value) loads are in
-  auto load_half = [&](const char *pool, int s, int &id_l, Half &r) {
+  auto load_words = [](const char *p) {  // W4 of them
+    if constexpr (W4 == 1) return make_uint4(*(const uint32_t *)p, 0, 0, 0);
+    else return load_bytes<4 * W4, false>(p);
+  };
+  auto load_half = [&](auto VAL, const char *pool, int s, int &id_l, Half &r) {
     const int i = 2 * (s - s0);
     if ((i & 63) == 0) id_l = id_s[min(i + lane, 2 * SEG + 11)];
     constexpr size_t TILE = tile_bytes(KVT, D);
     if constexpr (KVT == 3) {
       const char *t = pool + ((size_t)lane_value(id_l, (i & 63) + (w & 1)) * a.nkv + j) * TILE;
-      const bool val = w >= W / 2;
-      r.g[0] = load_bytes<D / 8, false>(t + (val ? value_code4<D>(lane) : key_code4<D>(lane)));
-      if (val) r.g[1] = load_bytes<D / 8, false>(t + value_scale4<D>(lane));
-      else r.g[1].x = *(const uint8_t *)(t + key_scale4<D>(lane));
+      const int at = (w >> 1) * 4 * W4;
+      if (decltype(VAL)::value) {
+        r.g[0] = load_words(t + at + value_code4<D>(lane));
+        r.g[1] = load_words(t + at + value_scale4<D>(lane));
+      } else {
+        r.g[0] = load_words(t + at + key_code4<D>(lane));
+        r.g[1].x = *(const uint8_t *)(t + key_scale4<D>(lane));
+      }
       return;
     }
     const int ia = lane_value(id_l, i & 63), ib = lane_value(id_l, (i & 63) + 1);
@@ -835,8 +847,8 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
       r.g[k] = *(const uint4 *)(t + (uint32_t)(lane * 16));
     }
   };
-  auto load_keys = [&](int s, Half &r) { load_half(a.kp, s, kid_l, r); };
-  auto load_values = [&](int s, Half &r) { load_half(a.vp, s, vid_l, r); };
+  auto load_keys = [&](int s, Half &r) { load_half(std::false_type(), a.kp, s, kid_l, r); };
+  auto load_values = [&](int s, Half &r) { load_half(std::true_type(), a.vp, s, vid_l, r); };
   // Keys: group (8 dims c, page, slot) at 32 c + 16 page + slot: step ks of the products reads groups
   // 64 ks + lane.
   auto store_keys = [&](int s, const Half &r) {
@@ -844,8 +856,8 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
     if constexpr (KVT == 3) {
       const float sc = scale_of<0>(r.g[1].x);
 #pragma unroll
-      for (int x = 0; x < D / 32; ++x)
-        kt[((lane >> 4) * (D / 32) + x) * 32 + (w & 1) * 16 + (lane & 15)] = keys4(word(r.g[0], x), sc);
+      for (int x = 0; x < W4; ++x)
+        kt[((lane >> 4) * (D / 32) + (w >> 1) * W4 + x) * 32 + (w & 1) * 16 + (lane & 15)] = keys4(word(r.g[0], x), sc);
       return;
     }
 #pragma unroll
@@ -875,9 +887,10 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
       const uint32_t m0 = (have > 0 ? 0xFFFFu : 0u) | (have > 1 ? 0xFFFF0000u : 0u);
       const uint32_t m1 = (have > 2 ? 0xFFFFu : 0u) | (have > 3 ? 0xFFFF0000u : 0u);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {  // dims mm and mm + 16 of tile t
+      for (int x = 0; x < W4; ++x) {  // dims mm and mm + 16 of tile t
+        const int t = (w >> 1) * W4 + x;
         uint2 lo, hi;
-        values4(word(r.g[0], t), word(r.g[1], t), lo, hi);
+        values4(word(r.g[0], x), word(r.g[1], x), lo, hi);
         vt[value_at(t, mm, q)] = make_uint2(lo.x & m0, lo.y & m1);
         vt[value_at(t, mm + 16, q)] = make_uint2(hi.x & m0, hi.y & m1);
       }
@@ -915,7 +928,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void k_tree_wide(TreeArgs 
     }
   };
   const int role = ROLES ? w / (W / 2) : 0;
-  auto load_own = [&](int s, Half &r) { load_half(role ? a.vp : a.kp, s, kid_l, r); };
+  auto load_own = [&](int s, Half &r) { load_half(std::false_type(), role ? a.vp : a.kp, s, kid_l, r); };
   auto store_own = [&](int s, const Half &r) {
     if (role) store_values(s, r);
     else store_keys(s, r);
