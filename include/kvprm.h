@@ -141,7 +141,7 @@ typedef struct {
  * first group_prefix_len_host[g] tokens, which must be a multiple of 16 and at most every
  * member's length (checked against lengths_host, which the hint requires), and be held by the
  * same physical pages in every member's row (not checked: the shared part is read through the
- * first member's row). Groups tile [0, B). With bf16 or fp8 caches and at most 64 groups the
+ * first member's row). Groups tile [0, B). With bf16, fp8 or 4-bit caches and at most 64 groups the
  * shared pages are read once per group instead of once per member; otherwise the hint is
  * ignored. A valid hint changes results only by floating-point summation order. */
 typedef struct {

@@ -1,5 +1,5 @@
 // Matrix-core attention of the verify-token pass for gfx950: the split-L paged chunk kernels over
-// private pages (k_attn_mx for bf16 and fp8 e4m3 caches, k_attn_f32), the shared-prefix kernel
+// private pages (k_attn_mx for bf16 and fp8 e4m3 caches, k_attn4 for 4-bit ones, k_attn_f32), the shared-prefix kernel
 // (k_prefix_mx), the log-sum-exp merge with the token's own key (k_merge_mx), and the whole step of
 // a short cache in one launch (k_attn_short, k_attn_short_f32).
 #include <hip/hip_runtime.h>

@@ -41,7 +41,7 @@ struct GroupTable {
 // private_chunk_rule).
 constexpr int kChunkPagesF32 = 32;  // longest chunk of an fp32 cache
 constexpr int kMaxChunks = 1024;  // chunk partials one merge handles
-constexpr int kMaxKvHeadsMx = 8;  // kv-heads with bf16 and fp8 caches
+constexpr int kMaxKvHeadsMx = 8;  // kv-heads with bf16, fp8 and 4-bit caches
 constexpr int kFineChunks = 128;  // chunks of one candidate at most, in chunks under 16 pages
 constexpr int kShortPages = 32;   // longest cache of the one-launch attention
 constexpr int kShortPages4 = 128;  // ... in 4 bits (fewer by short_pages)

@@ -1,5 +1,5 @@
 // Matrix-core (MFMA, v_mfma_f32_16x16x32_bf16) pipeline of the verify-token pass for gfx950,
-// used with bf16 weights and bf16 or fp8 (OCP e4m3) caches: the projections and their fused
+// used with bf16 weights and bf16, fp8 (OCP e4m3) or 4-bit caches: the projections and their fused
 // element-wise steps (this file) and the attention kernels (kvprm_attn.hip). Per layer:
 //
 //   q/k/v projection, RMSNorm scale and rotary in its epilogue      -> q, k_self, v_self
