@@ -116,8 +116,8 @@ typedef struct {
  *   k_scale, v_scale: [num_layers][num_pages][num_kv_heads]; NULL for other dtypes.
  * FP4_E2M1 pools hold codes and scales in the tile, 8 d_h + d_h / 2 bytes (pools 16-byte aligned; 4.25 bits a value;
  * written by kvprm_write_kv). A code (bit 3 the sign, then 0, 0.5, 1, 1.5, 2, 3, 4, 6) is multiplied by its scale, the
- * power of two with the biased exponent byte e: 2^(e - 127), e = 0 .. 252; 255 makes the 32 values NaN (253 and
- * 254: codes whose product passes fp32 become infinities).
+ * power of two with the biased exponent byte e: 2^(e - 127), e = 0 .. 252; 255 makes the 32 values NaN (253 and 254
+ * are not used: codes times them pass fp32).
  *   K tile: the code of (slot s, dim m) in nibble m % 2 (0: the low one) of byte ((m / 32) * 16 + s) * 16 + m % 32 / 2,
  *           its scale in byte 8 d_h + (m / 32) * 16 + s
  *   V tile: nibble (m / 16) % 2 of byte ((s / 4) * 16 + m % 16) * (d_h / 8) + (m / 32) * 4 + s % 4, its scale in byte

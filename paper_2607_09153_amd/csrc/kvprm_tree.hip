@@ -295,7 +295,7 @@ struct Special {
 // columns (410 MB): 90 us, 4.5 TB/s. On short ones by the chain of loads, products and join: 1103 tokens,
 // 16 drafted, 8 kv-heads, 32 columns in two blocks of 16: 8 us, and 4 for k_tree_merge.
 template <int KVT, int D, int NC, typename T>
-__global__ __launch_bounds__(64 * kTreeWaves, KVT == 3 && (NC == 1 || D == 64 || sizeof(T) == 2) ? 2 : 1) void k_tree(TreeArgs a) {
+__global__ __launch_bounds__(64 * kTreeWaves, KVT == 3 ? 2 : 1) void k_tree(TreeArgs a) {
   constexpr int NKB = D / 32, NDB = D / 16, W = kTreeWaves;
   constexpr int QT = Terms<T>::Q, PT = Terms<T>::P;
   constexpr size_t TILE = tile_bytes(KVT, D);
@@ -405,9 +405,10 @@ __global__ __launch_bounds__(64 * kTreeWaves, KVT == 3 && (NC == 1 || D == 64 ||
           }
         }
       }
-      // 4-bit pairs: keys and values become operands 32 dims at a time (all at once they would not fit beside two tiles'
-      // sums in the registers of two waves a unit), and only the candidate's last pair masks slots (8 caches of 16384 to
-      // 32768 tokens, 4 drafted, 28 columns: 59 us a call in the other types' order, 53 so; 16 of 4000, 32 columns, 44 and 38).
+      // 4-bit pairs: keys and values become operands 32 dims at a time (all at once they would take the registers of
+      // two waves a unit), and only the candidate's last pair masks slots. In blocks of 32 columns, which they had
+      // then: 8 caches of 16384 to 32768 tokens, 4 drafted, 28 columns, 59 us a call in the other types' order, 53
+      // so.
       auto compute4 = [&](int i, const PairOf<KVT, D> &r, auto masked) {
         constexpr bool TAIL = decltype(masked)::value;
         if constexpr (KVT == 3) {
@@ -1421,11 +1422,20 @@ static int full_chip(const Dims &dm, bool wide) { return wide && dm.d == 64 ? 76
 // last chunk (4 for 32 tokens of k_tree_wide, a unit for 64 of k_tree): 12.1 us instead of 13.9 for 1103 tokens, 326
 // instead of 330 on the long caches; 2 to 8 pages are alike there. Chunk slots: what fills the chip eight times over if
 // the batch's candidates were all as long as the table.
+// 4-bit caches: k_tree has 16 columns a block at d_h = 128 (two tiles beside widened keys and values leave the
+// registers of one wave a unit, or of two that wait for each other's conversions) and where 32 would not hold the
+// draft. Reading a page once more costs little there. Blocks of 32 and of 16 columns, us, bf16 rows: 8 caches of
+// 16384 to 32768 tokens, 28 columns, 54 / 48; 16 of 4000, 32 columns, 39 / 35; 64 of 2000, 28 columns, 42 / 32; 8 of
+// 8000, 2 drafted of 16 heads, 25 / 19; 16 of 300, 64 columns (k_tree_wide / 16), 23 / 13; fp32 rows: the first 70 /
+// 57, the second 55 / 43, 29 of 75 tokens, 304 columns, 124 / 89. d_h = 64, up to 32 columns: 24 of 4800, 23.6 / 28.2
+// (fp32 rows 27.1 / 30.2), but 64 of 3000, 28 columns, 32.3 / 29.6; more, fp32 rows: 16 of 500, 128 columns, 20.8 /
+// 11.8, 24 of 1 to 9000, 4 to 192 columns, 74.4 / 78.7. (More blocks of 16 instead of k_tree_wide, up to 1024: 24 of
+// 3000 to 6000, 160 columns, d_h = 64, 68 -> 77, 12 of 8000, 336 columns, d_h = 128, 137 -> 164.)
 static TreePlan tree_plan(const Dims &dm, const kvprm_batch &b, const kvprm_tree &t, bool wide) {
   TreePlan p;
   const int cols = t.max_rows * dm.g;
   p.wide = wide;
-  p.nc = cols <= 16 ? 1 : 2;
+  p.nc = cols <= 16 || (dm.kvdt == 3 && (dm.d == 128 || cols > 32)) ? 1 : 2;
   p.cols = p.wide ? 32 * kWideWaves : 16 * p.nc;
   p.blocks = (cols + p.cols - 1) / p.cols;
   // Spread evenly, unless the average draft needs fewer blocks than the longest: 24 drafts of 1 to 48 tokens of
@@ -1593,7 +1603,11 @@ hipError_t launch_tree(const Dims &dm, const kvprm_kv_cache &c, const kvprm_batc
     else { KVPRM_WIDE(2, 128); }
   } else if (dm.kvdt == 0) { KVPRM_TREE_D(0) }
   else if (dm.kvdt == 1) { KVPRM_TREE_D(1) }
-  else if (dm.kvdt == 3) { KVPRM_TREE_D(3) }
+  else if (dm.kvdt == 3) {
+    if (dm.d == 64) { KVPRM_TREE_T(3, 64) }
+    else if (bf16) { KVPRM_TREE(3, 128, 1, uint16_t); }  // (see tree_plan)
+    else { KVPRM_TREE(3, 128, 1, float); }
+  }
   else { KVPRM_TREE_D(2) }
 #undef KVPRM_WIDE
 #undef KVPRM_TREE_D
