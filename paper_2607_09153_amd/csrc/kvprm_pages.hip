@@ -58,6 +58,19 @@ static PageScan carve_pages(int64_t num_pages, void *base) {
 int64_t max_pool_pages() { return (int64_t)kMaxScanBlocks * kScanPages; }
 size_t pages_ws_bytes(int64_t num_pages) { return carve_pages(num_pages, nullptr).bytes; }
 
+// Division by a number that a call keeps, without a divide: the quotient by its rounded-down reciprocal is right or one too
+// small for x < 2^31.
+struct Divisor {
+  uint32_t d, inv;
+  static Divisor of(uint64_t n) { return {(uint32_t)n, n ? (uint32_t)(0xFFFFFFFFull / n) : 0}; }
+  __device__ __forceinline__ uint32_t split(uint32_t x, uint32_t &rest) const {
+    uint32_t q = __umulhi(x, inv);
+    rest = x - q * d;
+    if (rest >= d) ++q, rest -= d;
+    return q;
+  }
+};
+
 struct PageArgs {
   int num_pages, rows, max_pages;
   const int32_t *table, *lengths, *held;
@@ -75,6 +88,7 @@ struct PageArgs {
   float *scale[2];
   int layers, nkv;
   size_t page_bytes;  // of one page and layer, keys or values
+  Divisor by_entries, by_to, by_pieces, by_parts;  // max_pages; to_pages; page_bytes / 16; 2 layers
 };
 
 // The k-th page (from 0) whose bit is set: a search among the blocks' sums, one among the block's words, then the
@@ -401,7 +415,7 @@ __global__ __launch_bounds__(256) void k_compact_move(PageArgs a) {
 // counts and tables (read from the caches, each for itself), then write their share of the results and copy their
 // share of the pages. Nothing that a block reads is written by another, so that no block waits for one. Against the
 // launches above, whose plan is spread over the blocks (fork / compact, us): a beam of 64 rows of 290 pages in a pool of
-// 2270, 31 copies of 917 KB: 26 instead of 41; 4 rows of 10 pages 7 / 7, 20 / 19; 16384 pages, 64 rows of 200 entries
+// 2270, 31 copies of 917 KB: 24 instead of 41; 4 rows of 10 pages 7 / 7, 20 / 19; 16384 pages, 64 rows of 200 entries
 // 19 / 26, 31 / 39; 17900 pages, 256 rows of 300 entries 42 / 35, 56 / 33.
 constexpr int kOnePages = 16384, kOneThreads = 1024;
 constexpr int64_t kOneEntries = 1 << 17;  // entries of the rows
@@ -455,26 +469,50 @@ __device__ __forceinline__ int rank_word(const WordScan &s, int page) {
   return s.before[page >> 6] + __popcll(s.mask[page >> 6] & ((1ull << (page & 63)) - 1));
 }
 
-// f(row, entry, id) for every entry that a row holds; held: the rows' counts, in range. Eight loads in flight a thread.
-template <typename F>
-__device__ __forceinline__ void each_entry(const PageArgs &a, const int32_t *held, F f) {
-  constexpr int U = 8;
-  const uint32_t total = (uint32_t)(a.rows * a.max_pages);  // (at most kOneEntries)
-  for (uint32_t e0 = threadIdx.x; e0 < total; e0 += U * kOneThreads) {
-    int id[U], row[U], c[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const uint32_t e = min(e0 + u * kOneThreads, total - 1);
-      row[u] = (int)(e / (uint32_t)a.max_pages);
-      c[u] = (int)(e - (uint32_t)row[u] * a.max_pages);
-      if (e0 + u * kOneThreads >= total || c[u] >= held[row[u]]) c[u] = -1;
-      id[u] = a.table[e];
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (c[u] >= 0) f(row[u], c[u], id[u]);
+// The entries of the rows, eight in flight a thread; the first ones are asked for before anything else is known (with rows'
+// numbers, lengths and counts asked for then too, and no divides: the beam of 64 rows 25.9 -> 24.2 us, 16 rows of up to
+// 144 pages 10.1 -> 9.0).
+struct Entries {
+  static constexpr int U = 8;
+  int id[U];
+  __device__ __forceinline__ static uint32_t total(const PageArgs &a) {  // (at most kOneEntries)
+    return (uint32_t)(a.rows * a.max_pages);
   }
-}
+  __device__ __forceinline__ void load(const PageArgs &a, uint32_t e0) {
+    const uint32_t n = total(a);
+    if (n == 0) return;
+#pragma unroll
+    for (int u = 0; u < U; ++u) id[u] = a.table[min(e0 + u * kOneThreads, n - 1)];
+  }
+  // f(row, entry, id) for every entry that a row holds; held: the rows' counts, in range.
+  template <typename F>
+  __device__ __forceinline__ void each(const PageArgs &a, const int32_t *held, F f) {
+    const uint32_t n = total(a);
+    for (uint32_t e0 = threadIdx.x; e0 < n; e0 += U * kOneThreads) {
+      int now[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) now[u] = id[u];
+      if (e0 + U * kOneThreads < n) load(a, e0 + U * kOneThreads);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint32_t e = min(e0 + u * kOneThreads, n - 1);
+        uint32_t c;
+        const int row = (int)a.by_entries.split(e, c);
+        if (e0 + u * kOneThreads < n && (int)c < held[row]) f(row, (int)c, now[u]);
+      }
+    }
+  }
+};
+// Counts of the pages of this wave's first words, asked for early (word wave + 16 k, k < N).
+template <int N>
+struct Counts {
+  int n[N];
+  __device__ __forceinline__ void load(const PageArgs &a) {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+#pragma unroll
+    for (int k = 0; k < N; ++k) n[k] = a.refs[min((wave + kOneThreads / 64 * k) * 64 + lane, a.num_pages - 1)];
+  }
+};
 
 // Pages src[i] -> dst[i] of every layer, keys and values, spread over all threads of the grid in pieces of 16 bytes,
 // two of them in flight a thread (I: a type that counts them). Past the caches both ways: 485 pages of 917 KB (890 MB
@@ -482,7 +520,7 @@ __device__ __forceinline__ void each_entry(const PageArgs &a, const int32_t *hel
 template <typename I>
 __device__ __forceinline__ void copy_pieces(const PageArgs &a, const int32_t *src, const int32_t *dst, I total) {
   constexpr int U = 2;
-  const uint32_t per = (uint32_t)(a.page_bytes / 16);
+  const uint32_t per = a.by_pieces.d;
   const I threads = (I)gridDim.x * kOneThreads;
   for (I e0 = (I)blockIdx.x * kOneThreads + threadIdx.x; e0 < total; e0 += U * threads) {
     uint4 v[U];
@@ -490,8 +528,10 @@ __device__ __forceinline__ void copy_pieces(const PageArgs &a, const int32_t *sr
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const I e = min(e0 + u * threads, total - 1);
-      const uint32_t unit = (uint32_t)(e / per), at = (uint32_t)(e - (I)unit * per);
-      const uint32_t i = unit / (2 * a.layers), lp = unit - i * 2 * a.layers;
+      uint32_t unit, at, lp;
+      if constexpr (sizeof(I) == 4) unit = a.by_pieces.split(e, at);
+      else unit = (uint32_t)(e / per), at = (uint32_t)(e - (I)unit * per);
+      const uint32_t i = a.by_parts.split(unit, lp);
       char *pool = a.pool[lp & 1];
       const size_t base = (size_t)(lp >> 1) * a.num_pages;
       v[u] = ld_stream((const uint4 *)(pool + (base + src[i]) * a.page_bytes) + at);
@@ -530,21 +570,23 @@ __global__ __launch_bounds__(kOneThreads) void k_fork_one(PageArgs a) {
   __shared__ int child_s[kMaxBatch], eldest_s[kMaxBatch];   // of a row of `from`: its children, the first of them
   __shared__ int full_s[kMaxBatch], kept_s[kMaxBatch];      // its full pages; whether a child takes the next one
   __shared__ int src_s[kMaxBatch], dst_s[kMaxBatch];
-  __shared__ int held_s[kMaxBatch];
+  __shared__ int held_s[kMaxBatch], len_s[kMaxBatch];
   __shared__ int bad_s, empty_s, copies_s;
-  bool bad = false;
-  if (tid < a.rows) {
-    const int held = a.held[tid];
-    bad = held < 0 || held > a.max_pages;
-    held_s[tid] = bad ? 0 : held;
-  }
+  const int i = tid;
+  const int held = tid < a.rows ? a.held[tid] : 0, len = tid < a.rows ? a.lengths[tid] : 0;
+  const int p = i < a.children ? a.parent[i] : -1;
+  const int64_t room = i < a.children && a.room ? a.room[i] : 0;
+  Entries entries;
+  entries.load(a, tid);
+  Counts<4> counts;
+  counts.load(a);
+  bool bad = held < 0 || held > a.max_pages;
+  if (tid < a.rows) held_s[tid] = bad ? 0 : held, len_s[tid] = len;
   for (int i = tid; i < P; i += kOneThreads) count[i] = 0;
   for (int i = tid; i < words; i += kOneThreads) source[i] = 0;
   if (tid < kMaxBatch) child_s[tid] = kept_s[tid] = full_s[tid] = 0, eldest_s[tid] = kMaxBatch;
   if (tid == 0) bad_s = empty_s = copies_s = 0;
   __syncthreads();
-  const int i = tid;
-  const int p = i < a.children ? a.parent[i] : -1;
   bad = bad || p >= a.rows;
   if (p >= 0 && p < a.rows) {
     atomicAdd(&child_s[p], 1);
@@ -553,10 +595,9 @@ __global__ __launch_bounds__(kOneThreads) void k_fork_one(PageArgs a) {
   __syncthreads();
   if (i < a.children) {
     RowPlan r = {0, 0, 0, -1};
-    const int64_t room = a.room ? a.room[i] : 0;
     bad = bad || room < 0;
     if (p >= 0 && !bad) {
-      r.len = a.lengths[p];
+      r.len = len_s[p];
       bad = r.len < 0 || r.len > (int64_t)held_s[p] * kPage;
     }
     const int64_t want = (r.len + room + kPage - 1) / kPage;
@@ -586,18 +627,18 @@ __global__ __launch_bounds__(kOneThreads) void k_fork_one(PageArgs a) {
     if (blockIdx.x == 0 && tid < 4) a.result[tid] = tid == 0 ? 2 : 0;
     return;
   }
-  each_entry(a, held_s, [&](int row, int c, int id) {
+  entries.each(a, held_s, [&](int row, int c, int id) {
     const uint64_t share = c < full_s[row] ? child_s[row] : c == full_s[row] ? kept_s[row] : 0;
     if (id < 0 || id >= P) bad = true;
     else atomicAdd((unsigned long long *)&count[id], (unsigned long long)(share << 32 | 1));
   });
   __syncthreads();
   int empty = 0;
-  for (int word = wave; word < words; word += kOneThreads / 64) {
+  auto word_of = [&](int word, int refs) {
     const int page = word * 64 + lane;
     bool free = false;
     if (page < P) {
-      const int64_t others = (int64_t)a.refs[page] - (uint32_t)count[page], n = others + (int64_t)(count[page] >> 32);
+      const int64_t others = (int64_t)refs - (uint32_t)count[page], n = others + (int64_t)(count[page] >> 32);
       bad = bad || others < 0 || n > INT32_MAX;
       empty += n == 0;
       free = n == 0 && !(source[word] >> lane & 1);
@@ -605,7 +646,12 @@ __global__ __launch_bounds__(kOneThreads) void k_fork_one(PageArgs a) {
     }
     const uint64_t m = __ballot(free);
     if (lane == 0) mask[word] = m;
-  }
+  };
+  constexpr int WAVES = kOneThreads / 64;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (wave + WAVES * k < words) word_of(wave + WAVES * k, counts.n[k]);
+  for (int word = wave + 4 * WAVES; word < words; word += WAVES) word_of(word, a.refs[min(word * 64 + lane, P - 1)]);
   empty = lane_scan(empty);
   if (lane == 63 && empty) atomicAdd(&empty_s, empty);
   if (bad) bad_s = 1;
@@ -635,9 +681,10 @@ __global__ __launch_bounds__(kOneThreads) void k_fork_one(PageArgs a) {
     dst_s[k] = select_word(ws, first_s[i]);  // (the first fresh page of the row)
   }
   __syncthreads();
-  const int64_t threads = (int64_t)gridDim.x * kOneThreads, me = (int64_t)blockIdx.x * kOneThreads + tid;
-  for (int64_t e = me; e < (int64_t)a.children * a.to_pages; e += threads) {
-    const int row = (int)(e / a.to_pages), c = (int)(e - (int64_t)row * a.to_pages);
+  const uint32_t threads = gridDim.x * kOneThreads, me = blockIdx.x * kOneThreads + tid;
+  for (uint32_t e = me; e < (uint32_t)(a.children * a.to_pages); e += threads) {  // (at most 2^28)
+    uint32_t col;
+    const int row = (int)a.by_to.split(e, col), c = (int)col;
     const RowPlan r = row_s[row];
     int id = -1;
     if (c < r.shared) id = a.table[(size_t)a.parent[row] * a.max_pages + c];
@@ -645,7 +692,7 @@ __global__ __launch_bounds__(kOneThreads) void k_fork_one(PageArgs a) {
     a.to_table[e] = id;
     if (c == 0) a.to_lengths[row] = r.len, a.to_held[row] = r.held;
   }
-  for (int64_t page = me; page < P; page += threads) {
+  for (uint32_t page = me; page < (uint32_t)P; page += threads) {
     const bool free = mask[page >> 6] >> (page & 63) & 1;
     a.new_refs[page] = free && rank_word(ws, (int)page) < need ? 1 : (int)count[page];
   }
@@ -659,22 +706,28 @@ __global__ __launch_bounds__(kOneThreads) void k_compact_one(PageArgs a) {
   int32_t *before = (int32_t *)(mask + words), *src = before + words, *dst = src + P / 2;
   __shared__ int held_s[kMaxBatch];
   __shared__ int bad_s;
+  const int held = tid < a.rows ? a.held[tid] : 0;
+  Counts<4> counts;
+  counts.load(a);
+  Entries entries;
+  entries.load(a, tid);
   if (tid == 0) bad_s = 0;
-  bool bad = false;
-  if (tid < a.rows) {
-    const int held = a.held[tid];
-    bad = held < 0 || held > a.max_pages;
-    held_s[tid] = bad ? 0 : held;
-  }
-  for (int word = wave; word < words; word += kOneThreads / 64) {
-    const int page = word * 64 + lane, n = page < P ? a.refs[page] : 0;
+  bool bad = held < 0 || held > a.max_pages;
+  if (tid < a.rows) held_s[tid] = bad ? 0 : held;
+  auto word_of = [&](int word, int refs) {
+    const int n = word * 64 + lane < P ? refs : 0;
     bad = bad || n < 0;
     const uint64_t m = __ballot(n > 0);
     if (lane == 0) mask[word] = m;
-  }
+  };
+  constexpr int WAVES = kOneThreads / 64;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (wave + WAVES * k < words) word_of(wave + WAVES * k, counts.n[k]);
+  for (int word = wave + 4 * WAVES; word < words; word += WAVES) word_of(word, a.refs[min(word * 64 + lane, P - 1)]);
   const WordScan ws = {mask, before, words};
   const int live = scan_words(ws);
-  each_entry(a, held_s, [&](int, int, int id) {
+  entries.each(a, held_s, [&](int, int, int id) {
     bad = bad || id < 0 || id >= P || !(mask[id >> 6] >> (id & 63) & 1);
   });
   if (bad) bad_s = 1;
@@ -695,17 +748,18 @@ __global__ __launch_bounds__(kOneThreads) void k_compact_one(PageArgs a) {
   __syncthreads();
   // (alive pages only)
   auto goes = [&](int page) { return page < live ? page : dst[rank_word(ws, page) - stay]; };
-  const int64_t threads = (int64_t)gridDim.x * kOneThreads, me = (int64_t)blockIdx.x * kOneThreads + tid;
-  for (int64_t page = me; page < P; page += threads) {
+  const uint32_t threads = gridDim.x * kOneThreads, me = blockIdx.x * kOneThreads + tid;
+  for (uint32_t page = me; page < (uint32_t)P; page += threads) {
     const bool alive = mask[page >> 6] >> (page & 63) & 1;
     const int to = alive ? goes((int)page) : -1;
     a.moved[page] = to;
     if (alive) a.new_refs[to] = a.refs[page];
-    if (page >= live) a.new_refs[page] = 0;
+    if ((int)page >= live) a.new_refs[page] = 0;
   }
-  for (int64_t e = me; e < (int64_t)a.rows * a.max_pages; e += threads) {
-    const int row = (int)(e / a.max_pages), c = (int)(e - (int64_t)row * a.max_pages);
-    a.to_table[e] = c < held_s[row] ? goes(a.table[e]) : -1;
+  for (uint32_t e = me; e < Entries::total(a); e += threads) {
+    uint32_t c;
+    const int row = (int)a.by_entries.split(e, c);
+    a.to_table[e] = (int)c < held_s[row] ? goes(a.table[e]) : -1;
   }
   copy_pages(a, src, dst, moves);
 }
@@ -737,6 +791,9 @@ static PageArgs page_args(const Dims &dm, const kvprm_kv_cache &c, const kvprm_p
   if (dm.kvdt == 2) a.scale[0] = (float *)c.k_scale, a.scale[1] = (float *)c.v_scale;
   a.layers = dm.layers, a.nkv = dm.nkv;
   a.page_bytes = dm.nkv * tile_bytes(dm.kvdt, dm.d);
+  a.by_entries = Divisor::of(a.rows > 0 ? a.max_pages : 0);
+  a.by_pieces = Divisor::of(a.page_bytes / 16);
+  a.by_parts = Divisor::of(2 * (uint64_t)a.layers);
   return a;
 }
 
@@ -745,6 +802,7 @@ hipError_t launch_fork_pages(const Dims &dm, const kvprm_kv_cache &c, const kvpr
                              int32_t *new_refs, int32_t *result, void *ws, hipStream_t s) {
   PageArgs a = page_args(dm, c, from, refs, new_refs, result, ws);
   a.children = to.rows, a.to_pages = to.max_pages;
+  a.by_to = Divisor::of(a.children > 0 ? a.to_pages : 0);
   a.parent = parent, a.room = room;
   a.to_table = to.page_table, a.to_lengths = to.lengths, a.to_held = to.held;
   if (const int n = one_launch(a)) {
