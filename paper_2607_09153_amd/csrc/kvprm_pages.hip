@@ -569,7 +569,7 @@ __global__ __launch_bounds__(kOneThreads) void k_fork_one(PageArgs a) {
   __shared__ int first_s[kMaxBatch + 1];                    // fresh pages of the rows before
   __shared__ int child_s[kMaxBatch], eldest_s[kMaxBatch];   // of a row of `from`: its children, the first of them
   __shared__ int full_s[kMaxBatch], kept_s[kMaxBatch];      // its full pages; whether a child takes the next one
-  __shared__ int src_s[kMaxBatch], dst_s[kMaxBatch];
+  __shared__ int src_s[kMaxBatch], dst_s[kMaxBatch];        // the copies; dst_s is the child's number before
   __shared__ int held_s[kMaxBatch], len_s[kMaxBatch];
   __shared__ int bad_s, empty_s, copies_s;
   const int i = tid;
@@ -585,7 +585,7 @@ __global__ __launch_bounds__(kOneThreads) void k_fork_one(PageArgs a) {
   for (int i = tid; i < P; i += kOneThreads) count[i] = 0;
   for (int i = tid; i < words; i += kOneThreads) source[i] = 0;
   if (tid < kMaxBatch) child_s[tid] = kept_s[tid] = full_s[tid] = 0, eldest_s[tid] = kMaxBatch;
-  if (tid == 0) bad_s = empty_s = copies_s = 0;
+  if (tid == 0) bad_s = empty_s = 0;
   __syncthreads();
   bad = bad || p >= a.rows;
   if (p >= 0 && p < a.rows) {
@@ -658,13 +658,17 @@ __global__ __launch_bounds__(kOneThreads) void k_fork_one(PageArgs a) {
   const WordScan ws = {mask, before, words};
   const int have = scan_words(ws);
   if (tid < 64) {
-    int sum = 0;
+    // The copies are listed in the order of the children: every block takes its share of the pieces by its own list.
+    int sum = 0, copies = 0;
     for (int i0 = 0; i0 < a.children; i0 += 64) {
       const int c = i0 + tid, n = c < a.children ? row_s[c].held - row_s[c].shared : 0, cum = lane_scan(n);
+      const int copy = c < a.children ? row_s[c].copy : -1, at = lane_scan(copy >= 0 ? 1 : 0);
       if (c < a.children) first_s[c] = sum + cum - n;
+      if (copy >= 0) src_s[copies + at - 1] = copy, dst_s[copies + at - 1] = c;
       sum += __builtin_amdgcn_readlane(cum, 63);
+      copies += __builtin_amdgcn_readlane(at, 63);
     }
-    if (tid == 0) first_s[a.children] = sum;
+    if (tid == 0) first_s[a.children] = sum, copies_s = copies;
   }
   __syncthreads();
   const int need = first_s[a.children], status = bad_s ? 2 : need > have ? 1 : 0;
@@ -675,11 +679,7 @@ __global__ __launch_bounds__(kOneThreads) void k_fork_one(PageArgs a) {
     a.result[3] = status ? 0 : empty_s - need;
   }
   if (status) return;
-  if (i < a.children && row_s[i].copy >= 0) {
-    const int k = atomicAdd(&copies_s, 1);  // (the order of the copies is of no effect)
-    src_s[k] = row_s[i].copy;
-    dst_s[k] = select_word(ws, first_s[i]);  // (the first fresh page of the row)
-  }
+  if (tid < copies_s) dst_s[tid] = select_word(ws, first_s[dst_s[tid]]);  // (the first fresh page of the row)
   __syncthreads();
   const uint32_t threads = gridDim.x * kOneThreads, me = blockIdx.x * kOneThreads + tid;
   for (uint32_t e = me; e < (uint32_t)(a.children * a.to_pages); e += threads) {  // (at most 2^28)

@@ -264,3 +264,19 @@ def test_streams_and_graph():
         assert table.cpu().tolist() == [r + [-1] * (width - len(r)) for r in out]
         assert r2.cpu().tolist() == after and moved.cpu().tolist() == to
         pool.same()
+
+
+@pytest.mark.parametrize("cdt,layers", [("fp8", 3), ("bf16", 5), ("fp4", 1)])
+@pytest.mark.parametrize("children", [65, 128, 256])
+def test_many_copies_in_one_launch(cdt, layers, children):
+    """More children than a wave has lanes, in a pool that one launch serves. Most of them copy a partly filled page:
+    every block takes its share of all copies' bytes, so that the blocks have to list the copies in one order."""
+    _say("copies", cdt, children)
+    pool = Pool(cdt, 6 * children + 200, children, layers=layers)
+    rng = np.random.default_rng(children)
+    rows, lengths, refs = _case(rng, pool.pages, 20, 3, 5)
+    lengths = [min(n + (n % 16 == 0), 16 * len(r)) for n, r in zip(lengths, rows)]
+    parent = [int(p) for p in rng.integers(0, 20, size=children)]
+    room = [int(r) for r in rng.choice([0, 1, 16, 40], size=children)]
+    status, _, lens, _ = pool.fork(rows, lengths, parent, room, refs, 9, 12)
+    assert status == 0 and sum(n % 16 > 0 for n in lens) > children // 2
