@@ -143,7 +143,8 @@ typedef struct {
  * same physical pages in every member's row (not checked: the shared part is read through the
  * first member's row). Groups tile [0, B). With bf16, fp8 or 4-bit caches and at most 64 groups the
  * shared pages are read once per group instead of once per member; otherwise the hint is
- * ignored. A valid hint changes results only by floating-point summation order. */
+ * ignored. A valid hint changes results only by floating-point summation order (4-bit caches: and by
+ * the bits that kvprm_attention keeps of a query). */
 typedef struct {
   int32_t batch;                        /* B >= 0 */
   const int32_t *page_table;            /* device [B][max_pages] */
@@ -174,7 +175,7 @@ kvprm_status kvprm_workspace_size(kvprm_handle h, const kvprm_batch *batch, size
 /* Eq. (score) for every candidate: scores[b] = P(+) in [0, 1] and, if logits != NULL,
  * logits[b] = z_b = w_r . RMSNorm(x_b) + b_r (fp32, device [B]). The residual stream, queries,
  * softmax state and accumulators are fp32; weights and cache are read at their stored
- * precision. B = 0 returns KVPRM_OK and enqueues nothing. The workspace (device, 256-byte
+ * precision (4-bit caches: queries as kvprm_attention has them). B = 0 returns KVPRM_OK and enqueues nothing. The workspace (device, 256-byte
  * aligned, >= kvprm_workspace_size bytes) is scratch owned by the call until the stream
  * passes it; its contents on entry do not matter. */
 kvprm_status kvprm_score(kvprm_handle h, const kvprm_kv_cache *cache, const kvprm_batch *batch,
@@ -207,7 +208,9 @@ kvprm_status kvprm_score_static(kvprm_handle h, const kvprm_kv_cache *cache,
  * q-head h, o[b][h] = softmax(q K^T / sqrt(d_h)) V over the L_b cached keys/values of `layer`
  * and the extra key/value k_self[b][h / g], v_self[b][h / g] (the verify token's own).
  * q: device fp32 [B][n_q][d_h] (already rotated); k_self, v_self: device fp32 [B][n_kv][d_h];
- * o: device fp32 [B][n_q][d_h]. The prefix-sharing hint is honoured as in kvprm_score. */
+ * o: device fp32 [B][n_q][d_h]. The prefix-sharing hint is honoured as in kvprm_score.
+ * Over 4-bit caches a query's value meets the cached keys with an error of at most 2^-29 of the largest of its 32 dims (32 i
+ * to 32 i + 31; d_h = 64: 2^-33), those of a hinted prefix and other caches' with 2^-24 of itself. */
 kvprm_status kvprm_attention(kvprm_handle h, const kvprm_kv_cache *cache, const kvprm_batch *batch,
                              int32_t layer, const float *q, const float *k_self,
                              const float *v_self, void *workspace, size_t ws_bytes, float *o,

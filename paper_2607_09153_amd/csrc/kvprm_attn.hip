@@ -7,6 +7,7 @@
 #include <string.h>
 
 #include <type_traits>
+#include <utility>
 
 #include "kvprm_internal.h"
 #include "kvprm_attn_common.h"
@@ -264,20 +265,25 @@ __device__ __forceinline__ void walk_pages(const AttnArgs &a, int b, int j, int 
 
 // walk_pages over a 4-bit cache. Scores come from the matrix cores' scaled products of 4-bit keys as they lie in memory (16
 // tokens x 128 dims, a scale byte per lane: its 32 dims of its token) and the query in terms of 6 bits (e2m3), each with
-// a power of two for the lane's 32 dims: kTerms4 terms, each 2^-4 of the one before, keep 2^-20 of the 32 dims' largest.
-// (Such a product takes the time of a bf16 one of 32 dims, so that five terms cost 5/12 of three bf16 terms', and no
+// a power of two for the lane's 32 dims: kTerms4 terms, each 2^-4 of the one before. What a term leaves is at most 1/4 of
+// its scale, 1/8 and 1/16 after a second and a third, so that T terms are off by 2^-4 16^-(T-1) of the first scale, which is
+// below the 32 dims' largest / 3.75: 2^-29 of it for seven terms. A dim 1000 times the others leaves those 2^-19 of
+// themselves so, whatever its own keys are; five terms (2^-21) left 2^-11 and were off by 7e-4 in such scores
+// of 12. Seven terms take 2 to 5% more time than five (8 of 16384 to 32768 tokens, 28/4 heads 32.0 -> 33.1 us, 24 of 8000 to
+// 16000, 16/8 heads 66.8 -> 69.2, 64 of 500, 28/4 heads 10.6 -> 11.0), eight 5 to 11% (their registers leave two waves a unit).
+// (Such a product takes the time of a bf16 one of 32 dims, so that seven terms cost 7/12 of three bf16 terms', and no
 // conversion of keys. 8-bit terms keep no more bits and take twice the time.) At d_h = 64 a product holds two terms, one in
-// lanes 0 to 31 and one in the others, which read the same keys. Values become bf16 (exactly) for bf16 products with
+// lanes 0 to 31 and one in the others, which read the same keys: eight terms. Values become bf16 (exactly) for bf16 products with
 // weights in three terms. A step without a new maximum does not touch acc; slots at or past L are masked in the
 // chunk's last pair alone.
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-constexpr int kTerms4 = 5;
+constexpr int kTerms4 = 7;
 
 template <int D>
 struct Query4 {
   static constexpr int NQ = D == 128 ? kTerms4 : (kTerms4 + 1) / 2;  // products
   uint32_t t[NQ][6];
-  uint32_t scale[2];  // bytes: of products 0 to 3, and of the fourth
+  uint32_t scale[2];  // bytes: of products 0 to 3, and of the others
 };
 
 // The terms of a column's query (`present`: it exists) times `factor`, for this lane's 32 dims. A query that is not finite
@@ -334,25 +340,20 @@ __device__ __forceinline__ floatx4 score_term4(const uint4 &key, uint32_t scale,
   // (formats 4: e2m1, 2: e2m3)
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, 2, 0, (int)scale, K & 3, (int)q.scale[K >> 2]);
 }
-// Two pages' scores, their chains of products side by side.
+// Two pages' scores, their chains of products side by side, the smallest terms first (their sum is rounded at its own size:
+// errors of 3.1e-7 of the result's norm, 5e-7 with the largest first).
+template <int D, int... K>
+__device__ __forceinline__ void score_terms4(std::integer_sequence<int, K...>, const uint4 (&key)[2],
+                                             const uint32_t (&scale)[2], const Query4<D> &q, floatx4 &sa, floatx4 &sb) {
+  constexpr int LAST = Query4<D>::NQ - 1;
+  ((sa = score_term4<D, LAST - K>(key[0], scale[0], q, sa), sb = score_term4<D, LAST - K>(key[1], scale[1], q, sb)), ...);
+}
 template <int D>
 __device__ __forceinline__ void scores4(const uint4 (&key)[2], const uint32_t (&scale)[2], const Query4<D> &q, floatx4 &sa,
                                         floatx4 &sb) {
   sa = sb = floatx4{0.f, 0.f, 0.f, 0.f};
-  sa = score_term4<D, 0>(key[0], scale[0], q, sa);
-  sb = score_term4<D, 0>(key[1], scale[1], q, sb);
-  sa = score_term4<D, 1>(key[0], scale[0], q, sa);
-  sb = score_term4<D, 1>(key[1], scale[1], q, sb);
-  sa = score_term4<D, 2>(key[0], scale[0], q, sa);
-  sb = score_term4<D, 2>(key[1], scale[1], q, sb);
-  if constexpr (D == 128) {
-    sa = score_term4<D, 3>(key[0], scale[0], q, sa);
-    sb = score_term4<D, 3>(key[1], scale[1], q, sb);
-    sa = score_term4<D, 4>(key[0], scale[0], q, sa);
-    sb = score_term4<D, 4>(key[1], scale[1], q, sb);
-  }
+  score_terms4<D>(std::make_integer_sequence<int, Query4<D>::NQ>(), key, scale, q, sa, sb);
 }
-static_assert(kTerms4 == 5, "products of scores4");
 
 // The larger of two, NaN if one is (one instruction; fmaxf takes another for each operand that may be a signalling NaN).
 __device__ __forceinline__ float larger(float x, float y) { return __builtin_elementwise_maximum(x, y); }
