@@ -90,13 +90,14 @@ __device__ __forceinline__ void online_step(const uint4 *KA, const uint4 *KB, co
 #pragma unroll
   for (int i = 1; i < 8; ++i) mx = fmaxf(mx, sv[i]);
   mx = column_max(mx);
-  const float m_new = fmaxf(m_run, mx);  // finite once any valid token has been seen
-  const float alpha = (m_new == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+  // (-inf until a score is not: a masked token's or an overflowed one's, whose weights are 0)
+  const float m_new = fmaxf(m_run, mx), ms = m_new == -INFINITY ? 0.f : m_new;
+  const float alpha = __builtin_amdgcn_exp2f(m_run - ms);
   m_run = m_new;
   float pv[8], psum = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    pv[i] = ok[i] ? __builtin_amdgcn_exp2f(sv[i] - m_new) : 0.f;
+    pv[i] = ok[i] ? __builtin_amdgcn_exp2f(sv[i] - ms) : 0.f;
     psum += pv[i];
   }
   l_run = l_run * alpha + psum;
@@ -410,9 +411,10 @@ __device__ __forceinline__ void walk_pages4(const AttnArgs &a, int b, int j, int
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[nb][i] *= alpha;
     }
+    const float ms = m_run == -INFINITY ? 0.f : m_run;  // (all scores overflowed so far: weights of 0)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      s[i] = __builtin_amdgcn_exp2f(s[i] - m_run);  // (the pair's first token counts: m_run is not -inf)
+      s[i] = __builtin_amdgcn_exp2f(s[i] - ms);
       l_run += s[i];
     }
     uint32_t p[3][4];
@@ -1143,13 +1145,14 @@ __device__ __forceinline__ void walk_pages_f32(const AttnArgs &a, int b, int j, 
       sv[i] = t + i < L ? s : -INFINITY;
       mx = fmaxf(mx, sv[i]);
     }
-    const float m_new = fmaxf(m_run, column_max(mx));  // finite: the page holds a valid token
-    const float alpha = expf(m_run - m_new);
+    // (-inf until a token's score is not: scores that overflowed have weights of 0)
+    const float m_new = fmaxf(m_run, column_max(mx)), ms = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = expf(m_run - ms);
     m_run = m_new;
     float pv[4], ps = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      pv[i] = t + i < L ? expf(sv[i] - m_new) : 0.f;
+      pv[i] = t + i < L ? expf(sv[i] - ms) : 0.f;
       ps += pv[i];
     }
     l_run = l_run * alpha + ps;
