@@ -436,8 +436,8 @@ typedef struct {
  * costs no significant bit on either way, so that a code is rounded again only where it leaves e4m3's
  * normal range. Infinities and NaN are stored as NaN in fp8 (and do not enter the scale).
  * FP4_E2M1: the scale of 32 dims of a token is the smallest power of two s with 7 s >= |x| for all of them, 2^-100 to
- * 2^125 (error at most s; a smaller s would not lower it, since codes 4 and 6 lie 2 s apart), codes to the nearest, ties to
- * even. A token's bytes depend on it alone and are never changed by later ones. 32 dims that hold an
+ * 2^125 (error at most s; a smaller s would not lower it, since codes 4 and 6 lie 2 s apart; magnitudes above 7 * 2^125, of
+ * which no scale is that large, become 6 * 2^125, an error of up to 2 s), codes to the nearest, ties to even. A token's bytes depend on it alone and are never changed by later ones. 32 dims that hold an
  * infinity or NaN are stored as code 0 with scale byte 255: NaN, all of them.
  * Rows past max_pages * 16 tokens, with a row number outside [0, num_rows) or whose page id is outside
  * [0, num_pages) are dropped. No page may get rows of two candidates (checked with KVPRM_DEBUG=1).

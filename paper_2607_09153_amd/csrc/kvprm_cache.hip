@@ -589,7 +589,8 @@ __global__ __launch_bounds__(256) void k_read_kv(RowArgs a) {
 
 // Scale byte of 32 values of which the largest magnitude has the bits `amax` (as an integer, so that infinities and
 // NaN are the largest): the exponent, biased by 127, of the smallest s = 2^k with 7 s >= amax (7 = 1.75 * 2^2), from
-// 2^kMinScaleExp to 2^125. Values up to 7 s are off by at most s, as those between codes 4 s and 6 s are. 255 (NaN)
+// 2^kMinScaleExp to 2^125. Values up to 7 s are off by at most s, as those between codes 4 s and 6 s are; those above 7 *
+// 2^125 become 6 * 2^125 and are off by up to 2 s (a larger scale would make codes that pass fp32). 255 (NaN)
 // where the 32 hold something not finite.
 __device__ __forceinline__ uint32_t scale_byte4(uint32_t amax) {
   if (amax >= 0x7F800000u) return 255u;

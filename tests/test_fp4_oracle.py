@@ -101,3 +101,17 @@ def test_forks_that_cannot_be():
                    dict(rows=[[0, 4], [1, 2]])):
         assert cp.fork(**{**ok, **change})[0] == 2
     assert cp.fork(**{**ok, "room": [45], "to_pages": 9})[0] == 1
+
+
+def test_error_of_a_value():
+    """At most s up to 7 s; above 7 * 2^125, where the scale stays 2^125, at most 2 s, and 6 * 2^125 is what remains."""
+    rng = np.random.default_rng(4)
+    x = rng.uniform(-1, 1, size=(400, 32)) * 2.0 ** rng.integers(-90, 128, size=(400, 1))
+    x[0], x[1], x[2] = np.finfo(np.float32).max, 7 * 2.0 ** 125, np.nextafter(np.float32(7 * 2.0 ** 125), np.float32(np.inf))
+    code, scale = fp4.encode(x)
+    s = np.repeat(2.0 ** (scale.astype(np.float64) - 127), 32, axis=-1)
+    off = np.abs(fp4.decode(code, scale) - x)
+    above = np.abs(x) > 7 * 2.0 ** 125
+    assert above[0].all() and above[2].all() and not above[1].any()
+    assert (off[~above] <= s[~above]).all() and (off[above] <= 2 * s[above]).all() and (off[above] > s[above]).all()
+    assert (fp4.decode(code, scale)[above] == 6 * 2.0 ** 125 * np.sign(x[above])).all()
