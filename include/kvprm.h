@@ -534,7 +534,8 @@ kvprm_status kvprm_workspace_size_pages(kvprm_handle h, int32_t num_pages, size_
  * Status 0: done. 1: too few free pages. 2: inconsistent: a parent >= from->rows, a negative room, a held or a parent's
  * length outside its range, an entry outside [0, num_pages), a page with fewer refs than holders, a new row of more than
  * to->max_pages pages. With status 1 or 2 nothing but `result` is written ({1, needed, there were, 0}, {2, 0, 0, 0}).
- * `to` and `from`, refs and new_refs and all others must not overlap (KVPRM_E_INVALID). to->rows = 0 frees all rows.
+ * `to` and `from`, refs and new_refs and all others, the workspace, the pools and their fp8 scales among them, must not
+ * overlap (KVPRM_E_INVALID). to->rows = 0 frees all rows.
  * The pools of `cache` are WRITTEN (fresh copies). parent: device [to->rows]. */
 kvprm_status kvprm_fork_pages(kvprm_handle h, const kvprm_kv_cache *cache, const kvprm_page_rows *from,
                               const kvprm_page_rows *to, const int32_t *parent, const int32_t *room,

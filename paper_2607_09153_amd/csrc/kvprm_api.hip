@@ -1107,15 +1107,31 @@ struct Words {
   int64_t n;
   bool written;
 };
+static bool words_meet(const Words &x, const Words &y) {
+  const uintptr_t a = (uintptr_t)x.p, b = (uintptr_t)y.p;
+  return a && b && (x.written || y.written) && a < b + (uintptr_t)y.n * 4 && b < a + (uintptr_t)x.n * 4;
+}
 static kvprm_status check_words(const Words *w, int n, const char *fn) {
   for (int i = 0; i < n; ++i) {
     if ((uintptr_t)w[i].p % sizeof(int32_t) != 0) return fail(KVPRM_E_INVALID, "%s: an array not aligned to its elements", fn);
-    for (int k = 0; k < i; ++k) {
-      const uintptr_t a = (uintptr_t)w[i].p, b = (uintptr_t)w[k].p;
-      if (!a || !b || (!w[i].written && !w[k].written)) continue;
-      if (a < b + (uintptr_t)w[k].n * 4 && b < a + (uintptr_t)w[i].n * 4)
-        return fail(KVPRM_E_INVALID, "%s: an array that is written overlaps another", fn);
-    }
+    for (int k = 0; k < i; ++k)
+      if (words_meet(w[i], w[k])) return fail(KVPRM_E_INVALID, "%s: an array that is written overlaps another", fn);
+  }
+  return KVPRM_OK;
+}
+
+// The pools and, for fp8, their scales, which the calls on pages write, lie apart from each other and from the call's
+// arrays.
+static kvprm_status check_pools_apart(const kvprm_handle h, const kvprm_kv_cache *c, const Words *w, int n, const char *fn) {
+  const int64_t tiles = (int64_t)h->dm.layers * c->num_pages * h->dm.nkv;
+  const int64_t words = tiles * (int64_t)(tile_bytes(h->dm.kvdt, h->dm.d) / 4);
+  const Words pool[] = {{c->k_pages, words, true}, {c->v_pages, words, true},
+                        {h->dm.kvdt == 2 ? c->k_scale : nullptr, tiles, true}, {h->dm.kvdt == 2 ? c->v_scale : nullptr, tiles, true}};
+  for (int i = 0; i < 4; ++i) {
+    for (int k = 0; k < i; ++k)
+      if (words_meet(pool[i], pool[k])) return fail(KVPRM_E_INVALID, "%s: the cache's pools or scales overlap", fn);
+    for (int k = 0; k < n; ++k)
+      if (words_meet(pool[i], w[k])) return fail(KVPRM_E_INVALID, "%s: an array overlaps the cache's pools or scales", fn);
   }
   return KVPRM_OK;
 }
@@ -1166,8 +1182,10 @@ kvprm_status kvprm_fork_pages(kvprm_handle h, const kvprm_kv_cache *cache, const
                      {refs, cache->num_pages, false}, {new_refs, cache->num_pages, true}, {result, 4, true},
                      {m ? to->page_table : nullptr, m * to->max_pages, true}, {m ? to->lengths : nullptr, m, true},
                      {m ? to->held : nullptr, m, true}, {workspace, (int64_t)(pages_ws_bytes(cache->num_pages) / 4), true}};
-  if ((st = check_words(w, sizeof w / sizeof *w, fn)) != KVPRM_OK) return st;
+  constexpr int nw = sizeof w / sizeof *w;
+  if ((st = check_words(w, nw, fn)) != KVPRM_OK) return st;
   if ((st = check_pages_ws(cache->num_pages, workspace, ws_bytes, fn)) != KVPRM_OK) return st;
+  if ((st = check_pools_apart(h, cache, w, nw, fn)) != KVPRM_OK) return st;
   HIP_TRY(launch_fork_pages(h->dm, *cache, *from, *to, parent, room, refs, new_refs, result, workspace,
                             (hipStream_t)stream),
           "fork pages");
@@ -1188,8 +1206,10 @@ kvprm_status kvprm_compact_pages(kvprm_handle h, const kvprm_kv_cache *cache, co
   const Words w[] = {{n ? rows->page_table : nullptr, n * rows->max_pages, false}, {n ? rows->held : nullptr, n, false},
                      {n ? new_table : nullptr, n * rows->max_pages, true}, {refs, pages, false}, {new_refs, pages, true},
                      {moved, pages, true}, {result, 4, true}, {workspace, (int64_t)(pages_ws_bytes(pages) / 4), true}};
-  if ((st = check_words(w, sizeof w / sizeof *w, fn)) != KVPRM_OK) return st;
+  constexpr int nw = sizeof w / sizeof *w;
+  if ((st = check_words(w, nw, fn)) != KVPRM_OK) return st;
   if ((st = check_pages_ws(pages, workspace, ws_bytes, fn)) != KVPRM_OK) return st;
+  if ((st = check_pools_apart(h, cache, w, nw, fn)) != KVPRM_OK) return st;
   HIP_TRY(launch_compact_pages(h->dm, *cache, *rows, new_table, refs, new_refs, moved, result, workspace,
                                (hipStream_t)stream),
           "compact pages");

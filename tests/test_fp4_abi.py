@@ -127,3 +127,30 @@ def test_pages_workspace_size(handle):
     _refused(kv.KVPRM_E_INVALID, lambda: f(handle, 0))
     _refused(kv.KVPRM_E_INVALID, lambda: f(None, 4))
     _refused(kv.KVPRM_E_UNSUPPORTED, lambda: f(handle, (1 << 22) + 1))
+
+
+@pytest.mark.parametrize("cdt", ["f32", "bf16", "fp8", "fp4"])
+@pytest.mark.parametrize("call", [_fork, _compact])
+def test_pages_refuse_arrays_in_the_pools(call, cdt):
+    """The pools and their fp8 scales are written: no array or workspace lies in them, nor one over another."""
+    h = _handle(cdt, weight_dtype="f32" if cdt == "f32" else "bf16")
+    tile = {"f32": 64 * 64, "bf16": 32 * 64, "fp8": 16 * 64, "fp4": 17 * 32}[cdt]
+    tiles = 2 * POOL * 2  # layers, pages, kv-heads
+    k, v, ks, vs = (n * FAKE for n in (0x100, 0x200, 0x300, 0x400))
+    end = k + tiles * tile  # the first byte past the keys
+    names = ["ft", "fh", "refs", "new", "result", "tt"] + (["fl", "tl", "th", "parent", "room"] if call is _fork else ["moved"])
+    places = [k, v + 256, end - 4] + ([ks, vs + 4 * tiles - 4] if cdt == "fp8" else [])
+    cache = kv.make_cache(k, v, POOL, ks, vs)
+    try:
+        for at in places:
+            for name in names:
+                _refused(kv.KVPRM_E_INVALID, lambda: call(h, cache=cache, **{name: at}))
+        need = kv.kvprm_workspace_size_pages(h, POOL)
+        for at in (k, v + 256, k - need // 256 * 256 + 256) + ((ks, vs) if cdt == "fp8" else ()):
+            _refused(kv.KVPRM_E_INVALID, lambda: call(h, cache=cache, ws=at))
+        others = [(k, k, ks, vs), (k, end - 16, ks, vs), (end - 16, k, ks, vs)]
+        others += [(k, v, ks, ks), (k, v, end - 4, vs), (k, v, ks, ks + 4 * tiles - 4)] if cdt == "fp8" else []
+        for pools in others:
+            _refused(kv.KVPRM_E_INVALID, lambda: call(h, cache=kv.make_cache(*pools[:2], POOL, *pools[2:])))
+    finally:
+        kv.kvprm_destroy(h)
