@@ -229,9 +229,11 @@ static kvprm_status plan_for(const kvprm_handle h, const kvprm_batch *b, int ran
 // fp32 100 tokens 27.0 / 28.8 but 512 32.7 / 30.1; H = 1024 with 8 kv-heads, 100 tokens, 256 blocks
 // 46.9 / 49.0 but 512 blocks 61.3 / 58.6; 7B shape, 64 candidates of 300 148.8 / 154.8.
 // A 4-bit page takes a wave half the time of a bf16 one to load but the same to compute, and more blocks leave the
-// chunk kernel less to gain: up to 36 pages and 3 more for 8 blocks. One launch / chunks and merge, us: 1 candidate, 8
-// kv-heads of 128: 32 pages 8.4 / 10.1, 48 9.9 / 9.9, 80 12.3 / 9.8; 64 blocks: 48 10.0 / 10.6, 64 11.0 / 11.1, 80 12.6 /
-// 12.0; 256 blocks: 48 11.4 / 15.5, 128 18.0 / 23.3; d_h = 64, 256 blocks: 128 14.4 / 20.2, 64 blocks: 96 11.8 / 11.4.
+// chunk kernel less to gain: up to 36 pages and 3 more for 8 blocks. One launch / chunks and merge (two launches, whose
+// pace varies by 2), us: 1 candidate, 8 kv-heads of 128: 32 pages 8.5 / 11.0-13.2, 40 10.8 / 10.1-12.2, 48 10.7 / 9.8-11.8,
+// 80 13.2 / 9.9-11.9; 64 blocks: 48 10.9 / 10.7-12.2, 60 12.0 / 11.2-12.3, 80 13.4 / 12.5-13.4; 256 blocks: 48 12.5 / 15.5,
+// 96 16.5 / 20.8, 128 19.8 / 24.0; d_h = 64, 256 blocks: 128 15.6 / 20.0, 64 blocks: 60 10.8 / 10.5-11.9, 96 12.5 /
+// 11.6-12.6.
 constexpr int kShortBlocks = 256;
 static int short_pages(const Dims &dm, int blocks) {
   if (dm.kvdt == 3) return std::min(kShortPages4, 36 + blocks * 3 / 8);

@@ -630,8 +630,9 @@ __device__ __forceinline__ uint32_t half_on(uint32_t v) {
 // is read or changed, and the bytes of a value belong to one slot each. The rows of a tile are in registers (16
 // bytes of a row per lane and load; slots that get no row repeat one that does); the lanes that share a group of 32
 // dims find its largest magnitude, and the codes meet in LDS in the stored order.
-// Bound by memory on long prompts: 8 of 16384 to 32768 rows, 4 kv-heads of 128 dims, bf16 (520 MB moved): 103 us, 5.0
-// TB/s (99 with loads and stores past the caches, which the next reader of the pages would pay for). Single tokens of 16
+// Bound by memory on long prompts: 8 of 16384 to 32768 rows, 4 kv-heads of 128 dims, bf16 (528 MB moved): 104 us, 5.1
+// TB/s, fp32 (990 MB) 199 us, 5.0, in calls of this kernel alone (in turn with k_read_kv4 135 us, and
+// that one 84; bf16 99 with loads and stores past the caches, which the next reader of the pages would pay for). Single tokens of 16
 // sequences: 3.7 us, the launch.
 template <int D, typename S>
 __global__ __launch_bounds__(256) void k_write_kv4(RowArgs a) {
@@ -768,7 +769,7 @@ __global__ __launch_bounds__(256) void k_write_kv4(RowArgs a) {
   if (lane < D / 2 && (news >> slot & 1)) out[8 * D + lane] = (char)tb[8 * D + lane];
 }
 
-// k_read_kv for 4-bit tiles. Bound by memory: the same prompts back as rows, 101 us, 5.1 TB/s.
+// k_read_kv for 4-bit tiles. Bound by memory: the same prompts back as rows, 102 us, 5.2 TB/s, as fp32 rows 182 us, 5.4.
 template <int D, typename S>
 __global__ __launch_bounds__(256) void k_read_kv4(RowArgs a) {
   typedef RowMap<D, S> Map;

@@ -32,7 +32,7 @@ struct GroupTable {
   int private_items;                   // chunks of all candidates: full ones and a slot for each last one
   int one_launch;                      // short caches: k_attn_short in place of chunks and merge
   int cshift_prefix, cshift_private;   // chunk lengths (1 << shift pages) of the two kernels
-  int chunk_private;                   // the latter in pages (4-bit caches: any even number up to 64)
+  int chunk_private;                   // the latter in pages (4-bit caches: the lengths of chunk_pages4, even numbers up to 64)
   uint32_t cinv_private;               // ceil(2^32 / chunk_private): x / chunk_private = x * cinv >> 32 for x < 2^20
 };
 

@@ -130,8 +130,8 @@ PrivateChunks private_chunk_rule(const Dims &dm, int n, const int *pages, const 
 // 128): a pair takes 1, 1.5 and 2 on a unit of one, two and three waves (the resident ones; more follow in turn), a
 // wave's start and end 5, the merge 3 for every 1024 waves; at d_h = 64 1, 1.4, 1.8, 5 and 2. 52 batches (eight head
 // layouts, 1 to 64 candidates of up to 32k tokens, equal and ragged): 1.2% above each one's fastest of these lengths in
-// the mean, 8% at most; the fastest power of two is 2.6% above. (The limit on waves that the other types have: 2.1% above
-// the fastest power of two, 18% at most.) All heads in a block were slower wherever the rule of the other types
+// the mean, 6% at most; the fastest power of two is 3.0% above. (The limit on waves that the other types have: 1.8% above
+// the fastest power of two, 12% at most.) All heads in a block were slower wherever the rule of the other types
 // would take them.
 int chunk_pages4(const Dims &dm, int n, const int *pages, const int *slots, bool known) {
   static const int lengths[] = {64, 56, 48, 40, 32, 28, 24, 20, 16, 14, 12, 10, 8, 6, 4};

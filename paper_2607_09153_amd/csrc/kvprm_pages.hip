@@ -1,6 +1,7 @@
 // Pages of the cache for gfx950: rows of a page table forked into others with copy-on-write (kvprm_fork_pages), and the
 // live pages of a pool moved into its lowest ids (kvprm_compact_pages). Both plan on the device from holders' counts
-// and tables, in a few short launches, and end with one launch that copies the pages of all layers.
+// and tables and copy the pages of all layers: pools of up to kOnePages pages in one launch whose blocks plan each for
+// itself (k_fork_one, k_compact_one), larger ones in a few short launches that share a plan in the workspace.
 #include <hip/hip_runtime.h>
 
 #include "kvprm_attn_common.h"
@@ -416,7 +417,12 @@ __global__ __launch_bounds__(256) void k_compact_move(PageArgs a) {
 // share of the pages. Nothing that a block reads is written by another, so that no block waits for one. Against the
 // launches above, whose plan is spread over the blocks (fork / compact, us): a beam of 64 rows of 290 pages in a pool of
 // 2270, 31 copies of 917 KB: 24 instead of 41; 4 rows of 10 pages 7 / 7, 20 / 19; 16384 pages, 64 rows of 200 entries
-// 19 / 26, 31 / 39; 17900 pages, 256 rows of 300 entries 42 / 35, 56 / 33.
+// 19 / 26, 31 / 39. The entries, which every block walks, are limited where forks cross (pages of 2 KB, a copy for every
+// second row; one launch / several): 8000 pages, 64 rows of 512 19 / 35, 256 rows of 100, 300 and 512 19 / 41, 35 / 51 and
+// 50 / 58; 16384 pages, 64 of 512 23 / 34, 256 of 100, 300, 512 23 / 40, 38 / 48, 52 / 52. Compactions of such small pages
+// cross earlier (8000 pages, 256 rows of 300 and 512 30 / 34 and 44 / 33; 16384 pages 37 / 36, 50 / 36) but not those of a
+// model's (28 layers, 4 kv-heads of 128 in 4 bits, 243 KB a page: 197 / 267, 202 / 256; 388 / 515, 396 / 506), whose
+// copies are the call.
 constexpr int kOnePages = 16384, kOneThreads = 1024;
 constexpr int64_t kOneEntries = 1 << 17;  // entries of the rows
 

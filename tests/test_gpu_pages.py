@@ -280,3 +280,16 @@ def test_many_copies_in_one_launch(cdt, layers, children):
     room = [int(r) for r in rng.choice([0, 1, 16, 40], size=children)]
     status, _, lens, _ = pool.fork(rows, lengths, parent, room, refs, 9, 12)
     assert status == 0 and sum(n % 16 > 0 for n in lens) > children // 2
+
+
+@pytest.mark.parametrize("pages,n,width", [(900, 140, 1000), (1200, 256, 514)])
+def test_wide_tables_of_small_pools(pages, n, width):
+    """Tables of more entries than the one-launch calls take, over pools that they would take."""
+    _say("wide", pages, n, width)
+    pool = Pool("fp8", pages, n, layers=2)
+    rng = np.random.default_rng(n)
+    rows, lengths, refs = _case(rng, pages, n, 30, 2, spare=False)
+    parent = [int(p) for p in rng.integers(-1, n // 2, size=n)]
+    status, rows, lengths, refs = pool.fork(rows, lengths, parent, None, refs, width, width)
+    assert status == 0
+    assert _compact(pool, rows, refs, width) == 0
