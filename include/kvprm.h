@@ -210,7 +210,8 @@ kvprm_status kvprm_score_static(kvprm_handle h, const kvprm_kv_cache *cache,
  * q: device fp32 [B][n_q][d_h] (already rotated); k_self, v_self: device fp32 [B][n_kv][d_h];
  * o: device fp32 [B][n_q][d_h]. The prefix-sharing hint is honoured as in kvprm_score.
  * Over 4-bit caches a query's value meets the cached keys with an error of at most 2^-29 of the largest of its 32 dims (32 i
- * to 32 i + 31; d_h = 64: 2^-33), those of a hinted prefix and other caches' with 2^-24 of itself. */
+ * to 32 i + 31; d_h = 64: 2^-33) or 2^-92, those of a hinted prefix and other caches' with 2^-24 of itself. A score that
+ * passes fp32's range downwards is a weight of 0. */
 kvprm_status kvprm_attention(kvprm_handle h, const kvprm_kv_cache *cache, const kvprm_batch *batch,
                              int32_t layer, const float *q, const float *k_self,
                              const float *v_self, void *workspace, size_t ws_bytes, float *o,

@@ -3,6 +3,7 @@
 // (k_prefix_mx), the log-sum-exp merge with the token's own key (k_merge_mx), and the whole step of
 // a short cache in one launch (k_attn_short, k_attn_short_f32).
 #include <hip/hip_runtime.h>
+#include <float.h>
 #include <math.h>
 #include <string.h>
 
@@ -279,6 +280,11 @@ __device__ __forceinline__ void walk_pages(const AttnArgs &a, int b, int j, int 
 // chunk's last pair alone.
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 constexpr int kTerms4 = 7;
+// The products give scores times 2^-32, so that terms of unlike sign do not overflow on the way to a score that does (an
+// infinity of each sign would be a NaN): a stored key can be as large as fp32's range. What is left of a value, times log2(e)
+// / sqrt(d_h), below 2^-95 is lost.
+constexpr int kScoreShift4 = 32;
+constexpr float kScoreUnit4 = 4294967296.f;
 
 template <int D>
 struct Query4 {
@@ -310,13 +316,13 @@ __device__ __forceinline__ void query_terms4(const float *qr, bool present, floa
   for (int i = 0; i < 16; ++i)
     top = max(top, max(__float_as_uint(even[i]) & 0x7FFFFFFFu, __float_as_uint(odd[i]) & 0x7FFFFFFFu));
   // the smallest power of two s with 7.5 s >= the largest (7.5 = 1.875 * 2^2), kept where every term's scale is one
-  int e = max((int)(top >> 23) - 2 + ((top & 0x7FFFFFu) > 0x700000u), 4 * TERMS);
+  int e = max((int)(top >> 23) - 2 + ((top & 0x7FFFFFu) > 0x700000u), 4 * TERMS + kScoreShift4);
   uint32_t bytes[TERMS];
   u32x6 term[TERMS];
 #pragma unroll
   for (int k = 0; k < TERMS; ++k) {
     const float s = __uint_as_float((uint32_t)(e - 4 * k) << 23);
-    bytes[k] = top >= 0x7F800000u ? 255u : (uint32_t)(e - 4 * k);
+    bytes[k] = top >= 0x7F800000u ? 255u : (uint32_t)(e - 4 * k - kScoreShift4);
     term[k] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, s);  // even and odd dims side by side
     if (k + 1 == TERMS) break;
     const f32x32 back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(term[k], s);
@@ -385,7 +391,7 @@ __device__ __forceinline__ void walk_pages4(const AttnArgs &a, int b, int j, int
   load_pair(1, r1);
   __builtin_amdgcn_sched_barrier(0);
   Query4<D> q;
-  query_terms4<D>(qr, colv, kLog2e / sqrtf((float)D), lane, q);  // scores in log2 units
+  query_terms4<D>(qr, colv, kLog2e / sqrtf((float)D), lane, q);  // scores in log2 units, times 2^-32; m_run as well here
   auto compute = [&](int pp, const PairRaw4<D> &r, auto tail) {
     constexpr bool TAIL = decltype(tail)::value;
     floatx4 sa, sb;
@@ -403,7 +409,8 @@ __device__ __forceinline__ void walk_pages4(const AttnArgs &a, int b, int j, int
     for (int i = 1; i < 8; ++i) mx = larger(mx, s[i]);
     mx = column_reduce(mx, larger);
     if (__any(!(mx <= m_run))) {  // (a NaN among a column's scores becomes its maximum and stays)
-      const float mn = larger(m_run, mx), alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - mn);
+      const float mn = larger(m_run, mx);
+      const float alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run - mn) * kScoreUnit4);
       m_run = mn;
       l_run *= alpha;
 #pragma unroll
@@ -411,10 +418,10 @@ __device__ __forceinline__ void walk_pages4(const AttnArgs &a, int b, int j, int
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[nb][i] *= alpha;
     }
-    const float ms = m_run == -INFINITY ? 0.f : m_run;  // (all scores overflowed so far: weights of 0)
+    const float ms = fmaxf(m_run * kScoreUnit4, -FLT_MAX);  // (all scores overflowed so far: weights of 0)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      s[i] = __builtin_amdgcn_exp2f(s[i] - ms);
+      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], kScoreUnit4, -ms));
       l_run += s[i];
     }
     uint32_t p[3][4];
@@ -465,6 +472,7 @@ __device__ __forceinline__ void walk_pages4(const AttnArgs &a, int b, int j, int
     r0 = r1;
   }
   compute(last, r0, std::integral_constant<bool, true>{});
+  m_run *= kScoreUnit4;
 }
 
 // Which candidate and chunk block `id` of the private pages' grid has (see k_attn_mx), its length and shared pages.
@@ -814,11 +822,17 @@ __global__ __launch_bounds__(64 * kPrefixWaves) void k_prefix_mx(AttnArgs a) {
   {
     QueryRaw<D> qraw;
     load_query<KVT, D>(a.q + ((size_t)bcand * nq + (size_t)j * g + hh) * D, cq, qraw);
+    if (KVT == 3)  // (see kScoreShift4)
+#pragma unroll
+      for (int kk = 0; kk < NKB; ++kk) {
+        qraw.v[kk][0] = qraw.v[kk][0] * (1.f / kScoreUnit4);
+        qraw.v[kk][1] = qraw.v[kk][1] * (1.f / kScoreUnit4);
+      }
     query_ops<D>(qraw, present, qhi, qmd, qlo);
   }
   stash(0, s0);
   __syncthreads();
-  const float rs = kLog2e / sqrtf((float)D);  // scores in log2 units
+  const float rs = (KVT == 3 ? kScoreUnit4 : 1.f) * kLog2e / sqrtf((float)D);  // scores in log2 units
   float m_run = -INFINITY, l_run = 0.f;
   floatx4 acc[NDB];
 #pragma unroll

@@ -45,7 +45,8 @@ def _fill(cdt, nq, nkv, d, lengths, large, seed, shared=0):
     return c
 
 
-def _check(c, cdt, lengths, x, got, what):
+def _check(c, cdt, lengths, x, got, what, size=1.0):
+    """size: that of the queries beside N(0, 1), with which the scores' error grows."""
     nq, nkv, d = c.shape
     assert np.all(np.isfinite(got)), (what, np.argwhere(~np.isfinite(got))[:4])
     for b, n in enumerate(lengths):
@@ -56,7 +57,7 @@ def _check(c, cdt, lengths, x, got, what):
             K, V = np.concatenate([ck[:, j], x[1][b, j][None]]), np.concatenate([cv[:, j], x[2][b, j][None]])
             want = ko.attention(x[0][b, h].astype(np.float64), K, V)
             off = np.abs(got[b, h] - want).max()
-            assert off <= (2e-5 + 2.0 ** -16) * np.abs(V).max(), (what, b, h, off)
+            assert off <= (2e-5 * size + 2.0 ** -16) * np.abs(V).max(), (what, b, h, off)
 
 
 def _inputs(c, n, seed):
@@ -98,3 +99,21 @@ def test_shared_prefix(cdt, large):
     x = _inputs(c, 4, 5)
     hint = c.m.make_batch(4, c.dtab.data_ptr(), c.width, c.dlen.data_ptr(), SHARED, [0, 4], [320])
     _check(c, cdt, SHARED, x, _run(c, x, hint), "hint")
+
+
+@pytest.mark.parametrize("lo,hi", [(100, 100), (11, 11), (50, 150), (0, 1000), (1e4, 1e6)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_queries_far_past_the_range(d, lo, hi):
+    """4-bit caches: a query is summed in terms, whose parts of such a score pass the range with either sign."""
+    print("case: far", d, lo, hi, flush=True)
+    for lengths, large in ((LENGTHS, LARGE), (LENGTHS[:8], LARGE[:8])):
+        c = _fill("fp4", 4, 2, d, lengths, large, d)
+        x = _inputs(c, len(lengths), d)
+        x[0] = np.random.default_rng(7).uniform(lo, hi, size=x[0].shape).astype(np.float32)
+        batch = c.m.make_batch(len(lengths), c.dtab.data_ptr(), c.width, c.dlen.data_ptr(), lengths)
+        _check(c, "fp4", lengths, x, _run(c, x, batch), len(lengths), size=hi)
+    c = _fill("fp4", 4, 2, d, SHARED, [32] * 4, 3, shared=320)
+    x = _inputs(c, 4, 5)
+    x[0] = np.random.default_rng(8).uniform(lo, hi, size=x[0].shape).astype(np.float32)
+    hint = c.m.make_batch(4, c.dtab.data_ptr(), c.width, c.dlen.data_ptr(), SHARED, [0, 4], [320])
+    _check(c, "fp4", SHARED, x, _run(c, x, hint), "hint", size=hi)
