@@ -280,11 +280,6 @@ __device__ __forceinline__ void walk_pages(const AttnArgs &a, int b, int j, int 
 // chunk's last pair alone.
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 constexpr int kTerms4 = 7;
-// The products give scores times 2^-32, so that terms of unlike sign do not overflow on the way to a score that does (an
-// infinity of each sign would be a NaN): a stored key can be as large as fp32's range. What is left of a value, times log2(e)
-// / sqrt(d_h), below 2^-95 is lost.
-constexpr int kScoreShift4 = 32;
-constexpr float kScoreUnit4 = 4294967296.f;
 
 template <int D>
 struct Query4 {

@@ -108,6 +108,12 @@ __device__ __forceinline__ void unpack_pair(const PairRaw<D> &r, uint4 *KA, uint
 
 // ---- 4-bit tiles (layout: see kvprm_kv_cache)
 
+// Products of a query in several terms give scores times 2^-32, so that terms of unlike sign do not overflow on the way to
+// a score that does (an infinity of each sign would be a NaN): a stored key can be as large as fp32's range. What
+// is left of a value, times log2(e) / sqrt(d_h), below 2^-95 is lost.
+constexpr int kScoreShift4 = 32;
+constexpr float kScoreUnit4 = 4294967296.f;
+
 // N = 8 or 16 bytes into the low words of 16.
 template <int N, bool STREAM>
 __device__ __forceinline__ uint4 load_bytes(const char *p) {

@@ -396,6 +396,9 @@ __global__ __launch_bounds__(64 * kTreeWaves, KVT == 3 ? 2 : 1) void k_tree(Tree
             float v[8];
             load4((const float *)qr + dim, v);
             load4((const float *)qr + dim + 4, v + 4);
+            if (KVT == 3)  // (see kScoreShift4)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[e] *= 1.f / kScoreUnit4;
             uint32_t t[3][4];
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -413,6 +416,7 @@ __global__ __launch_bounds__(64 * kTreeWaves, KVT == 3 ? 2 : 1) void k_tree(Tree
         constexpr bool TAIL = decltype(masked)::value;
         if constexpr (KVT == 3) {
           const int left = L - (first + 2 * (w + W * i)) * kPage - 4 * cq;  // (as below)
+          const float rs4 = QT == 1 ? rs : rs * kScoreUnit4;
           floatx4 sa[NC], sb[NC];
 #pragma unroll
           for (int ct = 0; ct < NC; ++ct) sa[ct] = sb[ct] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -434,8 +438,8 @@ __global__ __launch_bounds__(64 * kTreeWaves, KVT == 3 ? 2 : 1) void k_tree(Tree
             float p[8];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              p[e] = sa[ct][e] * rs;
-              p[4 + e] = sb[ct][e] * rs;
+              p[e] = sa[ct][e] * rs4;
+              p[4 + e] = sb[ct][e] * rs4;
               if (TAIL) {
                 p[e] = left > e ? p[e] : -INFINITY;
                 p[4 + e] = left > 16 + e ? p[4 + e] : -INFINITY;

@@ -12,6 +12,7 @@ from oracle import growing_cache as gc
 from oracle import kvprm_oracle as ko
 
 import fp4_common
+from test_gpu_fp4_tree import Draft
 from test_gpu_tree import LAYER, Case
 
 pytestmark = pytest.mark.gpu
@@ -117,3 +118,28 @@ def test_queries_far_past_the_range(d, lo, hi):
     x[0] = np.random.default_rng(8).uniform(lo, hi, size=x[0].shape).astype(np.float32)
     hint = c.m.make_batch(4, c.dtab.data_ptr(), c.width, c.dlen.data_ptr(), SHARED, [0, 4], [320])
     _check(c, "fp4", SHARED, x, _run(c, x, hint), "hint", size=hi)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lo,hi", [(0.3, 0.4), (100, 100), (50, 150), (0, 1000)])
+@pytest.mark.parametrize("counts", [3, 60])
+@pytest.mark.parametrize("d", [64, 128])
+def test_drafts(d, counts, lo, hi, dtype):
+    """Drafted tokens over such 4-bit caches (within the bound of test_gpu_fp4_tree.py, times the queries' size)."""
+    print("case: drafts", d, counts, lo, hi, dtype, flush=True)
+    nq, nkv, lengths, large = 4, 2, LENGTHS[1:9], LARGE[1:9]
+    c = _fill("fp4", nq, nkv, d, lengths, large, d)
+    dr = Draft(c, dtype, [counts] * len(lengths), "chain", seed=d)
+    q = np.random.default_rng(counts).uniform(lo, hi, size=(dr.rows, nq * d)).astype(np.float32)
+    dr.x[:dr.rows, :nq * d] = torch.from_numpy(q).to(dr.x.dtype)
+    dr.dx = dr.x.cuda()
+    got = dr.run()[:dr.rows, :nq * d].double().numpy()
+    assert np.all(np.isfinite(got)), np.argwhere(~np.isfinite(got))[:4]
+    for b, n in enumerate(lengths):
+        rows = slice(b * counts, (b + 1) * counts)
+        x = dr.x[rows, :(nq + 2 * nkv) * d].double().numpy().reshape(counts, nq + 2 * nkv, d)
+        ck, cv = (c.cached(p, LAYER, b) for p in (0, 1))
+        want = gc.tree_attention(x[:, :nq], x[:, nq:nq + nkv], x[:, nq + nkv:], ck, cv, dr.sees[b]).reshape(counts, nq * d)
+        big = max(np.abs(cv).max(), np.abs(x[:, nq + nkv:]).max())
+        tol = 2e-5 * max(hi, 1) * big + ((2.0 ** -16) * big + 2.0 ** -8 * np.abs(want) if dtype == "bf16" else 0)
+        assert np.all(np.abs(got[rows] - want) <= tol), (b, np.abs(got[rows] - want).max(), big)
